@@ -437,6 +437,110 @@ retro_status retro_project_out(const float* o, int32_t rows, int32_t k, const vo
 retro_status retro_project_f32(const float* x, int32_t rows, int32_t k, const float* w,
                                int32_t n, float* y, int32_t accumulate, void* stream);
 
+/* ---- Prompts, chunks of prompts and rotated positions ---------------------------
+ * What precedes and surrounds the retrospective steps in a model whose keys and
+ * queries carry their positions: per-head norms and the rotation, the storage of
+ * a ragged batch of rows with both applied on the way, and the attention of these
+ * rows over everything stored.  Of retro_dims these calls use batch,
+ * num_kv_heads, group, head_dim, page_size, max_pages, num_phys_pages, dtype and
+ * sm_scale.  Rows are tokens: queries [rows][h_q][d], keys and values
+ * [rows][h_k][d] in dtype, where `*_stride` elements lie between the rows of an
+ * input (parts of one projection's output: its row length; else heads * d).
+ * Outputs are contiguous.  Every pointer is a device address, 16-byte aligned
+ * except the arrays of int32 and lse, and every stride a multiple of 16 bytes and
+ * no less than heads * d (RETRO_EINVAL otherwise). */
+
+/* Norm and rotation.  For a head's vector x at position p:
+ *   y = x * (mean(x^2) + eps)^(-1/2) * weight      (weight NULL: y = x)
+ * and, with (c, s) = table[p][i], pair i of y's first rot_dim elements becomes
+ *   (a, b) -> (a c - b s, b c + a s)
+ * in fp32, rounded once to dtype.  rot_dim: a multiple of 16 up to d; 0 leaves
+ * the rotation out (table may be NULL then). */
+typedef struct retro_rotary {
+  const float* table;   /* [positions][rot_dim / 2][2] cosine, sine (retro_rotary_table)  */
+  int32_t positions;    /* rows of table                                                */
+  int32_t rot_dim;      /* rotated elements of a head, the leading ones                  */
+  int32_t interleaved;  /* 0: pair i is (i, i + rot_dim / 2); 1: it is (2 i, 2 i + 1)     */
+  float eps;            /* >= 0, finite                                                 */
+  const void* q_norm;   /* [d] dtype, weights of the queries' norm; NULL: none           */
+  const void* k_norm;   /* [d] dtype, weights of the keys' norm; NULL: none              */
+} retro_rotary;
+
+/* A ragged batch of rows: sequence b has the rows row_start[b] .. row_start[b+1]-1
+ * (ascending, row_start[0] >= 0, row_start[batch] <= n_rows; an empty range is a
+ * sequence that takes no part), row row_start[b] + j at position start_pos[b] + j.
+ * A sequence with start_pos[b] < 0 takes no part.  Rows that belong to no
+ * sequence (in front of row_start[0], at or behind row_start[batch]) are not read
+ * and their outputs stay as they were, so that a captured call can be replayed
+ * for fewer rows.  n_rows: rows that the buffers hold; what reaches past it is cut. */
+typedef struct retro_chunk {
+  const int32_t* row_start;  /* [batch + 1] */
+  const int32_t* start_pos;  /* [batch]; not the cache's seq_lens array */
+  int32_t n_rows;
+} retro_chunk;
+
+/* Fills table [positions][rot_dim / 2][2] fp32 with cosine and sine of
+ * p * base^(-2 i / rot_dim), computed in fp64 and rounded once.  rot_dim a
+ * multiple of 16 in 16 .. 128, base > 0 and finite (RETRO_EINVAL otherwise).  A program
+ * whose frequencies are scaled in some other way fills its own table. */
+retro_status retro_rotary_table(float* table, int32_t positions, int32_t rot_dim, double base,
+                                void* stream);
+
+/* Norm and rotation of the queries and keys of `rows` rows at `positions` [rows]
+ * int32: q -> q_out [rows][h_q][d], k -> k_out [rows][h_k][d].  q or k may be NULL
+ * (then its output is not looked at).  q_out may be q, and k_out k, where their
+ * strides are h_q * d and h_k * d.  A row of negative position is not written; the
+ * rotated elements of one at or past rotary->positions become NaN.  positions may
+ * be NULL where rot_dim is 0.  rows == 0 does nothing.  E.g. for the window rows
+ * of a step: rotated queries for retro_step, rotated keys for retro_update_kv. */
+retro_status retro_rotate_qk(const retro_dims* dims, const retro_rotary* rotary,
+                             const int32_t* positions, int32_t rows, const void* q,
+                             int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                             void* k_out, void* stream);
+
+/* AppendKV (Alg. 1) of a ragged batch: what retro_append_kv does for row after
+ * row of every sequence, with keys normalised and rotated as `rotary` says (and
+ * the digests those of the stored keys), and queries likewise into q_out
+ * [n_rows][h_q][d] (q NULL: no queries).  start_pos[b] must equal seq_lens[b]
+ * for every sequence with rows; seq_lens[b] becomes start_pos[b] + the rows
+ * appended, and last_loaded of the pages that receive a key becomes step - 1 for
+ * every head (step 0, for a prompt before the first decode step, leaves it at its
+ * initial -1).  The first row whose page is not mapped is dropped with every
+ * later row of its sequence (slots past the new seq_lens, and digests and last_loaded of
+ * pages past it, are then unspecified).  Queries are written for dropped rows
+ * too (NaN past rotary->positions).  With rot_dim > 0, rotary->positions must be
+ * at least max_pages * P (RETRO_EINVAL).  n_rows == 0 does nothing. */
+retro_status retro_append_kv_rotary(const retro_dims* dims, int32_t step,
+                                    const retro_kv_cache* cache, const retro_chunk* chunk,
+                                    const retro_rotary* rotary, const void* q, int64_t q_stride,
+                                    const void* k, int64_t k_stride, const void* v,
+                                    int64_t v_stride, void* q_out, void* stream);
+
+/* Bytes of workspace that retro_chunk_attend needs for n_rows rows.  Scratch:
+ * nothing in it outlives a call, it needs no initialisation, and one call at a
+ * time may use it. */
+retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, size_t* bytes);
+
+/* Dense causal attention of a ragged batch over the paged cache: row at position
+ * p of sequence b, query head g of KV head h, takes every stored token i of the
+ * sequence with i <= p and i < seq_lens[b]:
+ *   out = sum_i softmax_i(sm_scale q . k_i) v_i,  lse = ln sum_i exp(sm_scale q . k_i)
+ * out [n_rows][h_q][d] dtype, lse [n_rows][h_q] fp32 (may be NULL).  A row that no
+ * token is left for gives (0, -inf).  The chunk's own keys and values are stored
+ * first (retro_append_kv_rotary, retro_prefill_kv, retro_append_kv_tokens); one row per
+ * sequence is dense decoding.  Tokens of pages that are not mapped are left out.
+ * Products and sums in fp32; for bf16 the softmax weights are rounded to bf16 for
+ * their product with the values (sums and log-normalisers take the unrounded ones).
+ * NaN and infinities as in retro_decode_attend: a NaN score, or one of +inf,
+ * makes its row NaN; a NaN or infinite value of a stored token can reach every
+ * row of its sequence and KV head in the same call; slots past seq_lens never count, whatever
+ * they hold.  Reads the cache only.  n_rows == 0 does nothing; more than 65535
+ * sequences, or n_rows * h_q * d >= 2^40, is RETRO_EUNSUPPORTED. */
+retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* cache,
+                                const retro_chunk* chunk, const void* q, int64_t q_stride,
+                                void* out, float* lse, void* workspace, size_t ws_bytes,
+                                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

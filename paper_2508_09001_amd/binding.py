@@ -26,7 +26,9 @@ EXPORTED = ("retro_version", "retro_status_string", "retro_k_max", "retro_worksp
             "retro_decode_attend", "retro_decode_attend_partials", "retro_step_attend_partials",
             "retro_copy_scores", "retro_merge_output_cache", "retro_step", "retro_step_noalloc",
             "retro_step_launches", "retro_attend_plan", "retro_pack_weight",
-            "retro_project_qkv", "retro_project_qkv_update", "retro_project_out", "retro_project_f32")
+            "retro_project_qkv", "retro_project_qkv_update", "retro_project_out", "retro_project_f32",
+            "retro_rotary_table", "retro_rotate_qk", "retro_append_kv_rotary",
+            "retro_chunk_workspace_size", "retro_chunk_attend")
 
 
 class RetroError(RuntimeError):
@@ -55,6 +57,16 @@ class Selection(C.Structure):
 
 class OutputCache(C.Structure):
     _fields_ = [("o_cache", C.c_void_p), ("lse_cache", C.c_void_p)]
+
+
+class Rotary(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("eps", C.c_float), ("q_norm", C.c_void_p),
+                ("k_norm", C.c_void_p)]
+
+
+class Chunk(C.Structure):
+    _fields_ = [("row_start", C.c_void_p), ("start_pos", C.c_void_p), ("n_rows", C.c_int32)]
 
 
 _lib = None
@@ -106,6 +118,15 @@ def load_library(path: str = LIB_PATH):
         "retro_project_f32": ([P, i32, i32, P, i32, P, i32, P], C.c_int),
         "retro_project_qkv_update": ([D, C.POINTER(KVCache), P, i32, P, i32, P, P, P, P],
                                      C.c_int),
+        "retro_rotary_table": ([P, i32, i32, C.c_double, P], C.c_int),
+        "retro_rotate_qk": ([D, C.POINTER(Rotary), P, i32, P, C.c_int64, P, C.c_int64, P, P, P],
+                            C.c_int),
+        "retro_append_kv_rotary": ([D, i32, C.POINTER(KVCache), C.POINTER(Chunk),
+                                    C.POINTER(Rotary), P, C.c_int64, P, C.c_int64, P, C.c_int64,
+                                    P, P], C.c_int),
+        "retro_chunk_workspace_size": ([D, i32, C.POINTER(C.c_size_t)], C.c_int),
+        "retro_chunk_attend": ([D, C.POINTER(KVCache), C.POINTER(Chunk), P, C.c_int64, P, P, P,
+                                C.c_size_t, P], C.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -289,3 +310,40 @@ def retro_project_qkv_update(dims: Dims, cache: KVCache, x, k: int, w_packed, n_
                                                    _ptr(w_packed), n_update, _ptr(q),
                                                    _ptr(k_new), _ptr(v_new), _stream(stream)),
            "retro_project_qkv_update")
+
+
+def retro_rotary_table(table, positions: int, rot_dim: int, base: float, stream=None) -> None:
+    _check(load_library().retro_rotary_table(_ptr(table), positions, rot_dim, base,
+                                             _stream(stream)), "retro_rotary_table")
+
+
+def retro_rotate_qk(dims: Dims, rotary: Rotary, positions, rows: int, q, q_stride: int, k,
+                    k_stride: int, q_out, k_out, stream=None) -> None:
+    _check(load_library().retro_rotate_qk(C.byref(dims), C.byref(rotary), _ptr(positions), rows,
+                                          _ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_out),
+                                          _ptr(k_out), _stream(stream)), "retro_rotate_qk")
+
+
+def retro_append_kv_rotary(dims: Dims, step: int, cache: KVCache, chunk: Chunk, rotary: Rotary,
+                           q, q_stride: int, k, k_stride: int, v, v_stride: int, q_out,
+                           stream=None) -> None:
+    _check(load_library().retro_append_kv_rotary(C.byref(dims), step, C.byref(cache),
+                                                 C.byref(chunk), C.byref(rotary), _ptr(q),
+                                                 q_stride, _ptr(k), k_stride, _ptr(v), v_stride,
+                                                 _ptr(q_out), _stream(stream)),
+           "retro_append_kv_rotary")
+
+
+def retro_chunk_workspace_size(dims: Dims, n_rows: int) -> int:
+    n = C.c_size_t(0)
+    _check(load_library().retro_chunk_workspace_size(C.byref(dims), n_rows, C.byref(n)),
+           "retro_chunk_workspace_size")
+    return n.value
+
+
+def retro_chunk_attend(dims: Dims, cache: KVCache, chunk: Chunk, q, q_stride: int, out, lse,
+                       workspace, ws_bytes: int, stream=None) -> None:
+    _check(load_library().retro_chunk_attend(C.byref(dims), C.byref(cache), C.byref(chunk),
+                                             _ptr(q), q_stride, _ptr(out), _ptr(lse),
+                                             _ptr(workspace), ws_bytes, _stream(stream)),
+           "retro_chunk_attend")

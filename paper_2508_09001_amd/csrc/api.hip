@@ -2,8 +2,11 @@
 // launch sequences of each call.  Nothing here allocates device memory.
 #include <math.h>
 
+#include <initializer_list>
+
 #include "internal.h"
 #include "proj.h"
+#include "rotary.h"
 
 namespace retro {
 
@@ -483,6 +486,116 @@ retro_status retro_step(const retro_dims* dims, int32_t step, const void* q_wind
     e = retro::launch_combine_merge(ga, step, 2, o_ws, l_ws, sel->num_selected, nullptr, nullptr,
                                     nullptr, nullptr, ocache, o_out, lse_out, cache, s);
   return from_hip(e);
+}
+
+}  // extern "C"
+
+namespace {
+
+bool aligned16(std::initializer_list<const void*> ps) {
+  uintptr_t bits = 0;
+  for (const void* p : ps) bits |= reinterpret_cast<uintptr_t>(p);
+  return (bits & 15u) == 0;
+}
+
+// an input of rows of `heads` vectors of d elements, whole 16-byte pieces
+bool rows_ok(const Geometry& g, const void* p, int64_t stride, int heads) {
+  return p && stride >= (int64_t)heads * g.D && stride % (16 / g.elt) == 0 && aligned16({p});
+}
+
+bool rotary_ok(const Geometry& g, const retro_rotary* r) {
+  return r && r->rot_dim >= 0 && r->rot_dim <= g.D && r->rot_dim % 16 == 0 &&
+         (r->interleaved == 0 || r->interleaved == 1) && r->eps >= 0.f && !isinf(r->eps) &&
+         (r->rot_dim == 0 || (r->table && r->positions > 0)) &&
+         aligned16({r->table, r->q_norm, r->k_norm});
+}
+
+bool chunk_ok(const retro_kv_cache* cache, const retro_chunk* c) {
+  return c && c->row_start && c->start_pos && c->n_rows >= 0 && c->start_pos != cache->seq_lens;
+}
+
+}  // namespace
+
+extern "C" {
+
+retro_status retro_rotary_table(float* table, int32_t positions, int32_t rot_dim, double base,
+                                void* stream) {
+  if (!table || !aligned16({table}) || positions < 1 || rot_dim < 16 || rot_dim > 128 ||
+      rot_dim % 16 || !(base > 0) || isinf(base))
+    return RETRO_EINVAL;
+  return from_hip(retro::launch_rotary_table(table, positions, rot_dim, base, (hipStream_t)stream));
+}
+
+retro_status retro_rotate_qk(const retro_dims* dims, const retro_rotary* rotary,
+                             const int32_t* positions, int32_t rows, const void* q,
+                             int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                             void* k_out, void* stream) {
+  Geometry g;
+  retro_status st = retro::make_geometry(dims, &g);
+  if (st != RETRO_OK) return st;
+  if (!rotary_ok(g, rotary) || rows < 0) return RETRO_EINVAL;
+  if (rows == 0) return RETRO_OK;
+  if ((!q && !k) || (rotary->rot_dim && !positions)) return RETRO_EINVAL;
+  if (q && (!rows_ok(g, q, q_stride, g.hq) || !rows_ok(g, q_out, (int64_t)g.hq * g.D, g.hq) ||
+            (q == q_out && q_stride != (int64_t)g.hq * g.D)))
+    return RETRO_EINVAL;
+  if (k && (!rows_ok(g, k, k_stride, g.hk) || !rows_ok(g, k_out, (int64_t)g.hk * g.D, g.hk) ||
+            (k == k_out && k_stride != (int64_t)g.hk * g.D)))
+    return RETRO_EINVAL;
+  if (!retro::rotate_qk_supported(g, rows, q, k)) return RETRO_EUNSUPPORTED;
+  return from_hip(retro::launch_rotate_qk(g, *rotary, positions, rows, q, q_stride, k, k_stride,
+                                          q_out, k_out, (hipStream_t)stream));
+}
+
+retro_status retro_append_kv_rotary(const retro_dims* dims, int32_t step,
+                                    const retro_kv_cache* cache, const retro_chunk* chunk,
+                                    const retro_rotary* rotary, const void* q, int64_t q_stride,
+                                    const void* k, int64_t k_stride, const void* v,
+                                    int64_t v_stride, void* q_out, void* stream) {
+  Geometry g;
+  retro_status st = prepare(dims, step, &g);
+  if (st != RETRO_OK) return st;
+  if (!cache_ok(cache) || !chunk_ok(cache, chunk) || !rotary_ok(g, rotary)) return RETRO_EINVAL;
+  if (rotary->rot_dim && rotary->positions < (int64_t)g.max_pages * g.P) return RETRO_EINVAL;
+  if (chunk->n_rows == 0) return RETRO_OK;
+  if (!rows_ok(g, k, k_stride, g.hk) || !rows_ok(g, v, v_stride, g.hk) ||
+      !aligned16({cache->k_cache, cache->v_cache}))
+    return RETRO_EINVAL;
+  if (q && (!rows_ok(g, q, q_stride, g.hq) || !rows_ok(g, q_out, (int64_t)g.hq * g.D, g.hq) ||
+            (q == q_out && q_stride != (int64_t)g.hq * g.D)))
+    return RETRO_EINVAL;
+  if (!retro::append_rotary_supported(g, chunk->n_rows)) return RETRO_EUNSUPPORTED;
+  return from_hip(retro::launch_append_rotary(g, step, *cache, *chunk, *rotary, q, q_stride, k,
+                                              k_stride, v, v_stride, q_out, (hipStream_t)stream));
+}
+
+retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, size_t* bytes) {
+  Geometry g;
+  if (!bytes || n_rows < 0) return RETRO_EINVAL;
+  retro_status st = retro::make_geometry(dims, &g);
+  if (st != RETRO_OK) return st;
+  if (!retro::chunk_attend_supported(g, n_rows)) return RETRO_EUNSUPPORTED;
+  *bytes = retro::chunk_workspace(g, n_rows);
+  return RETRO_OK;
+}
+
+retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* cache,
+                                const retro_chunk* chunk, const void* q, int64_t q_stride,
+                                void* out, float* lse, void* workspace, size_t ws_bytes,
+                                void* stream) {
+  Geometry g;
+  retro_status st = retro::make_geometry(dims, &g);
+  if (st != RETRO_OK) return st;
+  if (!cache_ok(cache) || !chunk_ok(cache, chunk)) return RETRO_EINVAL;
+  if (chunk->n_rows == 0) return RETRO_OK;
+  if (!rows_ok(g, q, q_stride, g.hq) || !rows_ok(g, out, (int64_t)g.hq * g.D, g.hq) ||
+      !aligned16({cache->k_cache, cache->v_cache}))
+    return RETRO_EINVAL;
+  if (!retro::chunk_attend_supported(g, chunk->n_rows)) return RETRO_EUNSUPPORTED;
+  if (!workspace || !aligned16({workspace}) || ws_bytes < retro::chunk_workspace(g, chunk->n_rows))
+    return RETRO_EWORKSPACE;
+  return from_hip(retro::launch_chunk_attend(g, *cache, *chunk, q, q_stride, out, lse, workspace,
+                                             (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,111 @@
+"""Arguments of the rotation, rotated-append and chunk-attention calls, checked on
+the host before anything is enqueued (CPU only)."""
+import ctypes as C
+import os
+
+import pytest
+
+INVALID, UNSUPPORTED, WORKSPACE, OK = -1, -2, -4, 0
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2508_09001_amd import binding
+    if not os.path.exists(binding.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    return binding
+
+
+A = 1 << 20  # an address that is 16-byte aligned and never dereferenced here
+
+
+def _dims(B, **kw):
+    base = dict(batch=2, num_kv_heads=8, group=4, head_dim=128, page_size=16, budget_tokens=16, window=0,
+                max_pages=64, num_phys_pages=128, dtype=B.RETRO_BF16, sm_scale=0.0)
+    base.update(kw)
+    return B.Dims(**base)
+
+
+def _rotary(B, **kw):
+    base = dict(table=A, positions=1024, rot_dim=128, interleaved=0, eps=1e-5, q_norm=A, k_norm=A)
+    base.update(kw)
+    return B.Rotary(**base)
+
+
+@pytest.mark.parametrize("kw", [dict(table=None), dict(table=A + 4), dict(positions=0), dict(positions=-1),
+                                dict(rot_dim=-16), dict(rot_dim=24), dict(rot_dim=144), dict(interleaved=2),
+                                dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
+                                dict(q_norm=A + 2), dict(k_norm=A + 8)])
+def test_bad_rotary(B, kw):
+    lib, r, d = B.load_library(), _rotary(B, **kw), _dims(B)
+    assert lib.retro_rotate_qk(C.byref(d), C.byref(r), A, 1, A, 4096, A, 1024, A, A, None) == INVALID
+    cache, ch = B.KVCache(*[A] * 6), B.Chunk(A + 64, A + 128, 4)
+    assert lib.retro_append_kv_rotary(C.byref(d), 0, C.byref(cache), C.byref(ch), C.byref(r), A, 4096, A, 1024,
+                                      A, 1024, A, None) == INVALID
+
+
+def test_rotary_table(B):
+    lib = B.load_library()
+    for args in ((None, 8, 64, 1e4), (A + 4, 8, 64, 1e4), (A, 0, 64, 1e4), (A, 8, 0, 1e4), (A, 8, 24, 1e4),
+                 (A, 8, 144, 1e4), (A, 8, 64, 0.0), (A, 8, 64, float("nan")), (A, 8, 64, float("inf"))):
+        assert lib.retro_rotary_table(*args, None) == INVALID
+
+
+def test_rotate_qk(B):
+    lib, r, d = B.load_library(), _rotary(B), _dims(B)
+
+    def call(dims=d, rot=r, pos=A, rows=3, q=A, qs=4096, k=A, ks=1024, qo=A, ko=A):
+        return lib.retro_rotate_qk(dims and C.byref(dims), rot and C.byref(rot), pos, rows, q, qs, k, ks, qo,
+                                   ko, None)
+
+    assert call(rows=0, pos=None, q=None, k=None) == OK            # nothing to do
+    for kw in (dict(dims=None), dict(rot=None), dict(pos=None), dict(rows=-1), dict(q=None, k=None),
+               dict(qo=None), dict(ko=None), dict(qs=4095), dict(qs=4100), dict(ks=1016), dict(q=A + 2),
+               dict(k=A + 8), dict(qo=A + 4), dict(qs=6144), dict(ks=2048)):   # (in place with a stride)
+        assert call(**kw) == INVALID, kw
+    assert call(dims=_dims(B, head_dim=96)) == UNSUPPORTED
+    # fp32: pieces of four elements
+    assert call(dims=_dims(B, dtype=B.RETRO_F32), qs=4098, qo=A + 16) == INVALID
+
+
+def test_append_rotary(B):
+    lib, d = B.load_library(), _dims(B)
+    full = B.KVCache(*[A] * 6)
+
+    def call(dims=d, step=0, cache=full, ch=(A + 64, A + 128, 5), rot=_rotary(B), q=A, qs=4096, k=A, ks=1024,
+             v=A, vs=1024, qo=A + 4096):
+        c = B.Chunk(*ch)
+        return lib.retro_append_kv_rotary(C.byref(dims), step, C.byref(cache), C.byref(c), C.byref(rot), q, qs,
+                                          k, ks, v, vs, qo, None)
+
+    assert call(ch=(A, A + 64, 0), q=None, k=None, v=None) == OK
+    for kw in (dict(step=-1), dict(cache=B.KVCache(A, A, None, A, A, A)), dict(ch=(None, A, 5)),
+               dict(ch=(A, None, 5)), dict(ch=(A + 64, A + 128, -1)),
+               dict(ch=(A + 64, A, 5)),                            # start_pos is the cache's seq_lens
+               dict(rot=_rotary(B, positions=1023)),               # a table shorter than the cache
+               dict(q=A + 2), dict(qs=4104 - 16), dict(qo=None), dict(k=None), dict(v=None), dict(ks=1020),
+               dict(vs=8), dict(cache=B.KVCache(A + 8, A, A, A, A, A)), dict(q=A + 4096, qs=6144)):
+        assert call(**kw) == INVALID, kw
+    assert call(rot=_rotary(B, positions=1023), dims=_dims(B, page_size=8)) == UNSUPPORTED
+
+
+def test_chunk_attend(B):
+    lib, d = B.load_library(), _dims(B)
+    full = B.KVCache(*[A] * 6)
+    ws = B.retro_chunk_workspace_size(d, 5)
+
+    def call(dims=d, cache=full, ch=(A + 64, A + 128, 5), q=A, qs=4096, out=A, lse=A, w=A, n=ws):
+        c = B.Chunk(*ch)
+        return lib.retro_chunk_attend(C.byref(dims), C.byref(cache), C.byref(c), q, qs, out, lse, w, n, None)
+
+    assert call(ch=(A + 64, A + 128, 0), q=None, out=None, w=None, n=0) == OK
+    for kw in (dict(cache=B.KVCache(A, A, A, A, None, A)), dict(ch=(None, A, 5)), dict(ch=(A, None, 5)),
+               dict(ch=(A + 64, A, 5)), dict(ch=(A, A + 64, -2)), dict(q=None), dict(q=A + 2), dict(qs=4088),
+               dict(qs=4097), dict(out=None), dict(out=A + 8), dict(cache=B.KVCache(A, A + 4, A, A, A, A))):
+        assert call(**kw) == INVALID, kw
+    assert call(w=None) == WORKSPACE and call(n=ws - 1) == WORKSPACE and call(w=A + 8) == WORKSPACE
+    assert call(dims=_dims(B, group=17)) == UNSUPPORTED
+    with pytest.raises(B.RetroError):
+        B.retro_chunk_workspace_size(d, -1)
+    assert lib.retro_chunk_workspace_size(C.byref(d), 5, None) == INVALID
