@@ -1,97 +1,833 @@
 // Dense causal attention of a ragged batch of rows over the paged cache.
+//
+// Rows of a KV head are (row of the chunk, query head of the group), G after G.
+// In tiles of 32 keys x 32 rows, S^T = K Q^T and O^T += V^T P^T on 32x32 matrix
+// instructions: a lane holds one row's scores, so that maximum, sum and
+// rescaling need one exchange (with the lane 32 away), and its exponentials are
+// the next product's operand as they lie: key row i of S^T is key
+// 16 (i / 16) + 8 (i / 4 % 2) + 4 (i / 8 % 2) + i % 4 of the tile for bf16 (where a
+// lane's operand is eight consecutive keys), key i for fp32 (four).
+//
+// A workgroup of eight wavefronts takes a unit of work in one of two ways:
+//   - few rows (at most 32 of a sequence and KV head): the wavefronts take 32 keys
+//     in turn, each through LDS of its own, without barriers, and join their
+//     (maximum, sum, output) at the end; bound by reading the cache;
+//   - many rows: 32 of 256 rows each, all over the same 64 keys (fp32: 32), which
+//     are copied into LDS for all, one stage ahead; bound by the matrix cores.
+// Long sequences are cut along the keys where there are too few tiles to fill the
+// GPU; a second launch joins the parts.  The units are laid out on the device,
+// from the arrays of the call, by every workgroup for itself.
+//
+// Pages lie in LDS as in memory, cut into 16-byte pieces whose order within a
+// row is xored with the row's number, so that the 16 lanes of a read fall into 16
+// different groups of banks; the copy engine writes LDS in order and reads
+// memory in the permuted one.
 #include "roles.h"
 #include "rotary.h"
 
 namespace retro {
 namespace {
 
-// One wavefront per (row, query head): 64 keys at a time, one per lane, and then
-// the elements of d spread over the lanes.
-template <typename T, int D>
-__global__ void __launch_bounds__(64) chunk_attend_kernel(Geometry g, retro_chunk ch,
-                                                          const T* __restrict__ kc,
-                                                          const T* __restrict__ vc,
-                                                          const int32_t* __restrict__ pt,
-                                                          const int32_t* __restrict__ seq_lens,
-                                                          const T* __restrict__ q, int64_t q_stride,
-                                                          T* __restrict__ out,
-                                                          float* __restrict__ lse) {
-  __shared__ float sq[D], sp[64];
-  __shared__ int sphys[64];
-  const int lane = threadIdx.x, row = blockIdx.x, hq = blockIdx.y, h = hq / g.G;
-  int b = 0;
-  Run run{0, 0, 0};
-  for (; b < g.batch; ++b) {
-    run = chunk_run(ch, b);
-    if (row >= run.row && row < run.row + run.n) break;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kRowsFew = 32;             // rows of a unit in the first way
+constexpr int kRowsMany = 32 * kWaves;   // and in the second
+constexpr int kCus = 256;
+constexpr int kManyPerCu = 4;            // units of many rows aimed for per compute unit
+constexpr int kMinMany = 8, kMinFew = 4; // least steps of 64 keys of a part
+
+struct AttendCall {
+  retro_chunk ch;
+  const void *kc, *vc;
+  const int32_t *pt, *seq_lens;
+  const void* q;
+  int64_t q_stride;
+  void* out;
+  float* lse;
+  float* parts;
+  int batch, hk, G, hq, max_pages, num_phys;
+  float scale;
+};
+
+// ---- the units of a call -------------------------------------------------------------
+
+struct Seq {
+  Run run;
+  int end;     // stored tokens that the rows may see
+  int tiles;   // row tiles per KV head
+  int steps;   // steps of 64 keys up to end
+  bool few;
+};
+
+__device__ __forceinline__ Seq load_seq(const AttendCall& a, int P, int b) {
+  Seq s;
+  s.run = b < a.batch ? chunk_run(a.ch, b) : Run{0, 0, 0};
+  const int64_t rows = (int64_t)s.run.n * a.G;
+  s.few = rows <= kRowsFew;
+  s.tiles = s.few ? (rows > 0) : (int)((rows + kRowsMany - 1) / kRowsMany);
+  const int len = b < a.batch && rows ? a.seq_lens[b] : 0;
+  s.end = (int)min((int64_t)min(max(len, 0), s.run.pos + s.run.n), (int64_t)a.max_pages * P);
+  s.steps = (s.end + 63) / 64;
+  return s;
+}
+
+// What every workgroup agrees on: the steps of a part.
+struct Cut {
+  int few, many;
+  __device__ int parts(const Seq& s) const {
+    if (!s.tiles) return 0;
+    const int u = s.few ? few : many;
+    return max((s.steps + u - 1) / u, 1);
   }
-  if (b == g.batch) return;
-  const int p = run.pos + row - run.row;
-  const int end = (int)min(min((int64_t)p + 1, (int64_t)seq_lens[b]), (int64_t)g.max_pages * g.P);
-  for (int i = lane; i < D; i += 64) sq[i] = to_f32(q[row * q_stride + hq * D + i]);
+};
+
+struct Unit {
+  int b, tile, h, part, parts;
+  int64_t slot;  // floats in front of its partial result (parts > 1)
+};
+
+constexpr int slot_floats(int rows, int D) { return rows * (D + 2); }
+
+// Sums over the workgroup's threads; scratch: one value per wavefront.
+template <int NW>
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* scratch, int tid) {
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  if ((tid & 63) == 0) scratch[tid >> 6] = x;
   __syncthreads();
-  float m = -INFINITY, l = 0.f, o[D / 64];
-  for (int i = 0; i < D / 64; ++i) o[i] = 0.f;
-  for (int k0 = 0; k0 < end; k0 += 64) {
-    const int key = k0 + lane;
-    int ph = key < end ? pt[(int64_t)b * g.max_pages + key / g.P] : -1;
-    if (ph >= g.num_phys) ph = -1;
-    float s = 0.f;
-    if (ph >= 0)
-      for (int i = 0; i < D; ++i)
-        s += sq[i] * to_f32(kc[(((int64_t)ph * g.hk + h) * g.P + key % g.P) * D + i]);
-    s = ph >= 0 ? s * g.sm_scale : -INFINITY;
-    const float mn = fmaxf(m, wave_max(s)), mu = mn == -INFINITY ? 0.f : mn;
-    const float e = ph >= 0 ? expf(s - mu) : 0.f, alpha = expf(m - mu);
-    l = l * alpha + wave_sum(e);
-    m = mn;
-    sp[lane] = e;
-    sphys[lane] = ph;
+  int64_t s = 0;
+  for (int i = 0; i < NW; ++i) s += scratch[i];
+  __syncthreads();
+  return s;
+}
+
+template <int NW>
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* scratch, int tid, int64_t& total) {
+  const int lane = tid & 63;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) scratch[tid >> 6] = x;
+  __syncthreads();
+  int64_t base = 0;
+  total = 0;
+  for (int i = 0; i < NW; ++i) {
+    if (i < tid >> 6) base += scratch[i];
+    total += scratch[i];
+  }
+  __syncthreads();
+  return base + x;
+}
+
+template <int NW>
+__device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, int64_t* scratch, int tid) {
+  int64_t w = 0;
+  for (int b = tid; b < a.batch; b += 64 * NW) {
+    const Seq s = load_seq(a, P, b);
+    w += (int64_t)s.tiles * s.steps;
+  }
+  w = block_sum<NW>(w, scratch, tid) * a.hk;
+  Cut c;
+  c.few = max((int)min((w + kCus - 1) / kCus, (int64_t)1 << 30), kMinFew);
+  c.many = max((int)min((w + kManyPerCu * kCus - 1) / (kManyPerCu * kCus), (int64_t)1 << 30), kMinMany);
+  return c;
+}
+
+struct FindLds {
+  int64_t scratch[kWaves];
+  int64_t slot;
+  int b, local;
+};
+
+// The sequence that item u belongs to, where a sequence has count(seq) items;
+// slots_before: floats of the partial results of the sequences in front of it.
+template <int NW, typename Count>
+__device__ __forceinline__ bool find_seq(const AttendCall& a, int P, int D, const Cut& cut, int64_t u,
+                                         FindLds& L, int tid, Count&& count, int& b, int64_t& local,
+                                         int64_t& slot) {
+  int64_t base = 0, slots = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64 * NW) {
+    const Seq s = load_seq(a, P, b0 + tid);
+    const int parts = cut.parts(s);
+    const int64_t n = count(s, parts);
+    const int64_t f = parts > 1 ? (int64_t)s.tiles * a.hk * parts *
+                                      slot_floats(s.few ? kRowsFew : kRowsMany, D) : 0;
+    int64_t total, slots_here;
+    const int64_t upto = base + block_scan<NW>(n, L.scratch, tid, total);
+    const int64_t fupto = slots + block_scan<NW>(f, L.scratch, tid, slots_here);
+    if (u >= upto - n && u < upto) {
+      L.b = b0 + tid;
+      L.local = (int)(u - (upto - n));
+      L.slot = fupto - f;
+    }
     __syncthreads();
-    for (int i = 0; i < D / 64; ++i) o[i] *= alpha;
-    for (int j = 0; j < 64; ++j) {
-      if (sphys[j] < 0) continue;
-      const T* vr = vc + ((int64_t)sphys[j] * g.hk + h) * g.P * D + (k0 + j) % g.P;
-      for (int i = 0; i < D / 64; ++i) o[i] += sp[j] * to_f32(vr[(lane + i * 64) * g.P]);
+    if (u < base + total) {
+      b = L.b;
+      local = L.local;
+      slot = L.slot;
+      __syncthreads();
+      return true;
+    }
+    base += total;
+    slots += slots_here;
+  }
+  return false;
+}
+
+// ---- LDS pieces ----------------------------------------------------------------------
+
+template <typename T, int D, int P>
+struct Shape {
+  static constexpr int E = 16 / sizeof(T);       // elements of a piece
+  static constexpr int KB = 32;                  // keys of a tile
+  static constexpr int CPR = D / E;              // pieces of a key row
+  static constexpr int CPV = P / E;              // pieces of a value row (one element of d of a page)
+  static constexpr int TILE = KB * D * sizeof(T);  // bytes of a tile's keys (and of its values)
+  static constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;  // keys of a shared stage
+  static constexpr int NB = KEYS / KB;
+  static constexpr int STAGE = 2 * NB * TILE;    // bytes of a stage: keys, then values
+  static constexpr int LOADS = TILE / 1024;      // wavefront copies of a tile's keys (or values)
+  static constexpr int PPP = P * D * (int)sizeof(T) / 1024;  // copies of a page
+  static constexpr int OWN = TILE <= 8192 ? kWaves : kWaves / 2;  // wavefronts in the first way
+  static constexpr int OROW = D + 4;             // row of the joining buffer
+  static constexpr int QC = CPR / 2;             // pieces of a row per lane half
+  // order of a key row's pieces, and of a value row's
+  static __device__ __forceinline__ int fk(int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; }
+  static __device__ __forceinline__ int fv(int d) { return d / (16 / CPV) % CPV; }
+};
+
+template <typename T, int D, int P>
+struct ChunkLds {
+  using S = Shape<T, D, P>;
+  union {
+    char stage[2][S::STAGE];
+    char own[S::OWN][2 * S::TILE];
+    float o[S::OWN][kRowsFew][S::OROW];
+  } u;
+  float m[kWaves][32], l[kWaves][32];
+  FindLds find;
+};
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+
+// 16 bytes per lane from memory at base + offset (a lane's own) to LDS at `to` +
+// 16 lane, asynchronously; counted like a load.  Written out because the compiler
+// waits for every copy in flight in front of any read of LDS.
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(to), "v"(offset), "s"(base)
+               : "memory");
+}
+// until at most N of the wavefront's loads and copies are in flight
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ u32x4 lds_piece(uint32_t at) {
+  return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)at;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  uint32_t w = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+  asm("" : "+v"(w));  // one conversion for the pair: its halves are taken from w
+  return w;
+}
+
+// ---- a wavefront's 32 rows -------------------------------------------------------------
+
+template <typename T, int D, int P>
+struct Rows {
+  using S = Shape<T, D, P>;
+  static constexpr int DT = D / 32;
+  u32x4 q[S::QC];
+  f32x16 acc[DT];
+  float m, l;   // running maximum of the scores (unscaled) and sum of the lane's half
+  int lim;      // last token that the lane's row may see
+  float c;      // scale * log2(e)
+  int half;
+  uint32_t koff[S::QC];          // the lane's pieces of a key tile
+  uint32_t voff[S::CPV / 2];     // and of a value tile's first 32 elements of d
+
+  __device__ __forceinline__ void init(int lane, float scale) {
+    half = lane >> 5;
+    const int r = lane & 31;
+    const int key = sizeof(T) == 2 ? (r & 16) + 8 * (r >> 2 & 1) + 4 * (r >> 3 & 1) + (r & 3) : r;
+#pragma unroll
+    for (int i = 0; i < S::QC; ++i)
+      koff[i] = key * D * sizeof(T) + ((2 * i + half) ^ S::fk(key)) * 16;
+#pragma unroll
+    for (int i = 0; i < S::CPV / 2; ++i)
+      voff[i] = r * P * sizeof(T) + ((2 * i + half) ^ S::fv(r)) * 16;
+    c = scale * kLog2e;
+  }
+
+  __device__ __forceinline__ void start(const T* row, bool live, int limit) {
+#pragma unroll
+    for (int i = 0; i < S::QC; ++i)
+      q[i] = live ? reinterpret_cast<const u32x4*>(row)[2 * i + half] : u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    lim = limit;
+  }
+
+  // S^T of one tile of keys
+  __device__ __forceinline__ f32x16 scores(uint32_t keys) const {
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < S::QC; ++i) {
+      const u32x4 k = lds_piece<T>(keys + koff[i]);
+      if constexpr (sizeof(T) == 2) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k),
+                                                    __builtin_bit_cast(bf16x8, q[i]), s, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(q[i][e]), s,
+                                                   0, 0, 0);
+      }
+    }
+    return s;
+  }
+
+  // key of register e within a tile, without the lane half's part
+  static __device__ constexpr int key_of(int e) {
+    return sizeof(T) == 2 ? 16 * (e / 8) + e % 8 : 8 * (e / 4) + e % 4;
+  }
+
+  // Scores to weights.  Masked: keys past the lane's last one, and keys of pages
+  // that are not mapped (bit i of bad: page i of the tiles).
+  template <int NB, bool MASK>
+  __device__ __forceinline__ void weights(f32x16 (&s)[NB], int key0, uint32_t bad) {
+    if constexpr (MASK) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int k = 32 * b + key_of(e) + S::E * half;
+          if (key0 + k > lim || (bad >> (k / P) & 1)) s[b][e] = -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = b ? 0 : 1; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
+    mx = rows_half_max(mx);
+    // The maximum follows only when a weight would pass 2^8: weights of up to 256
+    // lose nothing in fp32 or bf16, and most steps leave the output as it is.
+    if (wave_ballot((mx - m) * c > 8.f)) {
+      const float mn = fmaxf(m, mx);
+      const float alpha = __builtin_amdgcn_exp2f((m - mn) * c);
+      const float a = mn == -INFINITY ? 0.f : alpha;
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] *= a;
+      l *= a;
+      m = mn;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], c, -mc));
+        l += s[b][e];
+      }
+  }
+
+  // O^T += V^T P^T of one tile.  Masked: values of slots that hold no token of the
+  // sequence (stored: tokens of it from this tile's first key on) are taken as zero.
+  template <bool MASK>
+  __device__ __forceinline__ void values(uint32_t at, const f32x16& p, int stored, uint32_t bad) {
+    constexpr int STEPS = 32 / (2 * S::E);  // key pieces of a lane half
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) {
+      const int piece = 2 * t;  // (+ half) of the tile; pieces of a page: CPV
+      const uint32_t off = at + voff[piece % S::CPV / 2] + piece / S::CPV * (D * P * sizeof(T));
+      [[maybe_unused]] bf16x8 w;
+      if constexpr (sizeof(T) == 2) {
+        u32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = pack_bf16(p[8 * t + 2 * e], p[8 * t + 2 * e + 1]);
+        w = __builtin_bit_cast(bf16x8, x);
+      }
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        u32x4 v = lds_piece<T>(off + i * (32 * P * sizeof(T)));
+        if constexpr (MASK) {
+          const int k = S::E * (piece + half);
+          const int n = bad >> (k / P) & 1 ? 0 : stored - k;  // elements that count
+          if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] &= (n > 2 * e ? 0xffffu : 0u) | (n > 2 * e + 1 ? 0xffff0000u : 0u);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = n > e ? v[e] : 0u;
+          }
+        }
+        if constexpr (sizeof(T) == 2) {
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w, acc[i], 0,
+                                                           0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v[e]), p[4 * t + e], acc[i],
+                                                          0, 0, 0);
+        }
+      }
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+  if constexpr (sizeof(T) == 2) {
+    uint2 w;
+    w.x = pack_bf16(a, b);
+    w.y = pack_bf16(c, d);
+    *reinterpret_cast<uint2*>(p) = w;
+  } else {
+    *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
+  }
+}
+
+__device__ __forceinline__ float natural_lse(float m, float l, float scale) {
+  return l == 0.f ? -INFINITY : __builtin_fmaf(m, scale, __builtin_amdgcn_logf(l) * kLn2);
+}
+
+// ---- kernel ------------------------------------------------------------------------------
+
+template <typename T, int D, int P>
+__global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a, int snake) {
+  using S = Shape<T, D, P>;
+  using R_t = Rows<T, D, P>;
+  using Lds_t = ChunkLds<T, D, P>;
+  __shared__ __attribute__((aligned(1024))) Lds_t L;
+  const int tid = thread_index();
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t lds0 = lds_address(&L);
+  const Cut cut = make_cut<kWaves>(a, P, L.find.scratch, tid);
+  // a lane's place within a copy of keys, and of values: pieces in their LDS order
+  const uint32_t kcopy = lane / S::CPR * (D * sizeof(T)) + (lane % S::CPR ^ S::fk(lane / S::CPR)) * 16;
+  const uint32_t vcopy = lane / S::CPV * (P * sizeof(T)) + (lane % S::CPV ^ S::fv(lane / S::CPV)) * 16;
+  // pieces of copy i: rows further on, whose numbers change the order by this
+  constexpr int kRowsPerCopy = 64 / S::CPR;
+  auto kxor = [](int i) { return (uint32_t)S::fk(i * kRowsPerCopy & 31) << 4; };
+  auto vxor = [](int i) { return S::CPV == 8 ? (uint32_t)(i & 1) << 6 : 0u; };
+  const int64_t page_bytes = (int64_t)P * D * sizeof(T);
+
+  for (int64_t round = 0;; ++round) {
+    // longest first; every other round backwards, eight neighbours (one per XCD) together
+    int64_t k = blockIdx.x;
+    if ((round & 1) && snake) k = (int64_t)(gridDim.x / 8 - 1 - k / 8) * 8 + k % 8;
+    int b;
+    int64_t u, slot;
+    if (!find_seq<kWaves>(a, P, D, cut, round * gridDim.x + k, L.find, tid,
+                          [&](const Seq& s, int parts) { return (int64_t)s.tiles * a.hk * parts; }, b, u,
+                          slot))
+      break;
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int un = __builtin_amdgcn_readfirstlane((int)u);
+    const Seq s = load_seq(a, P, b);
+    // KV head fastest (a head's units meet in one L2), then row tiles, last first
+    const int h = un % a.hk, part = un / a.hk / s.tiles, tile = s.tiles - 1 - un / a.hk % s.tiles;
+    const int R = (int)min((int64_t)s.run.n * a.G - (int64_t)tile * kRowsMany, (int64_t)kRowsMany);
+    const int last = (tile * kRowsMany + R - 1) / a.G;        // last row of the chunk in the tile
+    const int end = min(s.end, s.run.pos + last + 1);         // tokens that the tile sees
+    const int steps = (end + 63) / 64;
+    const int u_steps = s.few ? cut.few : cut.many;
+    const int parts = max((steps + u_steps - 1) / u_steps, 1);
+    if (part >= parts) continue;
+    const int per = (steps + parts - 1) / parts;
+    const int key_begin = part * per * 64, key_end = min(end, (part + 1) * per * 64);
+    const int pages = (s.end + P - 1) / P;
+    const int32_t* pt = a.pt + (int64_t)b * a.max_pages;
+    const char* kh = (const char*)a.kc + h * page_bytes;
+    const char* vh = (const char*)a.vc + h * page_bytes;
+    const int64_t phys_bytes = page_bytes * a.hk;
+    // page i of the sequence: its number if mapped, else page 0 (never counted)
+    auto page_of = [&](int i, bool& bad) {
+      const int id = sload(pt + min(i, max(pages - 1, 0)));
+      bad = id < 0 || id >= a.num_phys;
+      return bad ? 0 : id;
+    };
+    // pages without a mapping among the next n (those past the end are cut by lengths)
+    auto bad_pages = [&](int page0, auto n) {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < decltype(n)::value; ++i) {
+        bool bad;
+        page_of(page0 + i, bad);
+        bits |= (uint32_t)bad << i;
+      }
+      return bits;
+    };
+    auto row_at = [&](int rho, bool& live, int& lim) {
+      live = rho < s.run.n * a.G;
+      const int r = min(rho, s.run.n * a.G - 1);
+      lim = min(s.run.pos + r / a.G, s.end - 1);
+      return (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride +
+             (int64_t)(h * a.G + r % a.G) * D;
+    };
+    float* part_o = a.parts + slot + (int64_t)un * slot_floats(s.few ? kRowsFew : kRowsMany, D);
+
+    if (s.few) {
+      constexpr int PT = 32 / P;  // pages of a tile
+      const int lane = thread_index() & 63;
+      R_t rows;
+      rows.init(lane, a.scale);
+      bool live;
+      int lim;
+      const T* qrow = row_at(lane & 31, live, lim);
+      rows.start(qrow, live, lim);
+      const int lim0 = min(s.run.pos, s.end - 1);
+      const uint32_t ks = lds0 + (uint32_t)offsetof(Lds_t, u) + wave * 2 * S::TILE;
+      const uint32_t vs = ks + S::TILE;
+      auto issue = [&](const char* base, uint32_t to, int key, uint32_t off, auto x) {
+#pragma unroll
+        for (int pg = 0; pg < PT; ++pg) {
+          bool bad;
+          const char* src = base + page_of(key / P + pg, bad) * phys_bytes;
+#pragma unroll
+          for (int i = 0; i < S::PPP; ++i)
+            copy_to_lds(src + i * 1024, off ^ x(pg * S::PPP + i), to + (pg * S::PPP + i) * 1024);
+        }
+      };
+      int key = key_begin + wave * 32;
+      const bool mine = wave < S::OWN && key < key_end;
+      if (mine) {
+        issue(kh, ks, key, kcopy, kxor);
+        issue(vh, vs, key, vcopy, vxor);
+        for (; key < key_end; key += S::OWN * 32) {
+          const int next = key + S::OWN * 32;
+          const uint32_t bad = bad_pages(key / P, std::integral_constant<int, PT>{});
+          f32x16 sc[1];
+          wait_loads<S::LOADS>();
+          sc[0] = rows.scores(ks);
+          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+          if (next < key_end) issue(kh, ks, next, kcopy, kxor);
+          if (bad || key + 31 > lim0) {
+            rows.template weights<1, true>(sc, key, bad);
+            if (next < key_end) wait_loads<S::LOADS>();
+            else wait_loads<0>();
+            rows.template values<true>(vs, sc[0], s.end - key, bad);
+          } else {
+            rows.template weights<1, false>(sc, key, bad);
+            if (next < key_end) wait_loads<S::LOADS>();
+            else wait_loads<0>();
+            rows.template values<false>(vs, sc[0], 32, 0);
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+          if (next < key_end) issue(vh, vs, next, vcopy, vxor);
+        }
+      }
+      // join the wavefronts' results
+      barrier();
+      const int r = lane & 31, nr = s.run.n * a.G;
+      rows.l = rows_half_sum(rows.l);
+      if (lane < 32) {
+        L.m[wave][r] = rows.m;
+        L.l[wave][r] = rows.l;
+      }
+      if (wave < S::OWN && r < nr)
+#pragma unroll
+        for (int i = 0; i < R_t::DT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<f32x4*>(&L.u.o[wave][r][i * 32 + 2 * e + 4 * rows.half]) =
+                f32x4{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
+      barrier();
+      for (int i = tid; i < nr * (D / 4); i += kThreads) {
+        const int row = i / (D / 4), d = i % (D / 4) * 4;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < S::OWN; ++w) m = fmaxf(m, L.m[w][row]);
+        const float mu = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < S::OWN; ++w) {
+          const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * rows.c);
+          const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
+          l = __builtin_fmaf(e, L.l[w][row], l);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
+        }
+        if (parts > 1) {
+          *reinterpret_cast<f32x4*>(part_o + row * D + d) = o;
+          if (d == 0) {
+            part_o[kRowsFew * D + row] = m;
+            part_o[kRowsFew * (D + 1) + row] = l;
+          }
+        } else {
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          const int64_t at = (int64_t)(s.run.row + row / a.G) * a.hq + h * a.G + row % a.G;
+          store4((T*)a.out + at * D + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+          if (d == 0 && a.lse) a.lse[at] = natural_lse(m, l, a.scale);
+        }
+      }
+      barrier();
+      continue;
+    }
+
+    // ---- many rows
+    constexpr int PS = S::KEYS / P;  // pages of a stage
+    const int lane = thread_index() & 63;
+    R_t rows;
+    rows.init(lane, a.scale);
+    const int rho0 = tile * kRowsMany + wave * 32;
+    const bool any = rho0 < s.run.n * a.G;
+    bool live;
+    int lim;
+    const T* qrow = row_at(rho0 + (lane & 31), live, lim);
+    rows.start(qrow, live, lim);
+    // the wavefront's rows all see the tokens up to lim0, none sees past lim1
+    const int lim0 = any ? min(s.run.pos + rho0 / a.G, s.end - 1) : -1;
+    const int lim1 = any ? min(s.run.pos + min(rho0 + 31, s.run.n * a.G - 1) / a.G, s.end - 1) : -1;
+    constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
+    static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
+    auto issue = [&](int key, uint32_t to) {
+      bool bad;
+      const int first = wave * MINE, i0 = first % S::PPP;
+      const int64_t off = page_of(key / P + first / S::PPP, bad) * phys_bytes + i0 * 1024;
+#pragma unroll
+      for (int i = 0; i < MINE; ++i)
+        copy_to_lds(kh + off + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
+#pragma unroll
+      for (int i = 0; i < MINE; ++i)
+        copy_to_lds(vh + off + i * 1024, vcopy ^ vxor(first + i), to + S::NB * S::TILE + (first + i) * 1024);
+    };
+    const uint32_t st = lds0 + (uint32_t)offsetof(Lds_t, u);
+    auto stage = [&](int key, uint32_t at) {
+      if (key > lim1) return;
+      f32x16 sc[S::NB];
+#pragma unroll
+      for (int i = 0; i < S::NB; ++i) sc[i] = rows.scores(at + i * S::TILE);
+      const uint32_t bad = bad_pages(key / P, std::integral_constant<int, PS>{});
+      const uint32_t v = at + S::NB * S::TILE;
+      if (bad || key + S::KEYS - 1 > lim0) {
+        rows.template weights<S::NB, true>(sc, key, bad);
+#pragma unroll
+        for (int i = 0; i < S::NB; ++i)
+          rows.template values<true>(v + i * S::TILE, sc[i], s.end - key - 32 * i, bad >> (i * 32 / P));
+      } else {
+        rows.template weights<S::NB, false>(sc, key, bad);
+#pragma unroll
+        for (int i = 0; i < S::NB; ++i)
+          rows.template values<false>(v + i * S::TILE, sc[i], 32, 0);
+      }
+    };
+    if (key_begin < key_end) {
+      issue(key_begin, st);
+      for (int key = key_begin; key < key_end; key += 2 * S::KEYS) {
+        wait_loads<0>();
+        barrier();
+        if (key + S::KEYS < key_end) issue(key + S::KEYS, st + S::STAGE);
+        stage(key, st);
+        if (key + S::KEYS >= key_end) break;
+        wait_loads<0>();
+        barrier();
+        if (key + 2 * S::KEYS < key_end) issue(key + 2 * S::KEYS, st);
+        stage(key + S::KEYS, st + S::STAGE);
+      }
+    }
+    rows.l = rows_half_sum(rows.l);
+    const int rt = wave * 32 + (lane & 31), rho = tile * kRowsMany + rt;
+    if (rho < s.run.n * a.G) {
+      if (parts > 1) {
+#pragma unroll
+        for (int i = 0; i < R_t::DT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<f32x4*>(part_o + rt * D + i * 32 + 2 * e + 4 * rows.half) =
+                f32x4{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
+        if (lane < 32) {
+          part_o[kRowsMany * D + rt] = rows.m;
+          part_o[kRowsMany * (D + 1) + rt] = rows.l;
+        }
+      } else {
+        const float inv = rows.l == 0.f ? 0.f : 1.f / rows.l;
+        const int64_t at = (int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G;
+        T* o = (T*)a.out + at * D;
+#pragma unroll
+        for (int i = 0; i < R_t::DT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            store4(o + i * 32 + 2 * e + 4 * rows.half, rows.acc[i][e] * inv, rows.acc[i][e + 1] * inv,
+                   rows.acc[i][e + 2] * inv, rows.acc[i][e + 3] * inv);
+        if (lane < 32 && a.lse) a.lse[at] = natural_lse(rows.m, rows.l, a.scale);
+      }
+    }
+    barrier();
+  }
+}
+
+// Joins the parts of the tiles that were cut: 32 rows of a tile and KV head per workgroup.
+constexpr int kJoinWaves = 4;
+constexpr int kJoinWeights = 64;  // parts whose weights lie in LDS at a time
+
+template <typename T, int D, int P>
+__global__ void __launch_bounds__(64 * kJoinWaves) chunk_join_kernel(AttendCall a) {
+  __shared__ FindLds find;
+  __shared__ float wt[kJoinWeights][32], inv_l[32];
+  const int tid = threadIdx.x;
+  const Cut cut = make_cut<kJoinWaves>(a, P, find.scratch, tid);
+  const float c = a.scale * kLog2e;
+  for (int64_t item = blockIdx.x;; item += gridDim.x) {
+    int b;
+    int64_t u, slot;
+    if (!find_seq<kJoinWaves>(a, P, D, cut, item, find, tid,
+                              [&](const Seq& s, int parts) {
+                                return parts > 1 ? (int64_t)s.tiles * a.hk * (s.few ? 1 : kRowsMany / 32) : 0;
+                              },
+                              b, u, slot))
+      break;
+    const Seq s = load_seq(a, P, b);
+    const int rows_unit = s.few ? kRowsFew : kRowsMany, blocks = rows_unit / 32;
+    const int block = (int)(u % blocks), h = (int)(u / blocks % a.hk), tile = (int)(u / blocks / a.hk);
+    const int R = (int)min((int64_t)s.run.n * a.G - (int64_t)tile * kRowsMany, (int64_t)kRowsMany);
+    const int end = min(s.end, s.run.pos + (tile * kRowsMany + R - 1) / a.G + 1);
+    const int u_steps = s.few ? cut.few : cut.many;
+    const int parts = max(((end + 63) / 64 + u_steps - 1) / u_steps, 1);
+    const int nr = min(R - block * 32, 32);
+    if (parts == 1 || nr <= 0) continue;
+    // part p of the tile is unit (p * tiles + tiles - 1 - tile) * hk + h of the sequence
+    const int64_t unit = slot_floats(rows_unit, D), first = slot + ((int64_t)(s.tiles - 1 - tile) * a.hk + h) * unit,
+                  step = (int64_t)s.tiles * a.hk * unit;
+    const float* p0 = a.parts + first;
+    const float* ml = p0 + rows_unit * D + block * 32;
+    // each row's maximum and sum over the parts
+    const int row = tid & 31;
+    float m = -INFINITY, l = 0.f;
+    if (row < nr) {
+      for (int p = 0; p < parts; ++p) m = fmaxf(m, ml[p * step + row]);
+      const float mu = m == -INFINITY ? 0.f : m;
+      for (int p = 0; p < parts; ++p)
+        l = __builtin_fmaf(__builtin_amdgcn_exp2f((ml[p * step + row] - mu) * c),
+                           ml[p * step + rows_unit + row], l);
+      if (tid < 32) {
+        inv_l[row] = l == 0.f ? 0.f : 1.f / l;
+        const int rho = tile * kRowsMany + block * 32 + row;
+        if (a.lse)
+          a.lse[(int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G] = natural_lse(m, l, a.scale);
+      }
+    }
+    constexpr int ITEMS = 32 * D / 4 / (64 * kJoinWaves);
+    f32x4 o[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int q0 = 0; q0 < parts; q0 += kJoinWeights) {
+      const int np = min(parts - q0, kJoinWeights);
+      __syncthreads();
+      const float mu = m == -INFINITY ? 0.f : m;
+      for (int p = tid >> 5; p < np; p += 2 * kJoinWaves)
+        if (row < nr) wt[p][row] = __builtin_amdgcn_exp2f((ml[(q0 + p) * step + row] - mu) * c);
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int e = tid + i * 64 * kJoinWaves, r = e / (D / 4), d = e % (D / 4) * 4;
+        if (r >= nr) continue;
+#pragma unroll 4
+        for (int p = 0; p < np; ++p) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(p0 + (q0 + p) * step + (block * 32 + r) * D + d);
+          const float w = wt[p][r];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[i][j] = __builtin_fmaf(w, x[j], o[i][j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int e = tid + i * 64 * kJoinWaves, r = e / (D / 4), d = e % (D / 4) * 4;
+      if (r >= nr) continue;
+      const int rho = tile * kRowsMany + block * 32 + r;
+      const int64_t at = (int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G;
+      const float w = inv_l[r];
+      store4((T*)a.out + at * D + d, o[i][0] * w, o[i][1] * w, o[i][2] * w, o[i][3] * w);
     }
     __syncthreads();
   }
-  const int64_t at = (int64_t)row * g.hq + hq;
-  for (int i = 0; i < D / 64; ++i) {
-    const float y = l == 0.f ? 0.f : o[i] / l;
-    if constexpr (sizeof(T) == 2) {
-      const __bf16 w = (__bf16)y;
-      out[at * D + lane + i * 64].bits = __builtin_bit_cast(uint16_t, w);
-    } else {
-      out[at * D + lane + i * 64] = y;
-    }
-  }
-  if (lse && lane == 0) lse[at] = l == 0.f ? -INFINITY : m + logf(l);
+}
+
+// The most units that any lengths can give: few rows, many rows.
+struct Bounds {
+  int64_t few, many;        // tiles of all sequences and KV heads
+  int64_t cut_few, cut_many;  // parts of cut tiles
+};
+Bounds bounds(const Geometry& g, int n_rows) {
+  Bounds x;
+  const int64_t rows = (int64_t)n_rows * g.G;
+  const int64_t steps = ((int64_t)g.max_pages * g.P + 63) / 64;
+  x.few = std::min<int64_t>(g.batch, n_rows) * g.hk;
+  const int64_t seqs = std::min<int64_t>(g.batch, rows / (kRowsFew + 1));
+  x.many = seqs ? (rows / kRowsMany + seqs) * g.hk : 0;
+  // a sequence cut into n >= 2 parts has more than n - 1 >= n / 2 parts' steps; the
+  // parts' steps are at least 1 / kCus (1 / (kManyPerCu kCus)) of all
+  x.cut_few = std::min(x.few * ((steps + kMinFew - 1) / kMinFew), (int64_t)2 * kCus);
+  x.cut_many = std::min(x.many * ((steps + kMinMany - 1) / kMinMany), (int64_t)2 * kManyPerCu * kCus);
+  if (steps <= kMinFew) x.cut_few = 0;
+  if (steps <= kMinMany) x.cut_many = 0;
+  return x;
 }
 
 }  // namespace
 
 bool chunk_attend_supported(const Geometry& g, int n_rows) {
-  return (int64_t)n_rows * g.hq * g.D < (int64_t)1 << 40 && g.hq <= 65535;
+  return (int64_t)n_rows * g.hq * g.D < (int64_t)1 << 40 && (int64_t)n_rows * g.G < (int64_t)1 << 31;
 }
 
-size_t chunk_workspace(const Geometry&, int) { return 256; }
+size_t chunk_workspace(const Geometry& g, int n_rows) {
+  const Bounds x = bounds(g, n_rows);
+  const size_t floats = x.cut_few * slot_floats(kRowsFew, g.D) + x.cut_many * slot_floats(kRowsMany, g.D);
+  return (floats * sizeof(float) + 255 & ~size_t(255)) + 256;
+}
 
 hipError_t launch_chunk_attend(const Geometry& g, const retro_kv_cache& c, const retro_chunk& ch,
-                               const void* q, int64_t q_stride, void* out, float* lse, void*,
+                               const void* q, int64_t q_stride, void* out, float* lse, void* ws,
                                hipStream_t s) {
-  const dim3 grid((unsigned)ch.n_rows, (unsigned)g.hq);
-  auto go = [&](auto t, auto d) {
+  const Bounds x = bounds(g, ch.n_rows);
+  const AttendCall a{ch,         c.k_cache, c.v_cache, c.page_table, c.seq_lens, q,
+                     q_stride,   out,       lse,       (float*)ws,   g.batch,    g.hk,
+                     g.G,        g.hq,      g.max_pages, g.num_phys, g.sm_scale};
+  const int64_t most = x.few + x.many + x.cut_few + x.cut_many;
+  const int grid = (int)std::min<int64_t>((most + 7) / 8 * 8, kCus);
+  const int64_t joins = (x.cut_few ? x.few : 0) + (x.cut_many ? x.many * (kRowsMany / 32) : 0);
+  auto go = [&](auto t, auto d, auto ps) {
     using T = decltype(t);
-    chunk_attend_kernel<T, decltype(d)::value><<<grid, 64, 0, s>>>(
-        g, ch, (const T*)c.k_cache, (const T*)c.v_cache, c.page_table, c.seq_lens, (const T*)q,
-        q_stride, (T*)out, lse);
+    constexpr int D = decltype(d)::value, P = decltype(ps)::value;
+    chunk_attend_kernel<T, D, P><<<grid, kThreads, 0, s>>>(a, 1);
+    if (joins > 0)
+      chunk_join_kernel<T, D, P><<<(unsigned)std::min<int64_t>(joins, 4 * kCus), 64 * kJoinWaves, 0, s>>>(a);
     return hipGetLastError();
+  };
+  auto with_page = [&](auto t, auto d) {
+    return g.P == 16 ? go(t, d, std::integral_constant<int, 16>{})
+                     : go(t, d, std::integral_constant<int, 32>{});
   };
   using D64 = std::integral_constant<int, 64>;
   using D128 = std::integral_constant<int, 128>;
-  if (g.dtype == RETRO_BF16) return g.D == 128 ? go(bf16_t{}, D128{}) : go(bf16_t{}, D64{});
-  return g.D == 128 ? go(float{}, D128{}) : go(float{}, D64{});
+  if (g.dtype == RETRO_BF16) return g.D == 128 ? with_page(bf16_t{}, D128{}) : with_page(bf16_t{}, D64{});
+  return g.D == 128 ? with_page(float{}, D128{}) : with_page(float{}, D64{});
 }
 
 }  // namespace retro
