@@ -516,9 +516,10 @@ retro_status retro_append_kv_rotary(const retro_dims* dims, int32_t step,
                                     const void* k, int64_t k_stride, const void* v,
                                     int64_t v_stride, void* q_out, void* stream);
 
-/* Bytes of workspace that retro_chunk_attend needs for n_rows rows.  Scratch:
- * nothing in it outlives a call, it needs no initialisation, and one call at a
- * time may use it. */
+/* Bytes of workspace that retro_chunk_attend needs for up to n_rows rows, whatever
+ * the lengths.  Zero-fill it once before its first use (the parts of a tile are
+ * counted there; a call leaves the counts at zero) and let one call at a time use
+ * it; calls of other dims may, one after the other. */
 retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, size_t* bytes);
 
 /* Dense causal attention of a ragged batch over the paged cache: row at position

@@ -14,9 +14,12 @@
 //     (maximum, sum, output) at the end; bound by reading the cache;
 //   - many rows: 32 of 256 rows each, all over the same 64 keys (fp32: 32), which
 //     are copied into LDS for all, one stage ahead; bound by the matrix cores.
-// Long sequences are cut along the keys where there are too few tiles to fill the
-// GPU; a second launch joins the parts.  The units are laid out on the device,
-// from the arrays of the call, by every workgroup for itself.
+// The work is laid out on the device, from the arrays of the call, by every
+// workgroup for itself: the steps of all sequences with few rows are one line, cut
+// into equal shares wherever that falls; tiles of many rows are cut along the keys
+// where there are too few of them to fill the GPU.  A tile's parts go to the
+// workspace, written and read past the L2s of the XCDs, and the workgroup that
+// finishes the last one joins them.
 //
 // Pages lie in LDS as in memory, cut into 16-byte pieces whose order within a
 // row is xored with the row's number, so that the 16 lanes of a read fall into 16
@@ -47,18 +50,19 @@ struct AttendCall {
   int64_t q_stride;
   void* out;
   float* lse;
-  float* parts;
+  int32_t* counters;
+  float *few, *many;  // parts' results
   int batch, hk, G, hq, max_pages, num_phys;
   float scale;
 };
 
-// ---- the units of a call -------------------------------------------------------------
+// ---- the work of a call ----------------------------------------------------------------
 
 struct Seq {
   Run run;
   int end;     // stored tokens that the rows may see
   int tiles;   // row tiles per KV head
-  int steps;   // steps of 64 keys up to end
+  int steps;   // steps of 64 keys up to end, at least one
   bool few;
 };
 
@@ -70,40 +74,19 @@ __device__ __forceinline__ Seq load_seq(const AttendCall& a, int P, int b) {
   s.tiles = s.few ? (rows > 0) : (int)((rows + kRowsMany - 1) / kRowsMany);
   const int len = b < a.batch && rows ? a.seq_lens[b] : 0;
   s.end = (int)min((int64_t)min(max(len, 0), s.run.pos + s.run.n), (int64_t)a.max_pages * P);
-  s.steps = (s.end + 63) / 64;
+  s.steps = max((s.end + 63) / 64, 1);
   return s;
 }
 
-// What every workgroup agrees on: the steps of a part.
+// What every workgroup agrees on.
 struct Cut {
-  int few, many;
-  __device__ int parts(const Seq& s) const {
-    if (!s.tiles) return 0;
-    const int u = s.few ? few : many;
-    return max((s.steps + u - 1) / u, 1);
-  }
+  int64_t few;        // steps of all sequences of few rows and their KV heads
+  int64_t share;      // a workgroup's share of them
+  int64_t many;       // steps of all tiles of many rows
+  int part;           // most steps of a part of such a tile
 };
 
-struct Unit {
-  int b, tile, h, part, parts;
-  int64_t slot;  // floats in front of its partial result (parts > 1)
-};
-
-constexpr int slot_floats(int rows, int D) { return rows * (D + 2); }
-
-// Sums over the workgroup's threads; scratch: one value per wavefront.
-template <int NW>
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* scratch, int tid) {
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  if ((tid & 63) == 0) scratch[tid >> 6] = x;
-  __syncthreads();
-  int64_t s = 0;
-  for (int i = 0; i < NW; ++i) s += scratch[i];
-  __syncthreads();
-  return s;
-}
-
-template <int NW>
+// Sums over the workgroup's threads; scratch: a value per wavefront.
 __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* scratch, int tid, int64_t& total) {
   const int lane = tid & 63;
   for (int o = 1; o < 64; o <<= 1) {
@@ -114,7 +97,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* scratch, int t
   __syncthreads();
   int64_t base = 0;
   total = 0;
-  for (int i = 0; i < NW; ++i) {
+  for (int i = 0; i < kWaves; ++i) {
     if (i < tid >> 6) base += scratch[i];
     total += scratch[i];
   }
@@ -122,60 +105,64 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* scratch, int t
   return base + x;
 }
 
-template <int NW>
 __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, int64_t* scratch, int tid) {
-  int64_t w = 0;
-  for (int b = tid; b < a.batch; b += 64 * NW) {
+  int64_t few = 0, many = 0;
+  for (int b = tid; b < a.batch; b += kThreads) {
     const Seq s = load_seq(a, P, b);
-    w += (int64_t)s.tiles * s.steps;
+    (s.few ? few : many) += (int64_t)s.tiles * s.steps * a.hk;
   }
-  w = block_sum<NW>(w, scratch, tid) * a.hk;
   Cut c;
-  c.few = max((int)min((w + kCus - 1) / kCus, (int64_t)1 << 30), kMinFew);
-  c.many = max((int)min((w + kManyPerCu * kCus - 1) / (kManyPerCu * kCus), (int64_t)1 << 30), kMinMany);
+  block_scan(few, scratch, tid, c.few);
+  block_scan(many, scratch, tid, c.many);
+  const int64_t n = gridDim.x;
+  c.share = max((c.few + n - 1) / n, (int64_t)kMinFew);
+  c.part = (int)min(max((c.few + c.many + kManyPerCu * n - 1) / (kManyPerCu * n), (int64_t)kMinMany),
+                    (int64_t)1 << 30);
   return c;
 }
 
 struct FindLds {
   int64_t scratch[kWaves];
-  int64_t slot;
-  int b, local;
+  int64_t local, before;
+  int b;
 };
 
-// The sequence that item u belongs to, where a sequence has count(seq) items;
-// slots_before: floats of the partial results of the sequences in front of it.
-template <int NW, typename Count>
-__device__ __forceinline__ bool find_seq(const AttendCall& a, int P, int D, const Cut& cut, int64_t u,
-                                         FindLds& L, int tid, Count&& count, int& b, int64_t& local,
-                                         int64_t& slot) {
-  int64_t base = 0, slots = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64 * NW) {
+// The sequence b that item u belongs to, where a sequence has count(seq) items, and
+// the item's number within it; before: the sum of other(seq) over the sequences in front.
+template <typename Count, typename Other>
+__device__ __forceinline__ bool find_seq(const AttendCall& a, int P, int64_t u, FindLds& L, int tid,
+                                         Count&& count, Other&& other, int& b, int64_t& local,
+                                         int64_t& before) {
+  int64_t base = 0, obase = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
     const Seq s = load_seq(a, P, b0 + tid);
-    const int parts = cut.parts(s);
-    const int64_t n = count(s, parts);
-    const int64_t f = parts > 1 ? (int64_t)s.tiles * a.hk * parts *
-                                      slot_floats(s.few ? kRowsFew : kRowsMany, D) : 0;
-    int64_t total, slots_here;
-    const int64_t upto = base + block_scan<NW>(n, L.scratch, tid, total);
-    const int64_t fupto = slots + block_scan<NW>(f, L.scratch, tid, slots_here);
+    const int64_t n = count(s), f = other(s);
+    int64_t total, ototal;
+    const int64_t upto = base + block_scan(n, L.scratch, tid, total);
+    const int64_t oupto = obase + block_scan(f, L.scratch, tid, ototal);
     if (u >= upto - n && u < upto) {
       L.b = b0 + tid;
-      L.local = (int)(u - (upto - n));
-      L.slot = fupto - f;
+      L.local = u - (upto - n);
+      L.before = oupto - f;
     }
     __syncthreads();
     if (u < base + total) {
-      b = L.b;
+      b = __builtin_amdgcn_readfirstlane(L.b);
       local = L.local;
-      slot = L.slot;
+      before = L.before;
       __syncthreads();
       return true;
     }
     base += total;
-    slots += slots_here;
+    obase += ototal;
   }
   return false;
 }
+
+// A part's result in the workspace: outputs not yet divided, maxima, sums.
+constexpr int slot_floats(int rows, int D) { return rows * (D + 2); }
+constexpr int kCounters = 2 * kManyPerCu * kCus + kCus;  // parts done of each cut tile; zero between calls
+constexpr size_t kCounterBytes = (kCounters * sizeof(int32_t) + 255) & ~size_t(255);
 
 // ---- LDS pieces ----------------------------------------------------------------------
 
@@ -199,6 +186,12 @@ struct Shape {
   static __device__ __forceinline__ int fv(int d) { return d / (16 / CPV) % CPV; }
 };
 
+// what several groups of lanes have of a row's parts
+struct JoinLds {
+  f32x4 o[kThreads];
+  float m[kThreads], l[kThreads];
+};
+
 template <typename T, int D, int P>
 struct ChunkLds {
   using S = Shape<T, D, P>;
@@ -206,8 +199,10 @@ struct ChunkLds {
     char stage[2][S::STAGE];
     char own[S::OWN][2 * S::TILE];
     float o[S::OWN][kRowsFew][S::OROW];
+    JoinLds join;
   } u;
   float m[kWaves][32], l[kWaves][32];
+  int last;
   FindLds find;
 };
 
@@ -415,364 +410,439 @@ __device__ __forceinline__ float natural_lse(float m, float l, float scale) {
   return l == 0.f ? -INFINITY : __builtin_fmaf(m, scale, __builtin_amdgcn_logf(l) * kLn2);
 }
 
+// ---- parts -------------------------------------------------------------------------------
+
+// Stores and loads of parts go past the XCDs' L2s, through a resource per part.
+__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t r, int at, f32x4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4v, v), r, at * 4, 0, kCpolSc1);
+}
+__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t r, int at, float v) {
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, at * 4, 0, kCpolSc1);
+}
+
+// Whether this workgroup is the last of `parts` to come here; its stores and the others' are then done.
+__device__ __forceinline__ bool last_part(int32_t* counter, int parts, int* flag, int tid) {
+  __builtin_amdgcn_s_waitcnt(0);  // this wavefront's stores have been acknowledged
+  __syncthreads();
+  if (tid == 0) {
+    const int n = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (n == parts - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = n == parts - 1;
+  }
+  __syncthreads();
+  return *flag != 0;
+}
+
+// Joins the parts of R rows: slot(p) is part p's result of `rows` rows.  D / 4 lanes
+// take a row; where there are fewer rows than lanes for it, several groups of
+// lanes share a row's parts.  done(row, l, m, d, o): four elements from d on.
+template <int D, typename Slot, typename Done>
+__device__ __forceinline__ void join_parts(JoinLds& L, int R, int rows, int parts, float c, int tid,
+                                           Slot&& slot, Done&& done) {
+  constexpr int LPR = D / 4, SUB = kThreads / LPR, AHEAD = 8;
+  const int sub = tid / LPR, d = tid % LPR * 4;
+  const int groups = max(SUB / R, 1), per = SUB / groups;  // rows at a time
+  for (int r0 = 0; r0 < R; r0 += per) {
+    const int row = r0 + sub % per, grp = sub / per;
+    const bool on = row < R && sub < per * groups;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+    if (on)
+      for (int p0 = grp; p0 < parts; p0 += AHEAD * groups) {
+        f32x4 x[AHEAD];
+        float pm[AHEAD], pl[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          const int p = p0 + i * groups;
+          const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(min(p, parts - 1)));
+          x[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (row * D + d) * 4, 0, kCpolSc1));
+          pm[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (rows * D + row) * 4, 0, kCpolSc1));
+          pl[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (rows * (D + 1) + row) * 4, 0, kCpolSc1));
+          if (p >= parts) pm[i] = -INFINITY;
+        }
+        float mn = m;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) mn = fmaxf(mn, pm[i]);
+        const float mu = mn == -INFINITY ? 0.f : mn;
+        const float keep = __builtin_amdgcn_exp2f((m - mu) * c);
+        l *= keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] *= keep;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          if (p0 + i * groups >= parts) continue;
+          const float e = __builtin_amdgcn_exp2f((pm[i] - mu) * c);
+          l = __builtin_fmaf(e, pl[i], l);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[i][j], o[j]);
+        }
+        m = mn;
+      }
+    if (groups > 1) {
+      L.o[tid] = o;
+      L.m[tid] = m;
+      L.l[tid] = l;
+      __syncthreads();
+      if (on && grp == 0) {
+        float mn = m;
+        for (int g = 1; g < groups; ++g) mn = fmaxf(mn, L.m[tid + g * per * LPR]);
+        const float mu = mn == -INFINITY ? 0.f : mn;
+        l = 0.f;
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < groups; ++g) {
+          const int t = tid + g * per * LPR;
+          const float e = __builtin_amdgcn_exp2f((L.m[t] - mu) * c);
+          l = __builtin_fmaf(e, L.l[t], l);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, L.o[t][j], o[j]);
+        }
+        m = mn;
+      }
+    }
+    if (on && grp == 0) done(row, m, l, d, o);
+  }
+}
+
+  // a sequence's pages: page i's number if it is mapped, else page 0 (never counted)
+  struct Pages {
+    const int32_t* table;
+    int last, num_phys;
+    __device__ __forceinline__ int operator()(int i, bool& bad) const {
+      const int id = sload(table + min(i, last));
+      bad = id < 0 || id >= num_phys;
+      return bad ? 0 : id;
+    }
+    // pages without a mapping among n (those past the end are cut by lengths)
+    template <int N>
+    __device__ __forceinline__ uint32_t bad(int page0) const {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        bool b;
+        (*this)(page0 + i, b);
+        bits |= (uint32_t)b << i;
+      }
+      return bits;
+    }
+  };
+
 // ---- kernel ------------------------------------------------------------------------------
 
 template <typename T, int D, int P>
-__global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a, int snake) {
+__global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   using S = Shape<T, D, P>;
   using R_t = Rows<T, D, P>;
   using Lds_t = ChunkLds<T, D, P>;
   __shared__ __attribute__((aligned(1024))) Lds_t L;
   const int tid = thread_index();
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t lds0 = lds_address(&L);
-  const Cut cut = make_cut<kWaves>(a, P, L.find.scratch, tid);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t st = lds_address(&L.u);
+  const Cut cut = make_cut(a, P, L.find.scratch, tid);
+  const int64_t page_bytes = (int64_t)P * D * sizeof(T), phys_bytes = page_bytes * a.hk;
   // a lane's place within a copy of keys, and of values: pieces in their LDS order
-  const uint32_t kcopy = lane / S::CPR * (D * sizeof(T)) + (lane % S::CPR ^ S::fk(lane / S::CPR)) * 16;
-  const uint32_t vcopy = lane / S::CPV * (P * sizeof(T)) + (lane % S::CPV ^ S::fv(lane / S::CPV)) * 16;
-  // pieces of copy i: rows further on, whose numbers change the order by this
+  uint32_t kcopy, vcopy;
+  {
+    const int lane = tid & 63;
+    kcopy = lane / S::CPR * (D * sizeof(T)) + (lane % S::CPR ^ S::fk(lane / S::CPR)) * 16;
+    vcopy = lane / S::CPV * (P * sizeof(T)) + (lane % S::CPV ^ S::fv(lane / S::CPV)) * 16;
+  }
+  // copy i of a tile: rows further on, whose numbers change the order by this
   constexpr int kRowsPerCopy = 64 / S::CPR;
   auto kxor = [](int i) { return (uint32_t)S::fk(i * kRowsPerCopy & 31) << 4; };
   auto vxor = [](int i) { return S::CPV == 8 ? (uint32_t)(i & 1) << 6 : 0u; };
-  const int64_t page_bytes = (int64_t)P * D * sizeof(T);
 
-  for (int64_t round = 0;; ++round) {
-    // longest first; every other round backwards, eight neighbours (one per XCD) together
-    int64_t k = blockIdx.x;
-    if ((round & 1) && snake) k = (int64_t)(gridDim.x / 8 - 1 - k / 8) * 8 + k % 8;
-    int b;
-    int64_t u, slot;
-    if (!find_seq<kWaves>(a, P, D, cut, round * gridDim.x + k, L.find, tid,
-                          [&](const Seq& s, int parts) { return (int64_t)s.tiles * a.hk * parts; }, b, u,
-                          slot))
-      break;
-    b = __builtin_amdgcn_readfirstlane(b);
-    const int un = __builtin_amdgcn_readfirstlane((int)u);
-    const Seq s = load_seq(a, P, b);
-    // KV head fastest (a head's units meet in one L2), then row tiles, last first
-    const int h = un % a.hk, part = un / a.hk / s.tiles, tile = s.tiles - 1 - un / a.hk % s.tiles;
-    const int R = (int)min((int64_t)s.run.n * a.G - (int64_t)tile * kRowsMany, (int64_t)kRowsMany);
-    const int last = (tile * kRowsMany + R - 1) / a.G;        // last row of the chunk in the tile
-    const int end = min(s.end, s.run.pos + last + 1);         // tokens that the tile sees
-    const int steps = (end + 63) / 64;
-    const int u_steps = s.few ? cut.few : cut.many;
-    const int parts = max((steps + u_steps - 1) / u_steps, 1);
-    if (part >= parts) continue;
-    const int per = (steps + parts - 1) / parts;
-    const int key_begin = part * per * 64, key_end = min(end, (part + 1) * per * 64);
-    const int pages = (s.end + P - 1) / P;
-    const int32_t* pt = a.pt + (int64_t)b * a.max_pages;
-    const char* kh = (const char*)a.kc + h * page_bytes;
-    const char* vh = (const char*)a.vc + h * page_bytes;
-    const int64_t phys_bytes = page_bytes * a.hk;
-    // page i of the sequence: its number if mapped, else page 0 (never counted)
-    auto page_of = [&](int i, bool& bad) {
-      const int id = sload(pt + min(i, max(pages - 1, 0)));
-      bad = id < 0 || id >= a.num_phys;
-      return bad ? 0 : id;
-    };
-    // pages without a mapping among the next n (those past the end are cut by lengths)
-    auto bad_pages = [&](int page0, auto n) {
-      uint32_t bits = 0;
+  auto pages_of = [&](const Seq& s, int b) {
+    return Pages{a.pt + (int64_t)b * a.max_pages, max((s.end + P - 1) / P - 1, 0), a.num_phys};
+  };
+  // row rho of a sequence's rows for KV head h (the last one for those behind it)
+  auto row_at = [&](const Seq& s, int h, int rho, bool& live, int& lim) {
+    live = rho < s.run.n * a.G;
+    const int r = min(rho, s.run.n * a.G - 1);
+    lim = min(s.run.pos + r / a.G, s.end - 1);
+    return (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride +
+           (int64_t)(h * a.G + r % a.G) * D;
+  };
+  // the result of such a row, four elements of d
+  auto finish = [&](const Seq& s, int h, int rho, float m, float l, int d, f32x4 o) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t at = (int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G;
+    store4((T*)a.out + at * D + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (d == 0 && a.lse) a.lse[at] = natural_lse(m, l, a.scale);
+  };
+
+  // ---- few rows: this workgroup's share of the line of steps
+  auto few_rows = [&]() {
+    constexpr int PT = 32 / P;  // pages of a tile
+    const int64_t mine = (int64_t)blockIdx.x * cut.share, upto = min(mine + cut.share, cut.few);
+    for (int64_t pos = mine; pos < upto;) {
+      int b;
+      int64_t local, before;
+      find_seq(a, P, pos, L.find, tid,
+               [&](const Seq& s) { return s.few ? (int64_t)s.tiles * s.steps * a.hk : 0; },
+               [](const Seq&) { return (int64_t)0; }, b, local, before);
+      const Seq s = load_seq(a, P, b);
+      const Pages page_of = pages_of(s, b);
+      const int nr = s.run.n * a.G;
+      // its KV heads, one after the other
+      for (int h = (int)(local / s.steps), step0 = (int)(local - (int64_t)h * s.steps);
+           h < a.hk && pos < upto; ++h, step0 = 0) {
+        const int n = (int)min((int64_t)(s.steps - step0), upto - pos);
+        const int key_begin = step0 * 64, key_end = min(s.end, (step0 + n) * 64);
+        const char* kh = (const char*)a.kc + h * page_bytes;
+        const char* vh = (const char*)a.vc + h * page_bytes;
+        const int lane = thread_index() & 63;
+        R_t rows;
+        rows.init(lane, a.scale);
+        bool live;
+        int lim;
+        const T* qrow = row_at(s, h, lane & 31, live, lim);
+        rows.start(qrow, live, lim);
+        const int lim0 = min(s.run.pos, s.end - 1);
+        const uint32_t ks = st + wave * 2 * S::TILE, vs = ks + S::TILE;
+        auto issue = [&](const char* base, uint32_t to, int key, uint32_t off, auto x) {
 #pragma unroll
-      for (int i = 0; i < decltype(n)::value; ++i) {
-        bool bad;
-        page_of(page0 + i, bad);
-        bits |= (uint32_t)bad << i;
+          for (int pg = 0; pg < PT; ++pg) {
+            bool bad;
+            const char* src = base + page_of(key / P + pg, bad) * phys_bytes;
+#pragma unroll
+            for (int i = 0; i < S::PPP; ++i)
+              copy_to_lds(src + i * 1024, off ^ x(pg * S::PPP + i), to + (pg * S::PPP + i) * 1024);
+          }
+        };
+        int key = key_begin + wave * 32;
+        if (wave < S::OWN && key < key_end) {
+          issue(kh, ks, key, kcopy, kxor);
+          issue(vh, vs, key, vcopy, vxor);
+          for (; key < key_end; key += S::OWN * 32) {
+            const int next = key + S::OWN * 32;
+            const uint32_t bad = page_of.template bad<PT>(key / P);
+            f32x16 sc[1];
+            wait_loads<S::LOADS>();
+            sc[0] = rows.scores(ks);
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+            if (next < key_end) issue(kh, ks, next, kcopy, kxor);
+            if (bad || key + 31 > lim0) {
+              rows.template weights<1, true>(sc, key, bad);
+              if (next < key_end) wait_loads<S::LOADS>();
+              else wait_loads<0>();
+              rows.template values<true>(vs, sc[0], s.end - key, bad);
+            } else {
+              rows.template weights<1, false>(sc, key, bad);
+              if (next < key_end) wait_loads<S::LOADS>();
+              else wait_loads<0>();
+              rows.template values<false>(vs, sc[0], 32, 0);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+            if (next < key_end) issue(vh, vs, next, vcopy, vxor);
+          }
+        }
+        // join the wavefronts' results
+        barrier();
+        const int r = lane & 31;
+        rows.l = rows_half_sum(rows.l);
+        if (lane < 32) {
+          L.m[wave][r] = rows.m;
+          L.l[wave][r] = rows.l;
+        }
+        if (wave < S::OWN && r < nr)
+#pragma unroll
+          for (int i = 0; i < R_t::DT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+              *reinterpret_cast<f32x4*>(&L.u.o[wave][r][i * 32 + 2 * e + 4 * rows.half]) =
+                  f32x4{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
+        barrier();
+        // a part: slot 2 k of workgroup k for what its share begins with, 2 k + 1 for what it ends with
+        const bool whole = n == s.steps;
+        const int64_t k = blockIdx.x;
+        auto slot = [&](int64_t i) { return a.few + i * slot_floats(kRowsFew, D); };
+        const __amdgpu_buffer_rsrc_t part = coherent_rsrc(slot(2 * k + (pos != mine)));
+        for (int i = tid; i < nr * (D / 4); i += kThreads) {
+          const int row = i / (D / 4), d = i % (D / 4) * 4;
+          float m = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < S::OWN; ++w) m = fmaxf(m, L.m[w][row]);
+          const float mu = m == -INFINITY ? 0.f : m;
+          float l = 0.f;
+          f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int w = 0; w < S::OWN; ++w) {
+            const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * rows.c);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
+            l = __builtin_fmaf(e, L.l[w][row], l);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
+          }
+          if (whole) {
+            finish(s, h, row, m, l, d, o);
+          } else {
+            put_part(part, row * D + d, o);
+            if (d == 0) {
+              put_part(part, kRowsFew * D + row, m);
+              put_part(part, kRowsFew * (D + 1) + row, l);
+            }
+          }
+        }
+        if (!whole) {
+          // the tile's steps are start .. start + steps - 1 of the line
+          const int64_t start = pos - step0, k0 = start / cut.share;
+          const int parts = (int)((start + s.steps - 1) / cut.share - k0) + 1;
+          if (last_part(a.counters + k0, parts, &L.last, tid))
+            join_parts<D>(
+                L.u.join, nr, kRowsFew, parts, rows.c, tid,
+                [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != k0 * cut.share)); },
+                [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, row, m, l, d, o); });
+        }
+        barrier();
+        pos += n;
       }
-      return bits;
-    };
-    auto row_at = [&](int rho, bool& live, int& lim) {
-      live = rho < s.run.n * a.G;
-      const int r = min(rho, s.run.n * a.G - 1);
-      lim = min(s.run.pos + r / a.G, s.end - 1);
-      return (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride +
-             (int64_t)(h * a.G + r % a.G) * D;
-    };
-    float* part_o = a.parts + slot + (int64_t)un * slot_floats(s.few ? kRowsFew : kRowsMany, D);
+    }
+  };
 
-    if (s.few) {
-      constexpr int PT = 32 / P;  // pages of a tile
+  // ---- many rows
+  auto many_rows = [&]() {
+    constexpr int PS = S::KEYS / P;  // pages of a stage
+    const int most = (int)cut.part;
+    auto parts_of = [&](int steps) { return (steps + most - 1) / most; };
+    for (int64_t round = 0;; ++round) {
+      // longest first; every other round backwards, eight neighbours (one per XCD) together
+      int64_t k = blockIdx.x;
+      if (round & 1) k = (int64_t)(gridDim.x / 8 - 1 - k / 8) * 8 + k % 8;
+      int b;
+      int64_t u, before;
+      if (!find_seq(a, P, round * gridDim.x + k, L.find, tid,
+                    [&](const Seq& s) { return s.few ? 0 : (int64_t)s.tiles * a.hk * parts_of(s.steps); },
+                    [&](const Seq& s) {
+                      return s.few || s.steps <= most ? 0 : (int64_t)s.tiles * a.hk * parts_of(s.steps);
+                    },
+                    b, u, before))
+        break;
+      const int un = __builtin_amdgcn_readfirstlane((int)u);
+      const Seq s = load_seq(a, P, b);
+      // KV head fastest (a head's units meet in one L2), then row tiles, last first
+      const int h = un % a.hk, part = un / a.hk / s.tiles, back = un / a.hk % s.tiles;
+      const int tile = s.tiles - 1 - back;
+      const int R = (int)min((int64_t)s.run.n * a.G - (int64_t)tile * kRowsMany, (int64_t)kRowsMany);
+      const int last = (tile * kRowsMany + R - 1) / a.G;   // last row of the chunk in the tile
+      const int end = min(s.end, s.run.pos + last + 1);    // tokens that the tile sees
+      const int steps = max((end + 63) / 64, 1), parts = parts_of(steps);
+      if (part >= parts) continue;
+      const int per = (steps + parts - 1) / parts;
+      const int key_begin = part * per * 64, key_end = min(end, (part + 1) * per * 64);
+      const Pages page_of = pages_of(s, b);
+      const char* kh = (const char*)a.kc + h * page_bytes;
+      const char* vh = (const char*)a.vc + h * page_bytes;
       const int lane = thread_index() & 63;
       R_t rows;
       rows.init(lane, a.scale);
+      const int rho0 = tile * kRowsMany + wave * 32;
+      const bool any = rho0 < s.run.n * a.G;
       bool live;
       int lim;
-      const T* qrow = row_at(lane & 31, live, lim);
+      const T* qrow = row_at(s, h, rho0 + (lane & 31), live, lim);
       rows.start(qrow, live, lim);
-      const int lim0 = min(s.run.pos, s.end - 1);
-      const uint32_t ks = lds0 + (uint32_t)offsetof(Lds_t, u) + wave * 2 * S::TILE;
-      const uint32_t vs = ks + S::TILE;
-      auto issue = [&](const char* base, uint32_t to, int key, uint32_t off, auto x) {
+      // the wavefront's rows all see the tokens up to lim0, none sees past lim1
+      const int lim0 = any ? min(s.run.pos + rho0 / a.G, s.end - 1) : -1;
+      const int lim1 =
+          any ? min(s.run.pos + min(rho0 + 31, s.run.n * a.G - 1) / a.G, s.end - 1) : -1;
+      constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
+      static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
+      auto issue = [&](int key, uint32_t to) {
+        bool bad;
+        const int first = wave * MINE, i0 = first % S::PPP;
+        const int64_t off = page_of(key / P + first / S::PPP, bad) * phys_bytes + i0 * 1024;
 #pragma unroll
-        for (int pg = 0; pg < PT; ++pg) {
-          bool bad;
-          const char* src = base + page_of(key / P + pg, bad) * phys_bytes;
+        for (int i = 0; i < MINE; ++i)
+          copy_to_lds(kh + off + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
 #pragma unroll
-          for (int i = 0; i < S::PPP; ++i)
-            copy_to_lds(src + i * 1024, off ^ x(pg * S::PPP + i), to + (pg * S::PPP + i) * 1024);
+        for (int i = 0; i < MINE; ++i)
+          copy_to_lds(vh + off + i * 1024, vcopy ^ vxor(first + i),
+                      to + S::NB * S::TILE + (first + i) * 1024);
+      };
+      auto stage = [&](int key, uint32_t at) {
+        if (key > lim1) return;
+        f32x16 sc[S::NB];
+#pragma unroll
+        for (int i = 0; i < S::NB; ++i) sc[i] = rows.scores(at + i * S::TILE);
+        const uint32_t bad = page_of.template bad<PS>(key / P);
+        const uint32_t v = at + S::NB * S::TILE;
+        if (bad || key + S::KEYS - 1 > lim0) {
+          rows.template weights<S::NB, true>(sc, key, bad);
+#pragma unroll
+          for (int i = 0; i < S::NB; ++i)
+            rows.template values<true>(v + i * S::TILE, sc[i], s.end - key - 32 * i,
+                                       bad >> (i * 32 / P));
+        } else {
+          rows.template weights<S::NB, false>(sc, key, bad);
+#pragma unroll
+          for (int i = 0; i < S::NB; ++i)
+            rows.template values<false>(v + i * S::TILE, sc[i], 32, 0);
         }
       };
-      int key = key_begin + wave * 32;
-      const bool mine = wave < S::OWN && key < key_end;
-      if (mine) {
-        issue(kh, ks, key, kcopy, kxor);
-        issue(vh, vs, key, vcopy, vxor);
-        for (; key < key_end; key += S::OWN * 32) {
-          const int next = key + S::OWN * 32;
-          const uint32_t bad = bad_pages(key / P, std::integral_constant<int, PT>{});
-          f32x16 sc[1];
-          wait_loads<S::LOADS>();
-          sc[0] = rows.scores(ks);
-          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-          if (next < key_end) issue(kh, ks, next, kcopy, kxor);
-          if (bad || key + 31 > lim0) {
-            rows.template weights<1, true>(sc, key, bad);
-            if (next < key_end) wait_loads<S::LOADS>();
-            else wait_loads<0>();
-            rows.template values<true>(vs, sc[0], s.end - key, bad);
-          } else {
-            rows.template weights<1, false>(sc, key, bad);
-            if (next < key_end) wait_loads<S::LOADS>();
-            else wait_loads<0>();
-            rows.template values<false>(vs, sc[0], 32, 0);
-          }
-          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-          if (next < key_end) issue(vh, vs, next, vcopy, vxor);
+      if (key_begin < key_end) {
+        issue(key_begin, st);
+        for (int key = key_begin; key < key_end; key += 2 * S::KEYS) {
+          wait_loads<0>();
+          barrier();
+          if (key + S::KEYS < key_end) issue(key + S::KEYS, st + S::STAGE);
+          stage(key, st);
+          if (key + S::KEYS >= key_end) break;
+          wait_loads<0>();
+          barrier();
+          if (key + 2 * S::KEYS < key_end) issue(key + 2 * S::KEYS, st);
+          stage(key + S::KEYS, st + S::STAGE);
         }
       }
-      // join the wavefronts' results
-      barrier();
-      const int r = lane & 31, nr = s.run.n * a.G;
       rows.l = rows_half_sum(rows.l);
-      if (lane < 32) {
-        L.m[wave][r] = rows.m;
-        L.l[wave][r] = rows.l;
-      }
-      if (wave < S::OWN && r < nr)
+      const int rt = wave * 32 + (lane & 31);
+      auto slot = [&](int p) {
+        return a.many + (before + ((int64_t)p * s.tiles + back) * a.hk + h) * slot_floats(kRowsMany, D);
+      };
+      const __amdgpu_buffer_rsrc_t dst = coherent_rsrc(slot(part));
+      if (rt < R) {
 #pragma unroll
         for (int i = 0; i < R_t::DT; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<f32x4*>(&L.u.o[wave][r][i * 32 + 2 * e + 4 * rows.half]) =
-                f32x4{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
-      barrier();
-      for (int i = tid; i < nr * (D / 4); i += kThreads) {
-        const int row = i / (D / 4), d = i % (D / 4) * 4;
-        float m = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < S::OWN; ++w) m = fmaxf(m, L.m[w][row]);
-        const float mu = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        f32x4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < S::OWN; ++w) {
-          const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * rows.c);
-          const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
-          l = __builtin_fmaf(e, L.l[w][row], l);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
-        }
-        if (parts > 1) {
-          *reinterpret_cast<f32x4*>(part_o + row * D + d) = o;
-          if (d == 0) {
-            part_o[kRowsFew * D + row] = m;
-            part_o[kRowsFew * (D + 1) + row] = l;
+          for (int e = 0; e < 16; e += 4) {
+            const int d = i * 32 + 2 * e + 4 * rows.half;
+            const f32x4 o{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
+            if (parts > 1) put_part(dst, rt * D + d, o);
+            else finish(s, h, tile * kRowsMany + rt, rows.m, rows.l, d, o);
           }
-        } else {
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          const int64_t at = (int64_t)(s.run.row + row / a.G) * a.hq + h * a.G + row % a.G;
-          store4((T*)a.out + at * D + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-          if (d == 0 && a.lse) a.lse[at] = natural_lse(m, l, a.scale);
+        if (parts > 1 && lane < 32) {
+          put_part(dst, kRowsMany * D + rt, rows.m);
+          put_part(dst, kRowsMany * (D + 1) + rt, rows.l);
         }
+      }
+      if (parts > 1) {
+        const int64_t first = before + (int64_t)back * a.hk + h;  // the tile's first part among all
+        if (last_part(a.counters + kCus + first, parts, &L.last, tid))
+          join_parts<D>(L.u.join, R, kRowsMany, parts, rows.c, tid, slot,
+                        [&](int row, float m, float l, int d, f32x4 o) {
+                          finish(s, h, tile * kRowsMany + row, m, l, d, o);
+                        });
       }
       barrier();
-      continue;
     }
+  };
 
-    // ---- many rows
-    constexpr int PS = S::KEYS / P;  // pages of a stage
-    const int lane = thread_index() & 63;
-    R_t rows;
-    rows.init(lane, a.scale);
-    const int rho0 = tile * kRowsMany + wave * 32;
-    const bool any = rho0 < s.run.n * a.G;
-    bool live;
-    int lim;
-    const T* qrow = row_at(rho0 + (lane & 31), live, lim);
-    rows.start(qrow, live, lim);
-    // the wavefront's rows all see the tokens up to lim0, none sees past lim1
-    const int lim0 = any ? min(s.run.pos + rho0 / a.G, s.end - 1) : -1;
-    const int lim1 = any ? min(s.run.pos + min(rho0 + 31, s.run.n * a.G - 1) / a.G, s.end - 1) : -1;
-    constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
-    static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
-    auto issue = [&](int key, uint32_t to) {
-      bool bad;
-      const int first = wave * MINE, i0 = first % S::PPP;
-      const int64_t off = page_of(key / P + first / S::PPP, bad) * phys_bytes + i0 * 1024;
-#pragma unroll
-      for (int i = 0; i < MINE; ++i)
-        copy_to_lds(kh + off + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
-#pragma unroll
-      for (int i = 0; i < MINE; ++i)
-        copy_to_lds(vh + off + i * 1024, vcopy ^ vxor(first + i), to + S::NB * S::TILE + (first + i) * 1024);
-    };
-    const uint32_t st = lds0 + (uint32_t)offsetof(Lds_t, u);
-    auto stage = [&](int key, uint32_t at) {
-      if (key > lim1) return;
-      f32x16 sc[S::NB];
-#pragma unroll
-      for (int i = 0; i < S::NB; ++i) sc[i] = rows.scores(at + i * S::TILE);
-      const uint32_t bad = bad_pages(key / P, std::integral_constant<int, PS>{});
-      const uint32_t v = at + S::NB * S::TILE;
-      if (bad || key + S::KEYS - 1 > lim0) {
-        rows.template weights<S::NB, true>(sc, key, bad);
-#pragma unroll
-        for (int i = 0; i < S::NB; ++i)
-          rows.template values<true>(v + i * S::TILE, sc[i], s.end - key - 32 * i, bad >> (i * 32 / P));
-      } else {
-        rows.template weights<S::NB, false>(sc, key, bad);
-#pragma unroll
-        for (int i = 0; i < S::NB; ++i)
-          rows.template values<false>(v + i * S::TILE, sc[i], 32, 0);
-      }
-    };
-    if (key_begin < key_end) {
-      issue(key_begin, st);
-      for (int key = key_begin; key < key_end; key += 2 * S::KEYS) {
-        wait_loads<0>();
-        barrier();
-        if (key + S::KEYS < key_end) issue(key + S::KEYS, st + S::STAGE);
-        stage(key, st);
-        if (key + S::KEYS >= key_end) break;
-        wait_loads<0>();
-        barrier();
-        if (key + 2 * S::KEYS < key_end) issue(key + 2 * S::KEYS, st);
-        stage(key + S::KEYS, st + S::STAGE);
-      }
+  // Reading the cache for few rows leaves the matrix cores idle and the other way
+  // round: every other workgroup of an XCD begins with the one, the rest with the other.
+  const bool turn = blockIdx.x >> 3 & 1;
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) {
+    if ((i == 0) != turn) {
+      if (cut.many) many_rows();
+    } else {
+      if (cut.few) few_rows();
     }
-    rows.l = rows_half_sum(rows.l);
-    const int rt = wave * 32 + (lane & 31), rho = tile * kRowsMany + rt;
-    if (rho < s.run.n * a.G) {
-      if (parts > 1) {
-#pragma unroll
-        for (int i = 0; i < R_t::DT; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            *reinterpret_cast<f32x4*>(part_o + rt * D + i * 32 + 2 * e + 4 * rows.half) =
-                f32x4{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
-        if (lane < 32) {
-          part_o[kRowsMany * D + rt] = rows.m;
-          part_o[kRowsMany * (D + 1) + rt] = rows.l;
-        }
-      } else {
-        const float inv = rows.l == 0.f ? 0.f : 1.f / rows.l;
-        const int64_t at = (int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G;
-        T* o = (T*)a.out + at * D;
-#pragma unroll
-        for (int i = 0; i < R_t::DT; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            store4(o + i * 32 + 2 * e + 4 * rows.half, rows.acc[i][e] * inv, rows.acc[i][e + 1] * inv,
-                   rows.acc[i][e + 2] * inv, rows.acc[i][e + 3] * inv);
-        if (lane < 32 && a.lse) a.lse[at] = natural_lse(rows.m, rows.l, a.scale);
-      }
-    }
-    barrier();
   }
 }
 
-// Joins the parts of the tiles that were cut: 32 rows of a tile and KV head per workgroup.
-constexpr int kJoinWaves = 4;
-constexpr int kJoinWeights = 64;  // parts whose weights lie in LDS at a time
-
-template <typename T, int D, int P>
-__global__ void __launch_bounds__(64 * kJoinWaves) chunk_join_kernel(AttendCall a) {
-  __shared__ FindLds find;
-  __shared__ float wt[kJoinWeights][32], inv_l[32];
-  const int tid = threadIdx.x;
-  const Cut cut = make_cut<kJoinWaves>(a, P, find.scratch, tid);
-  const float c = a.scale * kLog2e;
-  for (int64_t item = blockIdx.x;; item += gridDim.x) {
-    int b;
-    int64_t u, slot;
-    if (!find_seq<kJoinWaves>(a, P, D, cut, item, find, tid,
-                              [&](const Seq& s, int parts) {
-                                return parts > 1 ? (int64_t)s.tiles * a.hk * (s.few ? 1 : kRowsMany / 32) : 0;
-                              },
-                              b, u, slot))
-      break;
-    const Seq s = load_seq(a, P, b);
-    const int rows_unit = s.few ? kRowsFew : kRowsMany, blocks = rows_unit / 32;
-    const int block = (int)(u % blocks), h = (int)(u / blocks % a.hk), tile = (int)(u / blocks / a.hk);
-    const int R = (int)min((int64_t)s.run.n * a.G - (int64_t)tile * kRowsMany, (int64_t)kRowsMany);
-    const int end = min(s.end, s.run.pos + (tile * kRowsMany + R - 1) / a.G + 1);
-    const int u_steps = s.few ? cut.few : cut.many;
-    const int parts = max(((end + 63) / 64 + u_steps - 1) / u_steps, 1);
-    const int nr = min(R - block * 32, 32);
-    if (parts == 1 || nr <= 0) continue;
-    // part p of the tile is unit (p * tiles + tiles - 1 - tile) * hk + h of the sequence
-    const int64_t unit = slot_floats(rows_unit, D), first = slot + ((int64_t)(s.tiles - 1 - tile) * a.hk + h) * unit,
-                  step = (int64_t)s.tiles * a.hk * unit;
-    const float* p0 = a.parts + first;
-    const float* ml = p0 + rows_unit * D + block * 32;
-    // each row's maximum and sum over the parts
-    const int row = tid & 31;
-    float m = -INFINITY, l = 0.f;
-    if (row < nr) {
-      for (int p = 0; p < parts; ++p) m = fmaxf(m, ml[p * step + row]);
-      const float mu = m == -INFINITY ? 0.f : m;
-      for (int p = 0; p < parts; ++p)
-        l = __builtin_fmaf(__builtin_amdgcn_exp2f((ml[p * step + row] - mu) * c),
-                           ml[p * step + rows_unit + row], l);
-      if (tid < 32) {
-        inv_l[row] = l == 0.f ? 0.f : 1.f / l;
-        const int rho = tile * kRowsMany + block * 32 + row;
-        if (a.lse)
-          a.lse[(int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G] = natural_lse(m, l, a.scale);
-      }
-    }
-    constexpr int ITEMS = 32 * D / 4 / (64 * kJoinWaves);
-    f32x4 o[ITEMS];
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int q0 = 0; q0 < parts; q0 += kJoinWeights) {
-      const int np = min(parts - q0, kJoinWeights);
-      __syncthreads();
-      const float mu = m == -INFINITY ? 0.f : m;
-      for (int p = tid >> 5; p < np; p += 2 * kJoinWaves)
-        if (row < nr) wt[p][row] = __builtin_amdgcn_exp2f((ml[(q0 + p) * step + row] - mu) * c);
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        const int e = tid + i * 64 * kJoinWaves, r = e / (D / 4), d = e % (D / 4) * 4;
-        if (r >= nr) continue;
-#pragma unroll 4
-        for (int p = 0; p < np; ++p) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(p0 + (q0 + p) * step + (block * 32 + r) * D + d);
-          const float w = wt[p][r];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[i][j] = __builtin_fmaf(w, x[j], o[i][j]);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int e = tid + i * 64 * kJoinWaves, r = e / (D / 4), d = e % (D / 4) * 4;
-      if (r >= nr) continue;
-      const int rho = tile * kRowsMany + block * 32 + r;
-      const int64_t at = (int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G;
-      const float w = inv_l[r];
-      store4((T*)a.out + at * D + d, o[i][0] * w, o[i][1] * w, o[i][2] * w, o[i][3] * w);
-    }
-    __syncthreads();
-  }
-}
-
-// The most units that any lengths can give: few rows, many rows.
+// The most tiles and parts that any lengths can give.
 struct Bounds {
-  int64_t few, many;        // tiles of all sequences and KV heads
-  int64_t cut_few, cut_many;  // parts of cut tiles
+  int64_t few, many;  // tiles of all sequences and KV heads
+  int64_t parts;      // parts of cut tiles of many rows
 };
 Bounds bounds(const Geometry& g, int n_rows) {
   Bounds x;
@@ -781,12 +851,11 @@ Bounds bounds(const Geometry& g, int n_rows) {
   x.few = std::min<int64_t>(g.batch, n_rows) * g.hk;
   const int64_t seqs = std::min<int64_t>(g.batch, rows / (kRowsFew + 1));
   x.many = seqs ? (rows / kRowsMany + seqs) * g.hk : 0;
-  // a sequence cut into n >= 2 parts has more than n - 1 >= n / 2 parts' steps; the
-  // parts' steps are at least 1 / kCus (1 / (kManyPerCu kCus)) of all
-  x.cut_few = std::min(x.few * ((steps + kMinFew - 1) / kMinFew), (int64_t)2 * kCus);
-  x.cut_many = std::min(x.many * ((steps + kMinMany - 1) / kMinMany), (int64_t)2 * kManyPerCu * kCus);
-  if (steps <= kMinFew) x.cut_few = 0;
-  if (steps <= kMinMany) x.cut_many = 0;
+  // a tile of n >= 2 parts has more than n - 1 >= n / 2 times a part's most steps, and
+  // that is at least 1 / (kManyPerCu * grid) of all steps
+  x.parts = steps <= kMinMany ? 0
+                              : std::min(x.many * ((steps + kMinMany - 1) / kMinMany),
+                                         (int64_t)2 * kManyPerCu * kCus);
   return x;
 }
 
@@ -797,27 +866,37 @@ bool chunk_attend_supported(const Geometry& g, int n_rows) {
 }
 
 size_t chunk_workspace(const Geometry& g, int n_rows) {
-  const Bounds x = bounds(g, n_rows);
-  const size_t floats = x.cut_few * slot_floats(kRowsFew, g.D) + x.cut_many * slot_floats(kRowsMany, g.D);
-  return (floats * sizeof(float) + 255 & ~size_t(255)) + 256;
+  // every workgroup's share of few rows begins and ends with a part
+  const size_t floats = 2 * (size_t)kCus * slot_floats(kRowsFew, g.D) +
+                        bounds(g, n_rows).parts * slot_floats(kRowsMany, g.D);
+  return kCounterBytes + ((floats * sizeof(float) + 255) & ~size_t(255));
 }
 
 hipError_t launch_chunk_attend(const Geometry& g, const retro_kv_cache& c, const retro_chunk& ch,
                                const void* q, int64_t q_stride, void* out, float* lse, void* ws,
                                hipStream_t s) {
-  const Bounds x = bounds(g, ch.n_rows);
-  const AttendCall a{ch,         c.k_cache, c.v_cache, c.page_table, c.seq_lens, q,
-                     q_stride,   out,       lse,       (float*)ws,   g.batch,    g.hk,
-                     g.G,        g.hq,      g.max_pages, g.num_phys, g.sm_scale};
-  const int64_t most = x.few + x.many + x.cut_few + x.cut_many;
-  const int grid = (int)std::min<int64_t>((most + 7) / 8 * 8, kCus);
-  const int64_t joins = (x.cut_few ? x.few : 0) + (x.cut_many ? x.many * (kRowsMany / 32) : 0);
+  float* few = reinterpret_cast<float*>((char*)ws + kCounterBytes);
+  const AttendCall a{ch,
+                     c.k_cache,
+                     c.v_cache,
+                     c.page_table,
+                     c.seq_lens,
+                     q,
+                     q_stride,
+                     out,
+                     lse,
+                     (int32_t*)ws,
+                     few,
+                     few + 2 * (size_t)kCus * slot_floats(kRowsFew, g.D),
+                     g.batch,
+                     g.hk,
+                     g.G,
+                     g.hq,
+                     g.max_pages,
+                     g.num_phys,
+                     g.sm_scale};
   auto go = [&](auto t, auto d, auto ps) {
-    using T = decltype(t);
-    constexpr int D = decltype(d)::value, P = decltype(ps)::value;
-    chunk_attend_kernel<T, D, P><<<grid, kThreads, 0, s>>>(a, 1);
-    if (joins > 0)
-      chunk_join_kernel<T, D, P><<<(unsigned)std::min<int64_t>(joins, 4 * kCus), 64 * kJoinWaves, 0, s>>>(a);
+    chunk_attend_kernel<decltype(t), decltype(d)::value, decltype(ps)::value><<<kCus, kThreads, 0, s>>>(a);
     return hipGetLastError();
   };
   auto with_page = [&](auto t, auto d) {

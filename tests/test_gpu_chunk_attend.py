@@ -71,7 +71,7 @@ class Batch:
         self.out = torch.full((self.total, hq, d), 5.0).to(TD[dtype]).cuda()
         self.lse = torch.full((self.total, hq), 5.0).cuda()
         self.ws_bytes = B.retro_chunk_workspace_size(self.dims, self.total)
-        self.ws = torch.full((self.ws_bytes,), 255, dtype=torch.uint8, device="cuda")
+        self.ws = torch.zeros(self.ws_bytes, dtype=torch.uint8, device="cuda")
         print(f"[chunk] {dtype} hk={hk} G={G} d={d} P={P} seqs={seqs[:6]} unmapped={list(unmapped)}", flush=True)
 
     def run(self, lse=True):
