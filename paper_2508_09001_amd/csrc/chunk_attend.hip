@@ -281,8 +281,17 @@ struct Rows {
     lim = limit;
   }
 
-  // S^T of one tile of keys
-  __device__ __forceinline__ f32x16 scores(uint32_t keys) const {
+  // tiles are read from here on (LDS addresses), or `by` bytes further on
+  __device__ __forceinline__ void read_from(uint32_t keys, uint32_t vals) {
+#pragma unroll
+    for (int i = 0; i < S::QC; ++i) koff[i] += keys;
+#pragma unroll
+    for (int i = 0; i < S::CPV / 2; ++i) voff[i] += vals;
+  }
+  __device__ __forceinline__ void move_by(uint32_t by) { read_from(by, by); }
+
+  // S^T of the tile of keys `keys` bytes on
+  __device__ __forceinline__ f32x16 scores(int keys) const {
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -352,12 +361,12 @@ struct Rows {
   // O^T += V^T P^T of one tile.  Masked: values of slots that hold no token of the
   // sequence (stored: tokens of it from this tile's first key on) are taken as zero.
   template <bool MASK>
-  __device__ __forceinline__ void values(uint32_t at, const f32x16& p, int stored, uint32_t bad) {
+  __device__ __forceinline__ void values(int at, const f32x16& p, int stored, uint32_t bad) {
     constexpr int STEPS = 32 / (2 * S::E);  // key pieces of a lane half
 #pragma unroll
     for (int t = 0; t < STEPS; ++t) {
       const int piece = 2 * t;  // (+ half) of the tile; pieces of a page: CPV
-      const uint32_t off = at + voff[piece % S::CPV / 2] + piece / S::CPV * (D * P * sizeof(T));
+      const int more = at + piece / S::CPV * (int)(D * P * sizeof(T));
       [[maybe_unused]] bf16x8 w;
       if constexpr (sizeof(T) == 2) {
         u32x4 x;
@@ -367,7 +376,7 @@ struct Rows {
       }
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
-        u32x4 v = lds_piece<T>(off + i * (32 * P * sizeof(T)));
+        u32x4 v = lds_piece<T>(voff[piece % S::CPV / 2] + (more + i * (int)(32 * P * sizeof(T))));
         if constexpr (MASK) {
           const int k = S::E * (piece + half);
           const int n = bad >> (k / P) & 1 ? 0 : stored - k;  // elements that count
@@ -597,43 +606,42 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         int lim;
         const T* qrow = row_at(s, h, lane & 31, live, lim);
         rows.start(qrow, live, lim);
-        const int lim0 = min(s.run.pos, s.end - 1);
         const uint32_t ks = st + wave * 2 * S::TILE, vs = ks + S::TILE;
+        rows.read_from(ks, vs);
+        // copies a tile's keys or values; which of its pages are not mapped
         auto issue = [&](const char* base, uint32_t to, int key, uint32_t off, auto x) {
+          uint32_t bits = 0;
 #pragma unroll
           for (int pg = 0; pg < PT; ++pg) {
             bool bad;
             const char* src = base + page_of(key / P + pg, bad) * phys_bytes;
+            bits |= (uint32_t)bad << pg;
 #pragma unroll
             for (int i = 0; i < S::PPP; ++i)
               copy_to_lds(src + i * 1024, off ^ x(pg * S::PPP + i), to + (pg * S::PPP + i) * 1024);
           }
+          return bits;
         };
         int key = key_begin + wave * 32;
         if (wave < S::OWN && key < key_end) {
-          issue(kh, ks, key, kcopy, kxor);
+          uint32_t bad = issue(kh, ks, key, kcopy, kxor);
           issue(vh, vs, key, vcopy, vxor);
           for (; key < key_end; key += S::OWN * 32) {
             const int next = key + S::OWN * 32;
-            const uint32_t bad = page_of.template bad<PT>(key / P);
             f32x16 sc[1];
             wait_loads<S::LOADS>();
-            sc[0] = rows.scores(ks);
+            sc[0] = rows.scores(0);
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-            if (next < key_end) issue(kh, ks, next, kcopy, kxor);
-            if (bad || key + 31 > lim0) {
-              rows.template weights<1, true>(sc, key, bad);
-              if (next < key_end) wait_loads<S::LOADS>();
-              else wait_loads<0>();
-              rows.template values<true>(vs, sc[0], s.end - key, bad);
-            } else {
-              rows.template weights<1, false>(sc, key, bad);
-              if (next < key_end) wait_loads<S::LOADS>();
-              else wait_loads<0>();
-              rows.template values<false>(vs, sc[0], 32, 0);
-            }
+            uint32_t bad_next = 0;
+            if (next < key_end) bad_next = issue(kh, ks, next, kcopy, kxor);
+            // (masking every tile costs nothing here: the wavefront waits for memory)
+            rows.template weights<1, true>(sc, key, bad);
+            if (next < key_end) wait_loads<S::LOADS>();
+            else wait_loads<0>();
+            rows.template values<true>(0, sc[0], s.end - key, bad);
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
             if (next < key_end) issue(vh, vs, next, vcopy, vxor);
+            bad = bad_next;
           }
         }
         // join the wavefronts' results
@@ -741,16 +749,28 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       int lim;
       const T* qrow = row_at(s, h, rho0 + (lane & 31), live, lim);
       rows.start(qrow, live, lim);
-      // the wavefront's rows all see the tokens up to lim0, none sees past lim1
-      const int lim0 = any ? min(s.run.pos + rho0 / a.G, s.end - 1) : -1;
+      rows.read_from(st, st + S::NB * S::TILE);
+      // Every row sees the tokens up to the first row's; stages behind them, and all
+      // where a page is not mapped, are masked.  No row of the wavefront sees past lim1.
+      const int np = (key_end + P - 1) / P;
+      bool missing = false;
+      for (int i = key_begin / P + tid; i < np; i += kThreads) {
+        const int id = page_of.table[i];
+        missing |= id < 0 || id >= a.num_phys;
+      }
+      const int seen = __syncthreads_or(missing) ? 0 : min(s.run.pos + tile * kRowsMany / a.G, s.end - 1) + 1;
       const int lim1 =
           any ? min(s.run.pos + min(rho0 + 31, s.run.n * a.G - 1) / a.G, s.end - 1) : -1;
       constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
       static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
-      auto issue = [&](int key, uint32_t to) {
+      const int first = wave * MINE;
+      auto page_at = [&](int key) {  // of the wavefront's copies of the stage from this key on
         bool bad;
-        const int first = wave * MINE, i0 = first % S::PPP;
-        const int64_t off = page_of(key / P + first / S::PPP, bad) * phys_bytes + i0 * 1024;
+        return page_of(key / P + first / S::PPP, bad);
+      };
+      uint32_t to = st;
+      auto issue = [&](int page) {
+        const int64_t off = page * phys_bytes + first % S::PPP * 1024;
 #pragma unroll
         for (int i = 0; i < MINE; ++i)
           copy_to_lds(kh + off + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
@@ -759,39 +779,34 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
           copy_to_lds(vh + off + i * 1024, vcopy ^ vxor(first + i),
                       to + S::NB * S::TILE + (first + i) * 1024);
       };
-      auto stage = [&](int key, uint32_t at) {
-        if (key > lim1) return;
-        f32x16 sc[S::NB];
+      int key = key_begin;
+      int32_t by = S::STAGE;  // to the other stage
+      // stages up to key `upto`; in front of each, the copy of the next one is begun
+      auto stages = [&](auto masked, int upto) {
+        constexpr bool MASK = decltype(masked)::value;
+        for (; key < upto; key += S::KEYS) {
+          wait_loads<0>();
+          barrier();
+          to += by;
+          if (key + S::KEYS < key_end) issue(page_at(key + S::KEYS));
+          if (!MASK || key <= lim1) {
+            f32x16 sc[S::NB];
 #pragma unroll
-        for (int i = 0; i < S::NB; ++i) sc[i] = rows.scores(at + i * S::TILE);
-        const uint32_t bad = page_of.template bad<PS>(key / P);
-        const uint32_t v = at + S::NB * S::TILE;
-        if (bad || key + S::KEYS - 1 > lim0) {
-          rows.template weights<S::NB, true>(sc, key, bad);
+            for (int i = 0; i < S::NB; ++i) sc[i] = rows.scores(i * S::TILE);
+            const uint32_t bad = MASK ? page_of.template bad<PS>(key / P) : 0;
+            rows.template weights<S::NB, MASK>(sc, key, bad);
 #pragma unroll
-          for (int i = 0; i < S::NB; ++i)
-            rows.template values<true>(v + i * S::TILE, sc[i], s.end - key - 32 * i,
-                                       bad >> (i * 32 / P));
-        } else {
-          rows.template weights<S::NB, false>(sc, key, bad);
-#pragma unroll
-          for (int i = 0; i < S::NB; ++i)
-            rows.template values<false>(v + i * S::TILE, sc[i], 32, 0);
+            for (int i = 0; i < S::NB; ++i)
+              rows.template values<MASK>(i * S::TILE, sc[i], s.end - key - 32 * i, bad >> (i * 32 / P));
+          }
+          rows.move_by(by);
+          by = -by;
         }
       };
       if (key_begin < key_end) {
-        issue(key_begin, st);
-        for (int key = key_begin; key < key_end; key += 2 * S::KEYS) {
-          wait_loads<0>();
-          barrier();
-          if (key + S::KEYS < key_end) issue(key + S::KEYS, st + S::STAGE);
-          stage(key, st);
-          if (key + S::KEYS >= key_end) break;
-          wait_loads<0>();
-          barrier();
-          if (key + 2 * S::KEYS < key_end) issue(key + 2 * S::KEYS, st);
-          stage(key + S::KEYS, st + S::STAGE);
-        }
+        issue(page_at(key_begin));
+        stages(std::false_type{}, min(seen / S::KEYS * S::KEYS, key_end));
+        stages(std::true_type{}, key_end);
       }
       rows.l = rows_half_sum(rows.l);
       const int rt = wave * 32 + (lane & 31);
