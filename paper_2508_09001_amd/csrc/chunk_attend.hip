@@ -316,19 +316,22 @@ struct Rows {
     return sizeof(T) == 2 ? 16 * (e / 8) + e % 8 : 8 * (e / 4) + e % 4;
   }
 
-  // Scores to weights.  Masked: keys past the lane's last one, and keys of pages
-  // that are not mapped (bit i of bad: page i of the tiles).
-  template <int NB, bool MASK>
-  __device__ __forceinline__ void weights(f32x16 (&s)[NB], int key0, uint32_t bad) {
-    if constexpr (MASK) {
+  // Masked: keys past the lane's last one, and keys of pages that are not mapped (bit
+  // i of bad: page i of the tiles).
+  template <int NB>
+  __device__ __forceinline__ void mask(f32x16 (&s)[NB], int key0, uint32_t bad) const {
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int k = 32 * b + key_of(e) + S::E * half;
-          if (key0 + k > lim || (bad >> (k / P) & 1)) s[b][e] = -INFINITY;
-        }
-    }
+      for (int e = 0; e < 16; ++e) {
+        const int k = 32 * b + key_of(e) + S::E * half;
+        if (key0 + k > lim || (bad >> (k / P) & 1)) s[b][e] = -INFINITY;
+      }
+  }
+
+  // The running maximum with these scores; returns what to take from a score times c.
+  template <int NB>
+  __device__ __forceinline__ float follow(const f32x16 (&s)[NB]) {
     float mx = s[0][0];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -348,14 +351,84 @@ struct Rows {
       l *= a;
       m = mn;
     }
-    const float mc = m == -INFINITY ? 0.f : m * c;
+    return m == -INFINITY ? 0.f : m * c;
+  }
+  __device__ __forceinline__ float weight(float s, float mc) {
+    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, c, -mc));
+    l += w;
+    return w;
+  }
+  template <int NB>
+  __device__ __forceinline__ void weights(f32x16 (&s)[NB], float mc) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], c, -mc));
-        l += s[b][e];
+      for (int e = 0; e < 16; ++e) s[b][e] = weight(s[b][e], mc);
+  }
+
+  // The scores `next` of the tiles of keys from here on, the weights of `s` and their
+  // product with the tiles of values from here on, woven together: a matrix
+  // instruction takes 32 cycles of its unit and 4 to issue, so the vector
+  // instructions of the softmax run beside it, a share of them behind each; LDS is
+  // read four pieces ahead.  (sched_barrier: the compiler keeps this order.)
+  template <int NB>
+  __device__ __forceinline__ void weave(f32x16 (&s)[NB], f32x16 (&next)[NB], float mc) {
+    constexpr int SE = 16 / (32 / (2 * S::E));   // scores of a lane that a step of values takes
+    constexpr int NS = NB * S::QC, STEPS = NB * 16 / SE, TOTAL = NS + STEPS * DT;
+    constexpr int AHEAD = 4, EL = NB * 16, SPAN = TOTAL - DT;
+    u32x4 buf[AHEAD + 1];
+    [[maybe_unused]] bf16x8 w;
+    auto fetch = [&](int i) {
+      if (i < NS) return lds_piece<T>(koff[i / NB] + i % NB * S::TILE);
+      const int st = (i - NS) / DT, dt = (i - NS) % DT;          // step, 32 elements of d
+      const int piece = 2 * (st % (STEPS / NB)), tile = st / (STEPS / NB);
+      return lds_piece<T>(voff[piece % S::CPV / 2] +
+                          (tile * S::TILE + piece / S::CPV * (int)(D * P * sizeof(T)) +
+                           dt * (int)(32 * P * sizeof(T))));
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) buf[i] = fetch(i);
+#pragma unroll
+    for (int i = 0; i < TOTAL; ++i) {
+      if (i + AHEAD < TOTAL) buf[(i + AHEAD) % (AHEAD + 1)] = fetch(i + AHEAD);
+      const u32x4 x = buf[i % (AHEAD + 1)];
+      if (i < NS) {
+        f32x16& n = next[i % NB];
+        if (i < NB)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) n[e] = 0.f;
+        if constexpr (sizeof(T) == 2) {
+          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                      __builtin_bit_cast(bf16x8, q[i / NB]), n, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            n = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(q[i / NB][e]),
+                                                     n, 0, 0, 0);
+        }
+      } else {
+        const int st = (i - NS) / DT, dt = (i - NS) % DT, e0 = st * SE;
+        if constexpr (sizeof(T) == 2) {
+          if (dt == 0) {
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[e] = pack_bf16(s[e0 / 16][e0 % 16 + 2 * e], s[e0 / 16][e0 % 16 + 2 * e + 1]);
+            w = __builtin_bit_cast(bf16x8, y);
+          }
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), w, acc[dt], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), s[e0 / 16][e0 % 16 + e],
+                                                           acc[dt], 0, 0, 0);
+        }
       }
+#pragma unroll
+      for (int e = min(i * EL / SPAN, EL); e < min((i + 1) * EL / SPAN, EL); ++e)
+        s[e / 16][e % 16] = weight(s[e / 16][e % 16], mc);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
   // O^T += V^T P^T of one tile.  Masked: values of slots that hold no token of the
@@ -635,7 +708,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
             uint32_t bad_next = 0;
             if (next < key_end) bad_next = issue(kh, ks, next, kcopy, kxor);
             // (masking every tile costs nothing here: the wavefront waits for memory)
-            rows.template weights<1, true>(sc, key, bad);
+            rows.mask(sc, key, bad);
+            rows.weights(sc, rows.follow(sc));
             if (next < key_end) wait_loads<S::LOADS>();
             else wait_loads<0>();
             rows.template values<true>(0, sc[0], s.end - key, bad);
@@ -769,44 +843,85 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         return page_of(key / P + first / S::PPP, bad);
       };
       uint32_t to = st;
-      auto issue = [&](int page) {
-        const int64_t off = page * phys_bytes + first % S::PPP * 1024;
+      auto copy_keys = [&](int page) {
+        const char* src = kh + page * phys_bytes + first % S::PPP * 1024;
 #pragma unroll
         for (int i = 0; i < MINE; ++i)
-          copy_to_lds(kh + off + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
+          copy_to_lds(src + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
+      };
+      auto copy_values = [&](int page) {
+        const char* src = vh + page * phys_bytes + first % S::PPP * 1024;
 #pragma unroll
         for (int i = 0; i < MINE; ++i)
-          copy_to_lds(vh + off + i * 1024, vcopy ^ vxor(first + i),
+          copy_to_lds(src + i * 1024, vcopy ^ vxor(first + i),
                       to + S::NB * S::TILE + (first + i) * 1024);
       };
-      int key = key_begin;
+      // A stage of LDS holds 64 keys' values and the next 64 keys: while the weights of
+      // one are taken, the scores of the next are made.
+      int key = key_begin, page = 0, page_next = 0;
       int32_t by = S::STAGE;  // to the other stage
-      // stages up to key `upto`; in front of each, the copy of the next one is begun
-      auto stages = [&](auto masked, int upto) {
-        constexpr bool MASK = decltype(masked)::value;
-        for (; key < upto; key += S::KEYS) {
-          wait_loads<0>();
-          barrier();
-          to += by;
-          if (key + S::KEYS < key_end) issue(page_at(key + S::KEYS));
-          if (!MASK || key <= lim1) {
-            f32x16 sc[S::NB];
-#pragma unroll
-            for (int i = 0; i < S::NB; ++i) sc[i] = rows.scores(i * S::TILE);
-            const uint32_t bad = MASK ? page_of.template bad<PS>(key / P) : 0;
-            rows.template weights<S::NB, MASK>(sc, key, bad);
-#pragma unroll
-            for (int i = 0; i < S::NB; ++i)
-              rows.template values<MASK>(i * S::TILE, sc[i], s.end - key - 32 * i, bad >> (i * 32 / P));
-          }
-          rows.move_by(by);
-          by = -by;
-        }
+      // in front of the work on the stage at `key`: its copies are there, the next one's begin
+      auto turn = [&]() {
+        wait_loads<0>();
+        barrier();
+        to += by;
+        if (key + S::KEYS < key_end) copy_values(page);
+        if (key + 2 * S::KEYS < key_end) copy_keys(page_next);
+        page = page_next;
+        page_next = page_at(key + 3 * S::KEYS);
+      };
+      auto next_stage = [&]() {
+        rows.move_by(by);
+        by = -by;
+        key += S::KEYS;
       };
       if (key_begin < key_end) {
-        issue(page_at(key_begin));
-        stages(std::false_type{}, min(seen / S::KEYS * S::KEYS, key_end));
-        stages(std::true_type{}, key_end);
+        f32x16 sa[S::NB], sb[S::NB];
+        page = page_at(key);
+        page_next = page_at(key + S::KEYS);
+        copy_keys(page);
+        to += by;
+        copy_values(page);
+        if (key + S::KEYS < key_end) copy_keys(page_next);
+        page = page_next;
+        page_next = page_at(key + 2 * S::KEYS);
+        wait_loads<MINE>();
+        barrier();
+#pragma unroll
+        for (int i = 0; i < S::NB; ++i) sa[i] = rows.scores(i * S::TILE);
+        rows.move_by(by);
+        by = -by;
+        // stages that no mask touches, up to the last but one
+        const int clean = min(seen / S::KEYS * S::KEYS, key_end - S::KEYS);
+        auto step = [&](f32x16(&cur)[S::NB], f32x16(&next)[S::NB]) {
+          turn();
+          rows.weave(cur, next, rows.follow(cur));
+          next_stage();
+        };
+        while (key + S::KEYS < clean) {
+          step(sa, sb);
+          step(sb, sa);
+        }
+        if (key < clean) {
+          step(sa, sb);
+#pragma unroll
+          for (int i = 0; i < S::NB; ++i) sa[i] = sb[i];
+        }
+        while (key < key_end) {
+          turn();
+          if (key <= lim1) {
+            const uint32_t bad = page_of.template bad<PS>(key / P);
+            rows.mask(sa, key, bad);
+            rows.weights(sa, rows.follow(sa));
+#pragma unroll
+            for (int i = 0; i < S::NB; ++i)
+              rows.template values<true>(i * S::TILE, sa[i], s.end - key - 32 * i, bad >> (i * 32 / P));
+          }
+          if (key + S::KEYS <= lim1)
+#pragma unroll
+            for (int i = 0; i < S::NB; ++i) sa[i] = rows.scores(i * S::TILE);
+          next_stage();
+        }
       }
       rows.l = rows_half_sum(rows.l);
       const int rt = wave * 32 + (lane & 31);
