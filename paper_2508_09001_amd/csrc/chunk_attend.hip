@@ -39,7 +39,6 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRowsFew = 32;             // rows of a unit in the first way
 constexpr int kRowsMany = 32 * kWaves;   // and in the second
 constexpr int kCus = 256;
-constexpr int kListPages = 4096;         // page numbers in LDS, in a ring
 constexpr int kManyPerCu = 4;            // units of many rows aimed for per compute unit
 constexpr int kMinMany = 8, kMinFew = 4; // least steps of 64 keys of a part
 
@@ -203,7 +202,6 @@ struct ChunkLds {
     JoinLds join;
   } u;
   float m[kWaves][32], l[kWaves][32];
-  int pages[kListPages];
   int last;
   FindLds find;
 };
@@ -358,7 +356,6 @@ struct Rows {
   __device__ __forceinline__ float weight(float s, float mc) {
     const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s, c, -mc));
     l += w;
-    asm("" : "+v"(l));  // here, not all sums at the end
     return w;
   }
   template <int NB>
@@ -829,34 +826,22 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       rows.read_from(st, st + S::NB * S::TILE);
       // Every row sees the tokens up to the first row's; stages behind them, and all
       // where a page is not mapped, are masked.  No row of the wavefront sees past lim1.
-      const int page0 = key_begin / P;
+      const int np = (key_end + P - 1) / P;
       bool missing = false;
-      // Page numbers from page `from` on, into the ring: 0 for pages that are not mapped
-      // and for those behind the sequence's last (the last stage may see the others up
-      // to its end: tokens that no row of the tile sees, but whose values meet zero weights).
-      const int np = (key_end + S::KEYS - 1) / S::KEYS * PS;
-      auto list_pages = [&](int from, int n) {
-        for (int i = from + tid; i < min(from + n, np); i += kThreads) {
-          const int id = i <= page_of.last ? page_of.table[i] : 0;
-          const bool bad = id < 0 || id >= a.num_phys;
-          missing |= bad;
-          L.pages[i % kListPages] = bad ? 0 : id;
-        }
-      };
-      for (int i = page0 + kListPages + tid; i < min(np, page_of.last + 1); i += kThreads) {
+      for (int i = key_begin / P + tid; i < np; i += kThreads) {
         const int id = page_of.table[i];
         missing |= id < 0 || id >= a.num_phys;
       }
-      list_pages(page0, kListPages);
       const int seen = __syncthreads_or(missing) ? 0 : min(s.run.pos + tile * kRowsMany / a.G, s.end - 1) + 1;
       const int lim1 =
           any ? min(s.run.pos + min(rho0 + 31, s.run.n * a.G - 1) / a.G, s.end - 1) : -1;
       constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
       static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
       const int first = wave * MINE;
-      // of the wavefront's copies of the stage from this key on
-      auto page_at = [&](int key) { return L.pages[(key / P + first / S::PPP) % kListPages]; };
-      auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+      auto page_at = [&](int key) {  // of the wavefront's copies of the stage from this key on
+        bool bad;
+        return page_of(key / P + first / S::PPP, bad);
+      };
       uint32_t to = st;
       auto copy_keys = [&](int page) {
         const char* src = kh + page * phys_bytes + first % S::PPP * 1024;
@@ -880,13 +865,9 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         wait_loads<0>();
         barrier();
         to += by;
-        // the ring's other half has been used: page numbers further on
-        const int used = key / P - page0;
-        if (used && used % (kListPages / 2) == 0) list_pages(page0 + used + kListPages / 2, kListPages / 2);
-        const int page_now = uniform(page_next);
         if (key + S::KEYS < key_end) copy_values(page);
-        if (key + 2 * S::KEYS < key_end) copy_keys(page_now);
-        page = page_now;
+        if (key + 2 * S::KEYS < key_end) copy_keys(page_next);
+        page = page_next;
         page_next = page_at(key + 3 * S::KEYS);
       };
       auto next_stage = [&]() {
@@ -896,12 +877,13 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       };
       if (key_begin < key_end) {
         f32x16 sa[S::NB], sb[S::NB];
-        page = uniform(page_at(key));
+        page = page_at(key);
+        page_next = page_at(key + S::KEYS);
         copy_keys(page);
         to += by;
         copy_values(page);
-        page = uniform(page_at(key + S::KEYS));
-        if (key + S::KEYS < key_end) copy_keys(page);
+        if (key + S::KEYS < key_end) copy_keys(page_next);
+        page = page_next;
         page_next = page_at(key + 2 * S::KEYS);
         wait_loads<MINE>();
         barrier();
