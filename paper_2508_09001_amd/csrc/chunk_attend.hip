@@ -9,14 +9,15 @@
 // lane's operand is eight consecutive keys), key i for fp32 (four).
 //
 // A workgroup of eight wavefronts takes a unit of work in one of two ways:
-//   - few rows (at most 32 of a sequence and KV head): the wavefronts take 32 keys
-//     in turn, each through LDS of its own, without barriers, and join their
-//     (maximum, sum, output) at the end; bound by reading the cache;
+//   - 32 rows (all that a sequence has, or where there is too little work for the
+//     other way): the wavefronts take 32 keys in turn, each through LDS of its own,
+//     without barriers, and join their (maximum, sum, output) at the end; bound by
+//     reading the cache;
 //   - many rows: 32 of 256 rows each, all over the same 64 keys (fp32: 32), which
 //     are copied into LDS for all, one stage ahead; bound by the matrix cores.
 // The work is laid out on the device, from the arrays of the call, by every
-// workgroup for itself: the steps of all sequences with few rows are one line, cut
-// into equal shares wherever that falls; tiles of many rows are cut along the keys
+// workgroup for itself: the steps of all tiles of 32 rows are one line, cut into
+// equal shares wherever that falls; tiles of many rows are cut along the keys
 // where there are too few of them to fill the GPU.  A tile's parts go to the
 // workspace, written and read past the L2s of the XCDs, and the workgroup that
 // finishes the last one joins them.
@@ -41,6 +42,7 @@ constexpr int kRowsMany = 32 * kWaves;   // and in the second
 constexpr int kCus = 256;
 constexpr int kManyPerCu = 4;            // units of many rows aimed for per compute unit
 constexpr int kMinMany = 8, kMinFew = 4; // least steps of 64 keys of a part
+constexpr int kLeastMany = 4;            // least steps of tiles of many rows per workgroup
 
 struct AttendCall {
   retro_chunk ch;
@@ -60,30 +62,45 @@ struct AttendCall {
 
 struct Seq {
   Run run;
-  int end;     // stored tokens that the rows may see
-  int tiles;   // row tiles per KV head
-  int steps;   // steps of 64 keys up to end, at least one
-  bool few;
+  int end;    // stored tokens that the rows may see
+  int rows;   // of a KV head
+  bool few;   // they fit one tile of 32
+  __device__ __forceinline__ int tiles(int of) const { return (int)(((int64_t)rows + of - 1) / of); }
+  __device__ __forceinline__ int steps() const { return max((end + 63) / 64, 1); }  // of 64 keys
+  // tokens that the rows in front of `upto` see at most
+  __device__ __forceinline__ int seen(int upto, int G) const {
+    return min(end, run.pos + (min(upto, rows) - 1) / G + 1);
+  }
+  // Where tile i of 32 rows begins in the line of steps of a KV head's tiles.  A tile's
+  // place is as long as its steps or a little longer: tile j sees pos + (32 (j + 1) - 1) / G
+  // + 1 tokens, of which the sum over j < i has no simple form, but a bound on it has.
+  __device__ __forceinline__ int64_t place(int64_t i, int G) const {
+    if (few) return i * steps();
+    return (i * ((int64_t)run.pos + 1) * G + 16 * i * (i + 1)) / (64 * (int64_t)G) + 2 * i;
+  }
 };
 
 __device__ __forceinline__ Seq load_seq(const AttendCall& a, int P, int b) {
   Seq s;
   s.run = b < a.batch ? chunk_run(a.ch, b) : Run{0, 0, 0};
-  const int64_t rows = (int64_t)s.run.n * a.G;
-  s.few = rows <= kRowsFew;
-  s.tiles = s.few ? (rows > 0) : (int)((rows + kRowsMany - 1) / kRowsMany);
-  const int len = b < a.batch && rows ? a.seq_lens[b] : 0;
+  s.rows = s.run.n * a.G;
+  s.few = s.rows <= kRowsFew;
+  const int len = b < a.batch && s.rows ? a.seq_lens[b] : 0;
   s.end = (int)min((int64_t)min(max(len, 0), s.run.pos + s.run.n), (int64_t)a.max_pages * P);
-  s.steps = max((s.end + 63) / 64, 1);
   return s;
 }
 
 // What every workgroup agrees on.
 struct Cut {
-  int64_t few;        // steps of all sequences of few rows and their KV heads
+  bool all_line;      // no tiles of many rows
+  int64_t line;       // steps of all tiles of 32 rows, of all KV heads
   int64_t share;      // a workgroup's share of them
   int64_t many;       // steps of all tiles of many rows
   int part;           // most steps of a part of such a tile
+  __device__ __forceinline__ bool on_line(const Seq& s) const { return s.few || all_line; }
+  __device__ __forceinline__ int64_t line_of(const Seq& s, const AttendCall& a) const {
+    return on_line(s) ? a.hk * s.place(s.tiles(kRowsFew), a.G) : 0;
+  }
 };
 
 // Sums over the workgroup's threads; scratch: a value per wavefront.
@@ -105,18 +122,37 @@ __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* scratch, int t
   return base + x;
 }
 
+// Tiles of 256 rows read a key once from the L2 where those of 32 read it eight times,
+// but a part of one is long (eight steps), and there have to be many parts to fill the
+// GPU: below kLeastMany steps per workgroup all tiles are of 32 rows.  fp32 tiles always
+// are: its matrix instructions are 16 times slower, and the reading does not show.
+template <bool F32>
 __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, int64_t* scratch, int tid) {
-  int64_t few = 0, many = 0;
+  int64_t few = 0, small = 0, many = 0;
   for (int b = tid; b < a.batch; b += kThreads) {
     const Seq s = load_seq(a, P, b);
-    (s.few ? few : many) += (int64_t)s.tiles * s.steps * a.hk;
+    const int64_t line = a.hk * s.place(s.tiles(kRowsFew), a.G);
+    if (F32 || s.few) {
+      few += line;
+    } else {
+      small += line;
+      many += (int64_t)a.hk * s.tiles(kRowsMany) * s.steps();
+    }
   }
   Cut c;
-  block_scan(few, scratch, tid, c.few);
-  block_scan(many, scratch, tid, c.many);
   const int64_t n = gridDim.x;
-  c.share = max((c.few + n - 1) / n, (int64_t)kMinFew);
-  c.part = (int)min(max((c.few + c.many + kManyPerCu * n - 1) / (kManyPerCu * n), (int64_t)kMinMany),
+  block_scan(few, scratch, tid, c.line);
+  c.many = 0;
+  if constexpr (!F32) block_scan(many, scratch, tid, c.many);
+  c.all_line = F32 || c.many < kLeastMany * n;
+  if (!F32 && c.all_line && c.many) {
+    int64_t more;
+    block_scan(small, scratch, tid, more);
+    c.line += more;
+    c.many = 0;
+  }
+  c.share = max((c.line + n - 1) / n, (int64_t)kMinFew);
+  c.part = (int)min(max((c.line + c.many + kManyPerCu * n - 1) / (kManyPerCu * n), (int64_t)kMinMany),
                     (int64_t)1 << 30);
   return c;
 }
@@ -212,9 +248,11 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 
 // 16 bytes per lane from memory at base + offset (a lane's own) to LDS at `to` +
 // 16 lane, asynchronously; counted like a load.  Written out because the compiler
-// waits for every copy in flight in front of any read of LDS.
+// waits for every copy in flight in front of any read of LDS.  (The wait states are
+// those between a vector instruction that writes a scalar register and a load that
+// reads it, which the compiler does not count into text of ours.)
 __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(to), "v"(offset), "s"(base)
                : "memory");
@@ -619,7 +657,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   const int tid = thread_index();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t st = lds_address(&L.u);
-  const Cut cut = make_cut(a, P, L.find.scratch, tid);
+  const Cut cut = make_cut<sizeof(T) == 4>(a, P, L.find.scratch, tid);
   const int64_t page_bytes = (int64_t)P * D * sizeof(T), phys_bytes = page_bytes * a.hk;
   // a lane's place within a copy of keys, and of values: pieces in their LDS order
   uint32_t kcopy, vcopy;
@@ -638,8 +676,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   };
   // row rho of a sequence's rows for KV head h (the last one for those behind it)
   auto row_at = [&](const Seq& s, int h, int rho, bool& live, int& lim) {
-    live = rho < s.run.n * a.G;
-    const int r = min(rho, s.run.n * a.G - 1);
+    live = rho < s.rows;
+    const int r = min(rho, s.rows - 1);
     lim = min(s.run.pos + r / a.G, s.end - 1);
     return (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride +
            (int64_t)(h * a.G + r % a.G) * D;
@@ -652,24 +690,40 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
     if (d == 0 && a.lse) a.lse[at] = natural_lse(m, l, a.scale);
   };
 
-  // ---- few rows: this workgroup's share of the line of steps
+  // ---- tiles of 32 rows: this workgroup's share of the line of steps
   auto few_rows = [&]() {
     constexpr int PT = 32 / P;  // pages of a tile
-    const int64_t mine = (int64_t)blockIdx.x * cut.share, upto = min(mine + cut.share, cut.few);
+    const int64_t mine = (int64_t)blockIdx.x * cut.share, upto = min(mine + cut.share, cut.line);
     for (int64_t pos = mine; pos < upto;) {
       int b;
       int64_t local, before;
-      find_seq(a, P, pos, L.find, tid,
-               [&](const Seq& s) { return s.few ? (int64_t)s.tiles * s.steps * a.hk : 0; },
+      find_seq(a, P, pos, L.find, tid, [&](const Seq& s) { return cut.line_of(s, a); },
                [](const Seq&) { return (int64_t)0; }, b, local, before);
       const Seq s = load_seq(a, P, b);
       const Pages page_of = pages_of(s, b);
-      const int nr = s.run.n * a.G;
-      // its KV heads, one after the other
-      for (int h = (int)(local / s.steps), step0 = (int)(local - (int64_t)h * s.steps);
-           h < a.hk && pos < upto; ++h, step0 = 0) {
-        const int n = (int)min((int64_t)(s.steps - step0), upto - pos);
-        const int key_begin = step0 * 64, key_end = min(s.end, (step0 + n) * 64);
+      const int tiles = s.tiles(kRowsFew);
+      // its KV heads and their tiles, one after the other
+      const int64_t per_head = s.place(tiles, a.G);
+      int h = (int)(local / per_head), tile = 0;
+      local -= h * per_head;
+      for (int n = tiles; n > 1;) {  // the last tile that begins at or in front of local
+        const int half = n / 2;
+        if (s.place(tile + half, a.G) <= local) {
+          tile += half;
+          n -= half;
+        } else {
+          n = half;
+        }
+      }
+      int step0 = (int)(local - s.place(tile, a.G));
+      while (h < a.hk && pos < upto) {
+        const int rho0 = tile * kRowsFew, nr = min(s.rows - rho0, kRowsFew);
+        const int length = (int)(s.place(tile + 1, a.G) - s.place(tile, a.G));
+        const int n = (int)min((int64_t)(length - step0), upto - pos);
+        // (a place's last steps may lie behind the tile's end, in a sequence whose start_pos
+        // is out of range far behind: then nothing is read)
+        const int key_begin = min(step0, 1 << 24) * 64,
+                  key_end = (int)min((int64_t)s.seen(rho0 + kRowsFew, a.G), ((int64_t)step0 + n) * 64);
         const char* kh = (const char*)a.kc + h * page_bytes;
         const char* vh = (const char*)a.vc + h * page_bytes;
         const int lane = thread_index() & 63;
@@ -677,7 +731,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         rows.init(lane, a.scale);
         bool live;
         int lim;
-        const T* qrow = row_at(s, h, lane & 31, live, lim);
+        const T* qrow = row_at(s, h, rho0 + (lane & 31), live, lim);
         rows.start(qrow, live, lim);
         const uint32_t ks = st + wave * 2 * S::TILE, vs = ks + S::TILE;
         rows.read_from(ks, vs);
@@ -735,7 +789,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
                   f32x4{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
         barrier();
         // a part: slot 2 k of workgroup k for what its share begins with, 2 k + 1 for what it ends with
-        const bool whole = n == s.steps;
+        const bool whole = n == length;
         const int64_t k = blockIdx.x;
         auto slot = [&](int64_t i) { return a.few + i * slot_floats(kRowsFew, D); };
         const __amdgpu_buffer_rsrc_t part = coherent_rsrc(slot(2 * k + (pos != mine)));
@@ -756,7 +810,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
             for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
           }
           if (whole) {
-            finish(s, h, row, m, l, d, o);
+            finish(s, h, rho0 + row, m, l, d, o);
           } else {
             put_part(part, row * D + d, o);
             if (d == 0) {
@@ -766,17 +820,22 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
           }
         }
         if (!whole) {
-          // the tile's steps are start .. start + steps - 1 of the line
+          // the tile's steps are start .. start + length - 1 of the line
           const int64_t start = pos - step0, k0 = start / cut.share;
-          const int parts = (int)((start + s.steps - 1) / cut.share - k0) + 1;
+          const int parts = (int)((start + length - 1) / cut.share - k0) + 1;
           if (last_part(a.counters + k0, parts, &L.last, tid))
             join_parts<D>(
                 L.u.join, nr, kRowsFew, parts, rows.c, tid,
                 [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != k0 * cut.share)); },
-                [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, row, m, l, d, o); });
+                [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, rho0 + row, m, l, d, o); });
         }
         barrier();
         pos += n;
+        step0 = 0;
+        if (++tile == tiles) {
+          tile = 0;
+          ++h;
+        }
       }
     }
   };
@@ -793,20 +852,24 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       int b;
       int64_t u, before;
       if (!find_seq(a, P, round * gridDim.x + k, L.find, tid,
-                    [&](const Seq& s) { return s.few ? 0 : (int64_t)s.tiles * a.hk * parts_of(s.steps); },
                     [&](const Seq& s) {
-                      return s.few || s.steps <= most ? 0 : (int64_t)s.tiles * a.hk * parts_of(s.steps);
+                      return s.few ? 0 : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
+                    },
+                    [&](const Seq& s) {
+                      return s.few || s.steps() <= most
+                                 ? 0
+                                 : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
                     },
                     b, u, before))
         break;
       const int un = __builtin_amdgcn_readfirstlane((int)u);
       const Seq s = load_seq(a, P, b);
       // KV head fastest (a head's units meet in one L2), then row tiles, last first
-      const int h = un % a.hk, part = un / a.hk / s.tiles, back = un / a.hk % s.tiles;
-      const int tile = s.tiles - 1 - back;
-      const int R = (int)min((int64_t)s.run.n * a.G - (int64_t)tile * kRowsMany, (int64_t)kRowsMany);
-      const int last = (tile * kRowsMany + R - 1) / a.G;   // last row of the chunk in the tile
-      const int end = min(s.end, s.run.pos + last + 1);    // tokens that the tile sees
+      const int tiles = s.tiles(kRowsMany);
+      const int h = un % a.hk, part = un / a.hk / tiles, back = un / a.hk % tiles;
+      const int tile = tiles - 1 - back;
+      const int R = min(s.rows - tile * kRowsMany, kRowsMany);
+      const int end = s.seen(tile * kRowsMany + R, a.G);   // tokens that the tile sees
       const int steps = max((end + 63) / 64, 1), parts = parts_of(steps);
       if (part >= parts) continue;
       const int per = (steps + parts - 1) / parts;
@@ -818,7 +881,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       R_t rows;
       rows.init(lane, a.scale);
       const int rho0 = tile * kRowsMany + wave * 32;
-      const bool any = rho0 < s.run.n * a.G;
+      const bool any = rho0 < s.rows;
       bool live;
       int lim;
       const T* qrow = row_at(s, h, rho0 + (lane & 31), live, lim);
@@ -834,7 +897,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       }
       const int seen = __syncthreads_or(missing) ? 0 : min(s.run.pos + tile * kRowsMany / a.G, s.end - 1) + 1;
       const int lim1 =
-          any ? min(s.run.pos + min(rho0 + 31, s.run.n * a.G - 1) / a.G, s.end - 1) : -1;
+          any ? min(s.run.pos + min(rho0 + 31, s.rows - 1) / a.G, s.end - 1) : -1;
       constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
       static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
       const int first = wave * MINE;
@@ -926,7 +989,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       rows.l = rows_half_sum(rows.l);
       const int rt = wave * 32 + (lane & 31);
       auto slot = [&](int p) {
-        return a.many + (before + ((int64_t)p * s.tiles + back) * a.hk + h) * slot_floats(kRowsMany, D);
+        return a.many + (before + ((int64_t)p * tiles + back) * a.hk + h) * slot_floats(kRowsMany, D);
       };
       const __amdgpu_buffer_rsrc_t dst = coherent_rsrc(slot(part));
       if (rt < R) {
@@ -962,9 +1025,10 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
 #pragma unroll 1
   for (int i = 0; i < 2; ++i) {
     if ((i == 0) != turn) {
-      if (cut.many) many_rows();
+      if constexpr (sizeof(T) == 2)
+        if (cut.many) many_rows();
     } else {
-      if (cut.few) few_rows();
+      if (cut.line) few_rows();
     }
   }
 }

@@ -117,6 +117,43 @@ def test_chunks(dtype, P, d, hk, G, seqs):
     Batch(dtype, hk, G, d, P, seqs, seed=P + d + G).run().check()
 
 
+# enough work for tiles of 256 rows (bf16), whose stages of 64 keys and parts end inside
+# the sequences: at least 1024 steps of 64 keys over tiles and KV heads
+LARGE = [
+    ([(700, 0), (300, 2500), (64, 1000), (1, 700), (9, 130)], 8, 4),
+    ([(1500, 100), (600, 900)], 8, 1),
+    ([(200, 1500), (130, 3)], 4, 16),
+    ([(517, 1400), (300, 333)], 9, 3),
+]
+
+
+@pytest.mark.parametrize("P,d", [(16, 128), (32, 128), (16, 64), (32, 64)])
+@pytest.mark.parametrize("seqs,hk,G", LARGE, ids=[str(i) for i in range(len(LARGE))])
+def test_large_chunks(P, d, seqs, hk, G):
+    Batch("bf16", hk, G, d, P, seqs, seed=P + d + G).run().check()
+
+
+def test_large_chunk_fp32():
+    Batch("f32", 2, 4, 64, 16, [(700, 0), (300, 1500)], seed=2).run().check()
+
+
+def test_large_chunks_whose_keys_are_cut():
+    """A long context under few tiles: every tile in parts, joined by the last."""
+    Batch("bf16", 2, 4, 128, 16, [(150, 9000), (1, 5000)], seed=12).run().check()
+
+
+def test_large_chunks_and_pages_that_are_not_mapped():
+    un = [(0, 0), (0, 50), (0, 107), (1, 0), (1, 1), (2, 3), (2, 62)]
+    Batch("bf16", 8, 4, 128, 16, [(700, 1000), (300, 0), (40, 960)], seed=13, unmapped=un).run().check()
+
+
+def test_large_chunks_with_fewer_tokens_stored():
+    b = Batch("bf16", 8, 4, 64, 32, [(700, 1000), (300, 800), (300, 0)], seed=14)
+    lens = [1350, 500, 0]
+    b.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    b.run().check(lens)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_pages_that_are_not_mapped_are_left_out(dtype):
     seqs = [(1, 300), (40, 300), (90, 10), (1, 16), (20, 0)]
@@ -147,9 +184,13 @@ def test_many_sequences(dtype):
     Batch(dtype, 2, 2, 64, 16, seqs, seed=6).run().check()
 
 
-def test_no_lse_and_same_results_again():
-    b = Batch("bf16", 2, 4, 128, 16, [(1, 3000), (100, 700)], seed=7).run()
+@pytest.mark.parametrize("hk,seqs", [(2, [(1, 3000), (100, 700)]), (8, [(1, 3000), (400, 2000)])])
+def test_no_lse_and_same_results_again(hk, seqs):
+    b = Batch("bf16", hk, 4, 128, 16, seqs, seed=7).run()
     first, z = b.out.clone(), b.lse.clone()
+    for _ in range(10):
+        b.out.fill_(5.0)
+        assert torch.equal(b.run().out, first)
     b.out.fill_(5.0)
     b.lse.fill_(5.0)
     b.run(lse=False)
@@ -158,9 +199,10 @@ def test_no_lse_and_same_results_again():
     assert torch.equal(b.out, first) and torch.equal(b.lse, z)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_nan_and_infinite_scores(dtype):
-    b = Batch(dtype, 1, 2, 64, 16, [(3, 200), (40, 50)], seed=8)
+@pytest.mark.parametrize("dtype,ctx,more", [("bf16", 50, ()), ("f32", 50, ()),
+                                            ("bf16", 50, [(3000, 3000)] * 4)])   # (few rows, many rows)
+def test_nan_and_infinite_scores(dtype, ctx, more):
+    b = Batch(dtype, 1, 2, 64, 16, [(3, 200), (40, ctx), *more], seed=8)
     b.q[1, 0] = float("nan")                       # sequence 0, its first row, query head 0
     b.kc[b.pt[1, 2].long(), 0, 5, 0] = float("inf")  # position 37 of sequence 1: +-inf with every query
     b.run()
@@ -200,8 +242,9 @@ def test_captured_and_replayed_for_other_rows():
         (b.k, b.v, b.stored), b.seqs, (b.starts, b.rows) = keep, seqs, old
 
 
-def test_another_stream():
-    b = Batch("bf16", 2, 4, 128, 16, [(50, 500), (1, 2000)], seed=10).run()
+@pytest.mark.parametrize("hk,seqs", [(2, [(50, 500), (1, 2000)]), (8, [(500, 1500), (1, 2000)])])
+def test_another_stream(hk, seqs):
+    b = Batch("bf16", hk, 4, 128, 16, seqs, seed=10).run()
     want, z = b.out.clone(), b.lse.clone()
     b.out.fill_(5.0)
     b.lse.fill_(5.0)
