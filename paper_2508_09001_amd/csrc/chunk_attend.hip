@@ -40,7 +40,7 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRowsFew = 32;             // rows of a unit in the first way
 constexpr int kRowsMany = 32 * kWaves;   // and in the second
 constexpr int kCus = 256;
-constexpr int kManyPerCu = 4;            // units of many rows aimed for per compute unit
+constexpr int kManyPerCu = 1;            // units of many rows aimed for per compute unit
 constexpr int kMinMany = 8, kMinFew = 4; // least steps of 64 keys of a part
 constexpr int kLeastMany = 4;            // least steps of tiles of many rows per workgroup
 
@@ -222,10 +222,16 @@ struct Shape {
   static __device__ __forceinline__ int fv(int d) { return d / (16 / CPV) % CPV; }
 };
 
-// what several groups of lanes have of a row's parts
+// Joining parts.  32 rows: what several groups of lanes have of a row's parts.
 struct JoinLds {
   f32x4 o[kThreads];
   float m[kThreads], l[kThreads];
+};
+// Many rows: some parts' maxima, later their weights, and sums; what the rows have so far.
+constexpr int kJoinParts = 16;
+struct JoinManyLds {
+  float w[kJoinParts][kRowsMany], l[kJoinParts][kRowsMany];
+  float m[kRowsMany], sum[kRowsMany], keep[kRowsMany];
 };
 
 template <typename T, int D, int P>
@@ -236,6 +242,7 @@ struct ChunkLds {
     char own[S::OWN][2 * S::TILE];
     float o[S::OWN][kRowsFew][S::OROW];
     JoinLds join;
+    JoinManyLds join_many;
   } u;
   float m[kWaves][32], l[kWaves][32];
   int last;
@@ -251,11 +258,19 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // waits for every copy in flight in front of any read of LDS.  (The wait states are
 // those between a vector instruction that writes a scalar register and a load that
 // reads it, which the compiler does not count into text of ours.)
+// ONCE: not kept in the caches (16 tokens at 8K to 32K, 1.15 GB: 212 -> 196 us).
+template <bool ONCE>
 __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
-               :
-               : "s"(to), "v"(offset), "s"(base)
-               : "memory");
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                 :
+                 : "s"(to), "v"(offset), "s"(base)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"(to), "v"(offset), "s"(base)
+                 : "memory");
 }
 // until at most N of the wavefront's loads and copies are in flight
 template <int N>
@@ -553,11 +568,11 @@ __device__ __forceinline__ bool last_part(int32_t* counter, int parts, int* flag
   return *flag != 0;
 }
 
-// Joins the parts of R rows: slot(p) is part p's result of `rows` rows.  D / 4 lanes
+// Joins the parts of R of a tile's 32 rows: slot(p) is part p's result.  D / 4 lanes
 // take a row; where there are fewer rows than lanes for it, several groups of
 // lanes share a row's parts.  done(row, l, m, d, o): four elements from d on.
 template <int D, typename Slot, typename Done>
-__device__ __forceinline__ void join_parts(JoinLds& L, int R, int rows, int parts, float c, int tid,
+__device__ __forceinline__ void join_few(JoinLds& L, int R, int parts, float c, int tid,
                                            Slot&& slot, Done&& done) {
   constexpr int LPR = D / 4, SUB = kThreads / LPR, AHEAD = 8;
   const int sub = tid / LPR, d = tid % LPR * 4;
@@ -576,8 +591,8 @@ __device__ __forceinline__ void join_parts(JoinLds& L, int R, int rows, int part
           const int p = p0 + i * groups;
           const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(min(p, parts - 1)));
           x[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (row * D + d) * 4, 0, kCpolSc1));
-          pm[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (rows * D + row) * 4, 0, kCpolSc1));
-          pl[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (rows * (D + 1) + row) * 4, 0, kCpolSc1));
+          pm[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (kRowsFew * D + row) * 4, 0, kCpolSc1));
+          pl[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (kRowsFew * (D + 1) + row) * 4, 0, kCpolSc1));
           if (p >= parts) pm[i] = -INFINITY;
         }
         float mn = m;
@@ -645,6 +660,76 @@ __device__ __forceinline__ void join_parts(JoinLds& L, int R, int rows, int part
       return bits;
     }
   };
+
+// The same for up to 256 rows: a slot is read by all threads at once, 16 bytes of up
+// to 16 rows each (D 128), which keeps 128 KB on the way.  (Row after row, eight parts
+// at a time, nine parts of 256 rows took 100 us: the loads go to memory.)
+template <int D, typename Slot, typename Done>
+__device__ __forceinline__ void join_many(JoinManyLds& L, int R, int parts, float c, int tid,
+                                          Slot&& slot, Done&& done) {
+  constexpr int ITEMS = kRowsMany * (D / 4) / kThreads, PER = kThreads / (D / 4);
+  const int row0 = tid / (D / 4), d = tid % (D / 4) * 4;  // rows row0 + i * PER
+  f32x4 o[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (tid < kRowsMany) {
+    L.m[tid] = -INFINITY;
+    L.sum[tid] = 0.f;
+  }
+  for (int q0 = 0; q0 < parts; q0 += kJoinParts) {
+    const int np = min(parts - q0, kJoinParts);
+    for (int i = tid; i < np * kRowsMany; i += kThreads) {
+      const int p = i / kRowsMany, row = i % kRowsMany;
+      if (row >= R) continue;
+      const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(q0 + p));
+      L.w[p][row] = __uint_as_float(
+          __builtin_amdgcn_raw_buffer_load_b32(r, (kRowsMany * D + row) * 4, 0, kCpolSc1));
+      L.l[p][row] = __uint_as_float(
+          __builtin_amdgcn_raw_buffer_load_b32(r, (kRowsMany * (D + 1) + row) * 4, 0, kCpolSc1));
+    }
+    __syncthreads();
+    if (tid < R) {
+      float m = L.m[tid];
+      for (int p = 0; p < np; ++p) m = fmaxf(m, L.w[p][tid]);
+      const float mu = m == -INFINITY ? 0.f : m, keep = __builtin_amdgcn_exp2f((L.m[tid] - mu) * c);
+      float sum = L.sum[tid] * keep;
+      for (int p = 0; p < np; ++p) {
+        const float w = __builtin_amdgcn_exp2f((L.w[p][tid] - mu) * c);
+        sum = __builtin_fmaf(w, L.l[p][tid], sum);
+        L.w[p][tid] = w;
+      }
+      L.m[tid] = m;
+      L.sum[tid] = sum;
+      L.keep[tid] = keep;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] *= row0 + i * PER < R ? L.keep[row0 + i * PER] : 0.f;
+    for (int p = 0; p < np; ++p) {
+      const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(q0 + p));
+      f32x4 x[ITEMS];
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int row = min(row0 + i * PER, R - 1);
+        x[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (row * D + d) * 4, 0, kCpolSc1));
+      }
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const float w = L.w[p][min(row0 + i * PER, R - 1)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] = __builtin_fmaf(w, x[i][j], o[i][j]);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    const int row = row0 + i * PER;
+    if (row < R) done(row, L.m[row], L.sum[row], d, o[i]);
+  }
+}
 
 // ---- kernel ------------------------------------------------------------------------------
 
@@ -745,7 +830,10 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
             bits |= (uint32_t)bad << pg;
 #pragma unroll
             for (int i = 0; i < S::PPP; ++i)
-              copy_to_lds(src + i * 1024, off ^ x(pg * S::PPP + i), to + (pg * S::PPP + i) * 1024);
+              if (s.few)  // the only tile of these keys
+                copy_to_lds<true>(src + i * 1024, off ^ x(pg * S::PPP + i), to + (pg * S::PPP + i) * 1024);
+              else
+                copy_to_lds<false>(src + i * 1024, off ^ x(pg * S::PPP + i), to + (pg * S::PPP + i) * 1024);
           }
           return bits;
         };
@@ -824,8 +912,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
           const int64_t start = pos - step0, k0 = start / cut.share;
           const int parts = (int)((start + length - 1) / cut.share - k0) + 1;
           if (last_part(a.counters + k0, parts, &L.last, tid))
-            join_parts<D>(
-                L.u.join, nr, kRowsFew, parts, rows.c, tid,
+            join_few<D>(
+                L.u.join, nr, parts, rows.c, tid,
                 [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != k0 * cut.share)); },
                 [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, rho0 + row, m, l, d, o); });
         }
@@ -910,13 +998,13 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         const char* src = kh + page * phys_bytes + first % S::PPP * 1024;
 #pragma unroll
         for (int i = 0; i < MINE; ++i)
-          copy_to_lds(src + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
+          copy_to_lds<false>(src + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
       };
       auto copy_values = [&](int page) {
         const char* src = vh + page * phys_bytes + first % S::PPP * 1024;
 #pragma unroll
         for (int i = 0; i < MINE; ++i)
-          copy_to_lds(src + i * 1024, vcopy ^ vxor(first + i),
+          copy_to_lds<false>(src + i * 1024, vcopy ^ vxor(first + i),
                       to + S::NB * S::TILE + (first + i) * 1024);
       };
       // A stage of LDS holds 64 keys' values and the next 64 keys: while the weights of
@@ -1010,10 +1098,10 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       if (parts > 1) {
         const int64_t first = before + (int64_t)back * a.hk + h;  // the tile's first part among all
         if (last_part(a.counters + kCus + first, parts, &L.last, tid))
-          join_parts<D>(L.u.join, R, kRowsMany, parts, rows.c, tid, slot,
-                        [&](int row, float m, float l, int d, f32x4 o) {
-                          finish(s, h, tile * kRowsMany + row, m, l, d, o);
-                        });
+          join_many<D>(L.u.join_many, R, parts, rows.c, tid, slot,
+                       [&](int row, float m, float l, int d, f32x4 o) {
+                         finish(s, h, tile * kRowsMany + row, m, l, d, o);
+                       });
       }
       barrier();
     }
