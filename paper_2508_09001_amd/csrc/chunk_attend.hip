@@ -40,9 +40,8 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRowsFew = 32;             // rows of a unit in the first way
 constexpr int kRowsMany = 32 * kWaves;   // and in the second
 constexpr int kCus = 256;
-constexpr int kManyPerCu = 1;            // units of many rows aimed for per compute unit
 constexpr int kMinMany = 8, kMinFew = 4; // least steps of 64 keys of a part
-constexpr int kLeastMany = 4;            // least steps of tiles of many rows per workgroup
+constexpr int kScans = 4;                // prefix sums made together
 
 struct AttendCall {
   retro_chunk ch;
@@ -80,11 +79,12 @@ struct Seq {
   }
 };
 
+__device__ __forceinline__ Seq make_seq(Run run, int end, int G) {
+  const int rows = run.n * G;
+  return Seq{run, end, rows, rows <= kRowsFew};
+}
 __device__ __forceinline__ Seq load_seq(const AttendCall& a, int P, int b) {
-  Seq s;
-  s.run = b < a.batch ? chunk_run(a.ch, b) : Run{0, 0, 0};
-  s.rows = s.run.n * a.G;
-  s.few = s.rows <= kRowsFew;
+  Seq s = make_seq(b < a.batch ? chunk_run(a.ch, b) : Run{0, 0, 0}, 0, a.G);
   const int len = b < a.batch && s.rows ? a.seq_lens[b] : 0;
   s.end = (int)min((int64_t)min(max(len, 0), s.run.pos + s.run.n), (int64_t)a.max_pages * P);
   return s;
@@ -103,101 +103,140 @@ struct Cut {
   }
 };
 
-// Sums over the workgroup's threads; scratch: a value per wavefront.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* scratch, int tid, int64_t& total) {
-  const int lane = tid & 63;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) scratch[tid >> 6] = x;
-  __syncthreads();
-  int64_t base = 0;
-  total = 0;
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < tid >> 6) base += scratch[i];
-    total += scratch[i];
-  }
-  __syncthreads();
-  return base + x;
+// A prefix sum over a wavefront, as wave_inclusive_scan, in 64 bits.
+template <int CTRL, int ROW_MASK, bool BOUND_ZERO>
+__device__ __forceinline__ int64_t dpp_i64(int64_t x) {
+  const uint32_t lo = dpp_i<CTRL, ROW_MASK, BOUND_ZERO>((int)(uint32_t)x);
+  const uint32_t hi = dpp_i<CTRL, ROW_MASK, BOUND_ZERO>((int)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
 }
-
-// Tiles of 256 rows read a key once from the L2 where those of 32 read it eight times,
-// but a part of one is long (eight steps), and there have to be many parts to fill the
-// GPU: below kLeastMany steps per workgroup all tiles are of 32 rows.  fp32 tiles always
-// are: its matrix instructions are 16 times slower, and the reading does not show.
-template <bool F32>
-__device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, int64_t* scratch, int tid) {
-  int64_t few = 0, small = 0, many = 0;
-  for (int b = tid; b < a.batch; b += kThreads) {
-    const Seq s = load_seq(a, P, b);
-    const int64_t line = a.hk * s.place(s.tiles(kRowsFew), a.G);
-    if (F32 || s.few) {
-      few += line;
-    } else {
-      small += line;
-      many += (int64_t)a.hk * s.tiles(kRowsMany) * s.steps();
+__device__ __forceinline__ int64_t wave_scan_i64(int64_t x) {
+  x += dpp_i64<0x111, 0xF, true>(x);
+  x += dpp_i64<0x112, 0xF, true>(x);
+  x += dpp_i64<0x114, 0xF, true>(x);
+  x += dpp_i64<0x118, 0xF, true>(x);
+  x += dpp_i64<0x142, 0xA, false>(x);
+  x += dpp_i64<0x143, 0xC, false>(x);
+  return x;
+}
+// Prefix sums of N values over the workgroup's threads, and their totals.
+template <int N>
+struct Scan {
+  int64_t of[N], total[N];
+};
+template <int N>
+__device__ __forceinline__ void block_scan(Scan<N>& s, int64_t (&scratch)[kScans][kWaves], int tid) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    s.of[j] = wave_scan_i64(s.of[j]);
+    if ((tid & 63) == 63) scratch[j][tid >> 6] = s.of[j];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    int64_t base = 0;
+    s.total[j] = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      if (i < tid >> 6) base += scratch[j][i];
+      s.total[j] += scratch[j][i];
     }
+    s.of[j] += base;
   }
-  Cut c;
-  const int64_t n = gridDim.x;
-  block_scan(few, scratch, tid, c.line);
-  c.many = 0;
-  if constexpr (!F32) block_scan(many, scratch, tid, c.many);
-  c.all_line = F32 || c.many < kLeastMany * n;
-  if (!F32 && c.all_line && c.many) {
-    int64_t more;
-    block_scan(small, scratch, tid, more);
-    c.line += more;
-    c.many = 0;
-  }
-  c.share = max((c.line + n - 1) / n, (int64_t)kMinFew);
-  c.part = (int)min(max((c.line + c.many + kManyPerCu * n - 1) / (kManyPerCu * n), (int64_t)kMinMany),
-                    (int64_t)1 << 30);
-  return c;
+  __syncthreads();
 }
 
 struct FindLds {
-  int64_t scratch[kWaves];
+  int64_t scratch[kScans][kWaves];
   int64_t local, before;
+  int4 first[kThreads];  // run and end of the first sequences
   int b;
 };
+__device__ __forceinline__ Seq first_seq(const FindLds& L, int b, int G) {
+  const int4 x = L.first[b];
+  return make_seq(Run{x.x, x.y, x.z}, x.w, G);
+}
+
+// Tiles of 256 rows read a key once from the L2 where those of 32 read it eight times,
+// but a part of one is long (eight steps, or all) and its joining moves 256 rows.  So
+// where there are few of them, with long sequences and little work in all, all tiles
+// are of 32 rows (us, 32 against 256 rows; 8 KV heads of 4 query heads): 64 rows at 2000
+// tokens 34 and 47, 128 at 4000 49 and 57; but 256 at 2000 53 and 50, 512 at 4000 136
+// and 69, 128 rows of a new prompt 33 and 21.  fp32 tiles always are of 32 rows: its
+// matrix instructions are 16 times slower, and the reading does not show.
+template <bool F32>
+__device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, int tid) {
+  enum { kLine, kSmall, kMany, kTiles };
+  Scan<4> x;
+  for (int j = 0; j < 4; ++j) x.of[j] = 0;
+  for (int b = tid; b < a.batch; b += kThreads) {
+    const Seq s = load_seq(a, P, b);
+    if (b < kThreads) L.first[b] = int4{s.run.row, s.run.n, s.run.pos, s.end};
+    const int64_t line = a.hk * s.place(s.tiles(kRowsFew), a.G);
+    if (F32 || s.few) {
+      x.of[kLine] += line;
+    } else {
+      const int64_t tiles = (int64_t)a.hk * s.tiles(kRowsMany);
+      x.of[kSmall] += line;
+      x.of[kMany] += tiles * s.steps();
+      x.of[kTiles] += tiles;
+    }
+  }
+  block_scan(x, L.scratch, tid);
+  const int64_t n = gridDim.x, many = x.total[kMany], tiles = x.total[kTiles];
+  Cut c;
+  c.all_line = F32 || (many < 5 * n && 8 * tiles < n && many > 16 * tiles);
+  c.line = x.total[kLine] + (c.all_line ? x.total[kSmall] : 0);
+  c.many = c.all_line ? 0 : many;
+  c.share = max((c.line + n - 1) / n, (int64_t)kMinFew);
+  c.part = (int)min(max((c.line + c.many + n - 1) / n, (int64_t)kMinMany), (int64_t)1 << 30);
+  return c;
+}
 
 // The sequence b that item u belongs to, where a sequence has count(seq) items, and
 // the item's number within it; before: the sum of other(seq) over the sequences in front.
 template <typename Count, typename Other>
 __device__ __forceinline__ bool find_seq(const AttendCall& a, int P, int64_t u, FindLds& L, int tid,
-                                         Count&& count, Other&& other, int& b, int64_t& local,
+                                         Count&& count, Other&& other, Seq& seq, int& b, int64_t& local,
                                          int64_t& before) {
   int64_t base = 0, obase = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
-    const Seq s = load_seq(a, P, b0 + tid);
-    const int64_t n = count(s), f = other(s);
-    int64_t total, ototal;
-    const int64_t upto = base + block_scan(n, L.scratch, tid, total);
-    const int64_t oupto = obase + block_scan(f, L.scratch, tid, ototal);
+    const Seq s = b0 ? load_seq(a, P, b0 + tid)
+                     : first_seq(L, min(tid, a.batch - 1), a.G);
+    const bool is = b0 + tid < a.batch;
+    const int64_t n = is ? count(s) : 0, f = is ? other(s) : 0;
+    Scan<2> x{{n, f}, {}};
+    block_scan(x, L.scratch, tid);
+    const int64_t upto = base + x.of[0];
     if (u >= upto - n && u < upto) {
       L.b = b0 + tid;
       L.local = u - (upto - n);
-      L.before = oupto - f;
+      L.before = obase + x.of[1] - f;
     }
     __syncthreads();
-    if (u < base + total) {
-      b = __builtin_amdgcn_readfirstlane(L.b);
+    if (u < base + x.total[0]) {
+      auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+      b = uniform(L.b);
+      if (b < kThreads) {
+        const int4 x = L.first[b];
+        seq = make_seq(Run{uniform(x.x), uniform(x.y), uniform(x.z)}, uniform(x.w), a.G);
+      } else {
+        seq = load_seq(a, P, b);
+      }
       local = L.local;
       before = L.before;
       __syncthreads();
       return true;
     }
-    base += total;
-    obase += ototal;
+    base += x.total[0];
+    obase += x.total[1];
   }
   return false;
 }
 
 // A part's result in the workspace: outputs not yet divided, maxima, sums.
 constexpr int slot_floats(int rows, int D) { return rows * (D + 2); }
-constexpr int kCounters = 2 * kManyPerCu * kCus + kCus;  // parts done of each cut tile; zero between calls
+constexpr int kCounters = 2 * kCus + kCus;  // parts done of each cut tile; zero between calls
 constexpr size_t kCounterBytes = (kCounters * sizeof(int32_t) + 255) & ~size_t(255);
 
 // ---- LDS pieces ----------------------------------------------------------------------
@@ -742,7 +781,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   const int tid = thread_index();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t st = lds_address(&L.u);
-  const Cut cut = make_cut<sizeof(T) == 4>(a, P, L.find.scratch, tid);
+  const Cut cut = make_cut<sizeof(T) == 4>(a, P, L.find, tid);
   const int64_t page_bytes = (int64_t)P * D * sizeof(T), phys_bytes = page_bytes * a.hk;
   // a lane's place within a copy of keys, and of values: pieces in their LDS order
   uint32_t kcopy, vcopy;
@@ -780,11 +819,11 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
     constexpr int PT = 32 / P;  // pages of a tile
     const int64_t mine = (int64_t)blockIdx.x * cut.share, upto = min(mine + cut.share, cut.line);
     for (int64_t pos = mine; pos < upto;) {
-      int b;
-      int64_t local, before;
+      int b = 0;
+      int64_t local = 0, before;
+      Seq s;
       find_seq(a, P, pos, L.find, tid, [&](const Seq& s) { return cut.line_of(s, a); },
-               [](const Seq&) { return (int64_t)0; }, b, local, before);
-      const Seq s = load_seq(a, P, b);
+               [](const Seq&) { return (int64_t)0; }, s, b, local, before);
       const Pages page_of = pages_of(s, b);
       const int tiles = s.tiles(kRowsFew);
       // its KV heads and their tiles, one after the other
@@ -939,6 +978,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       if (round & 1) k = (int64_t)(gridDim.x / 8 - 1 - k / 8) * 8 + k % 8;
       int b;
       int64_t u, before;
+      Seq s;
       if (!find_seq(a, P, round * gridDim.x + k, L.find, tid,
                     [&](const Seq& s) {
                       return s.few ? 0 : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
@@ -948,10 +988,9 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
                                  ? 0
                                  : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
                     },
-                    b, u, before))
+                    s, b, u, before))
         break;
       const int un = __builtin_amdgcn_readfirstlane((int)u);
-      const Seq s = load_seq(a, P, b);
       // KV head fastest (a head's units meet in one L2), then row tiles, last first
       const int tiles = s.tiles(kRowsMany);
       const int h = un % a.hk, part = un / a.hk / tiles, back = un / a.hk % tiles;
@@ -1134,10 +1173,10 @@ Bounds bounds(const Geometry& g, int n_rows) {
   const int64_t seqs = std::min<int64_t>(g.batch, rows / (kRowsFew + 1));
   x.many = seqs ? (rows / kRowsMany + seqs) * g.hk : 0;
   // a tile of n >= 2 parts has more than n - 1 >= n / 2 times a part's most steps, and
-  // that is at least 1 / (kManyPerCu * grid) of all steps
+  // that is at least 1 / grid of all steps
   x.parts = steps <= kMinMany ? 0
                               : std::min(x.many * ((steps + kMinMany - 1) / kMinMany),
-                                         (int64_t)2 * kManyPerCu * kCus);
+                                         (int64_t)2 * kCus);
   return x;
 }
 
