@@ -113,14 +113,15 @@ struct Turn {
     }
   }
 
-  // the weights of a norm for the lane's piece and its partner's
+  // the weights of a norm for the lane's piece and its partner's, as stored
   struct Weights {
-    float own[E], other[E];
+    u32x4 own, other;
   };
   __device__ void weights(const void* w, Weights& out) const {
+    out.own = out.other = u32x4{0, 0, 0, 0};
     if (!w) return;
-    unpack<T>(reinterpret_cast<const u32x4*>(w)[c], out.own);
-    unpack<T>(reinterpret_cast<const u32x4*>(w)[partner(c)], out.other);
+    out.own = reinterpret_cast<const u32x4*>(w)[c];
+    out.other = reinterpret_cast<const u32x4*>(w)[partner(c)];
   }
 
   __device__ u32x4 operator()(u32x4 raw, bool norm, const Weights& w, const Angles& a,
@@ -143,10 +144,13 @@ struct Turn {
       if constexpr (LPV >= 16) ss += dpp_f<kDppMirror>(ss);
       if constexpr (LPV >= 32) ss = rows_pair_sum(ss);
       const float r = 1.0f / sqrtf(ss * (1.0f / D) + eps);
+      float own[E], theirs[E];
+      unpack<T>(w.own, own);
+      unpack<T>(w.other, theirs);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        x[i] = x[i] * r * w.own[i];
-        z[i] = z[i] * r * w.other[i];
+        x[i] = x[i] * r * own[i];
+        z[i] = z[i] * r * theirs[i];
       }
     }
     if (interleaved) {
@@ -168,33 +172,48 @@ struct Turn {
   }
 };
 
-// One wavefront per row and 64 / LPV heads (queries' first, then keys').
-template <typename T, int D>
+// One wavefront per row and ITER times 64 / LPV heads (queries' first, then keys'):
+// the row's angles are read once for them, and their pieces are on the way together.
+template <typename T, int D, int ITER>
 __global__ void __launch_bounds__(256) rotate_qk_kernel(
     retro_rotary r, const int32_t* __restrict__ positions, int rows, int heads_q, int heads_k,
     const T* q, int64_t q_stride, const T* k, int64_t k_stride, T* q_out, T* k_out) {
   using Tn = Turn<T, D>;
   constexpr int VPW = 64 / Tn::LPV;
   const int lane = threadIdx.x & 63;
-  const int groups = (heads_q + heads_k + VPW - 1) / VPW;
+  const int heads = heads_q + heads_k, groups = (heads + ITER * VPW - 1) / (ITER * VPW);
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int row = (int)(unit / groups);
-  const int head = (int)(unit - (int64_t)row * groups) * VPW + lane / Tn::LPV;
-  if (row >= rows || head >= heads_q + heads_k) return;
+  const int head0 = (int)(unit - (int64_t)row * groups) * ITER * VPW + lane / Tn::LPV;
+  if (row >= rows || head0 >= heads) return;
   const int pos = positions ? positions[row] : 0;
-  if (pos < 0) return;
-  const bool is_q = head < heads_q;
-  const T* src = is_q ? q + row * q_stride + head * D : k + row * k_stride + (head - heads_q) * D;
-  T* dst = is_q ? q_out + ((int64_t)row * heads_q + head) * D
-                : k_out + ((int64_t)row * heads_k + head - heads_q) * D;
   const Tn turn(r, lane);
-  const u32x4 raw = reinterpret_cast<const u32x4*>(src)[turn.c];
-  const void* w = is_q ? r.q_norm : r.k_norm;
+  u32x4 raw[ITER];
+  typename Tn::Weights wq, wk;
+#pragma unroll
+  for (int i = 0; i < ITER; ++i) {
+    const int head = min(head0 + i * VPW, heads - 1);
+    const T* src = head < heads_q ? q + row * q_stride + head * D
+                                  : k + row * k_stride + (head - heads_q) * D;
+    raw[i] = reinterpret_cast<const u32x4*>(src)[turn.c];
+  }
+  if (pos < 0) return;
+  turn.weights(r.q_norm, wq);
+  turn.weights(r.k_norm, wk);
   typename Tn::Angles a;
-  typename Tn::Weights wt;
   turn.angles(pos, a);
-  turn.weights(w, wt);
-  reinterpret_cast<u32x4*>(dst)[turn.c] = turn(raw, w != nullptr, wt, a, lane);
+#pragma unroll
+  for (int i = 0; i < ITER; ++i) {
+    const int head = head0 + i * VPW;
+    if (head >= heads) return;
+    const bool is_q = head < heads_q;
+    T* dst = is_q ? q_out + ((int64_t)row * heads_q + head) * D
+                  : k_out + ((int64_t)row * heads_k + head - heads_q) * D;
+    const u32x4 y = turn(raw[i], (is_q ? r.q_norm : r.k_norm) != nullptr, is_q ? wq : wk, a, lane);
+    u32x4* at = reinterpret_cast<u32x4*>(dst) + turn.c;
+    if (ITER > 1) __builtin_nontemporal_store(y, at);  // more than the L2s hold
+    else *at = y;
+  }
 }
 
 // ---- append ------------------------------------------------------------------------
@@ -250,7 +269,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   const int tid = threadIdx.x, lane = tid & 63;
   Run run;
   int page;
-  const int b = find_page(ch, g.batch, PS, lane, blockIdx.x, run, page);
+  // a page's workgroups are neighbours: they read and write neighbouring memory
+  const int kinds = q ? 2 * g.hk : g.hk, kind = blockIdx.x % kinds;
+  const int b = find_page(ch, g.batch, PS, lane, blockIdx.x / kinds, run, page);
   if (b < 0) return;
   const int lp0 = run.pos / PS, lp = lp0 + page;
   // slots of this page that the run fills, and the row of slot 0
@@ -261,21 +282,29 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   typename Tn::Angles a;
   typename Tn::Weights wt;
 
-  if ((int)blockIdx.y >= g.hk) {  // queries
-    const int h0 = (blockIdx.y - g.hk) * g.G;
+  if (kind >= g.hk) {  // queries
+    const int h0 = (kind - g.hk) * g.G;
     turn.weights(r.q_norm, wt);
-    const int nv = (s1 - s0) * g.G;  // vectors: G heads of each row
-    for (int i = tid / LPV; i < nv; i += kAppendThreads / LPV) {
-      const int t = s0 + i / g.G, h = h0 + i % g.G;
-      const u32x4 raw = reinterpret_cast<const u32x4*>(q + (row0 + t) * q_stride + h * D)[turn.c];
+    constexpr int AHEAD = 4;  // heads of a row on the way together
+    for (int t = s0 + tid / LPV; t < s1; t += kAppendThreads / LPV) {
       turn.angles(lp * PS + t, a);
-      reinterpret_cast<u32x4*>(q_out + ((row0 + t) * g.hq + h) * D)[turn.c] =
-          turn(raw, r.q_norm != nullptr, wt, a, lane);
+      for (int g0 = 0; g0 < g.G; g0 += AHEAD) {
+        u32x4 raw[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          raw[i] = reinterpret_cast<const u32x4*>(q + (row0 + t) * q_stride +
+                                                  (h0 + min(g0 + i, g.G - 1)) * D)[turn.c];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (g0 + i < g.G)
+            reinterpret_cast<u32x4*>(q_out + ((row0 + t) * g.hq + h0 + g0 + i) * D)[turn.c] =
+                turn(raw[i], r.q_norm != nullptr, wt, a, lane);
+      }
     }
     return;
   }
 
-  const int h = blockIdx.y;
+  const int h = kind;
   if (page == 0 && h == 0) {  // the sequence's new length: up to its first page that is not mapped
     const int np = run_pages(run, PS);
     if (tid == 0) first_bad = np;
@@ -296,19 +325,29 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   if (phys < 0 || phys >= g.num_phys) return;
   const int64_t blk = ((int64_t)phys * g.hk + h) * PS * D;
   turn.weights(r.k_norm, wt);
-  for (int t = s0 + tid / LPV; t < s1; t += kAppendThreads / LPV) {
-    const u32x4 kr = reinterpret_cast<const u32x4*>(k + (row0 + t) * k_stride + h * D)[turn.c];
-    const u32x4 vr = reinterpret_cast<const u32x4*>(v + (row0 + t) * v_stride + h * D)[turn.c];
+  constexpr int NP = PS * LPV / kAppendThreads;  // passes over a page's rows
+  u32x4 kr[NP], vr[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int t = tid / LPV + i * (kAppendThreads / LPV);
+    if (t < s0 || t >= s1) continue;
+    kr[i] = reinterpret_cast<const u32x4*>(k + (row0 + t) * k_stride + h * D)[turn.c];
+    vr[i] = reinterpret_cast<const u32x4*>(v + (row0 + t) * v_stride + h * D)[turn.c];
+  }
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int t = tid / LPV + i * (kAppendThreads / LPV);
+    if (t < s0 || t >= s1) continue;
     turn.angles(lp * PS + t, a);
-    const u32x4 kt = turn(kr, r.k_norm != nullptr, wt, a, lane);
+    const u32x4 kt = turn(kr[i], r.k_norm != nullptr, wt, a, lane);
     reinterpret_cast<u32x4*>(kc + blk + t * D)[turn.c] = kt;
     *reinterpret_cast<u32x4*>(ks + t * ROW + turn.c * E) = kt;
-    *reinterpret_cast<u32x4*>(vs + t * ROW + turn.c * E) = vr;
+    *reinterpret_cast<u32x4*>(vs + t * ROW + turn.c * E) = vr[i];
   }
   __syncthreads();
   // values: E consecutive tokens of one element of d per piece
   for (int e = tid; e < D * (PS / E); e += kAppendThreads) {
-    const int i = e % D, t0 = e / D * E;
+    const int i = e / (PS / E), t0 = e % (PS / E) * E;
     if (t0 + E <= s0 || t0 >= s1) continue;
     T* dst = vc + blk + (int64_t)i * PS + t0;
     T x[E];
@@ -347,14 +386,25 @@ auto with_type_and_dim(const Geometry& g, F f) {
   return g.D == 128 ? f(float{}, D128{}) : f(float{}, D64{});
 }
 
+// Groups of heads per wavefront: one where there are few rows (64 rows of 40 heads: 4.0
+// us), five where the wavefronts fill the GPU many times over (8192 rows of 40 heads, 172
+// MB: 60 us with one, 54, 52, 49, 48 and 48 with 2, 3, 4, 5 and 8; 40 us, 4.3 TB/s, with
+// the outputs written past the L2s).
+constexpr int kManyGroups = 5;
+int rotate_groups(const Geometry& g, int rows, bool q, bool k) {
+  const int64_t vpw = 64 / (g.D * g.elt / 16), heads = (q ? g.hq : 0) + (int64_t)(k ? g.hk : 0);
+  return rows * ((heads + vpw - 1) / vpw) > 16384 ? kManyGroups : 1;
+}
 int64_t rotate_blocks(const Geometry& g, int rows, bool q, bool k) {
-  const int vpw = 64 / (g.D * g.elt / 16);
+  const int64_t vpw = 64 / (g.D * g.elt / 16) * rotate_groups(g, rows, q, k);
   const int64_t heads = (q ? g.hq : 0) + (int64_t)(k ? g.hk : 0);
   return (rows * ((heads + vpw - 1) / vpw) + 3) / 4;
 }
 
-// every sequence's pages: at most n / P + 2 of each
-int64_t append_units(const Geometry& g, int n_rows) { return n_rows / g.P + 2 * (int64_t)g.batch; }
+// every sequence's pages, at most n / P + 2 of each, times the workgroups of a page
+int64_t append_blocks(const Geometry& g, int n_rows, bool q) {
+  return (n_rows / g.P + 2 * (int64_t)std::min(g.batch, n_rows)) * (q ? 2 : 1) * g.hk;
+}
 
 }  // namespace
 
@@ -374,23 +424,27 @@ hipError_t launch_rotate_qk(const Geometry& g, const retro_rotary& r, const int3
                             int64_t k_stride, void* q_out, void* k_out, hipStream_t s) {
   return with_type_and_dim(g, [&](auto t, auto d) {
     using T = decltype(t);
-    rotate_qk_kernel<T, decltype(d)::value>
-        <<<(unsigned)rotate_blocks(g, rows, q, k), 256, 0, s>>>(
-            r, positions, rows, q ? g.hq : 0, k ? g.hk : 0, (const T*)q, q_stride, (const T*)k,
-            k_stride, (T*)q_out, (T*)k_out);
-    return hipGetLastError();
+    auto go = [&](auto iter) {
+      rotate_qk_kernel<T, decltype(d)::value, decltype(iter)::value>
+          <<<(unsigned)rotate_blocks(g, rows, q, k), 256, 0, s>>>(
+              r, positions, rows, q ? g.hq : 0, k ? g.hk : 0, (const T*)q, q_stride, (const T*)k,
+              k_stride, (T*)q_out, (T*)k_out);
+      return hipGetLastError();
+    };
+    return rotate_groups(g, rows, q, k) == 1 ? go(std::integral_constant<int, 1>{})
+                                             : go(std::integral_constant<int, kManyGroups>{});
   });
 }
 
 bool append_rotary_supported(const Geometry& g, int n_rows) {
-  return append_units(g, n_rows) < (int64_t)1 << 31 && g.hk <= 32767;
+  return append_blocks(g, n_rows, true) < (int64_t)1 << 31;
 }
 
 hipError_t launch_append_rotary(const Geometry& g, int step, const retro_kv_cache& c,
                                 const retro_chunk& ch, const retro_rotary& r, const void* q,
                                 int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, void* q_out, hipStream_t s) {
-  const dim3 grid((unsigned)append_units(g, ch.n_rows), (unsigned)(q ? 2 * g.hk : g.hk));
+  const unsigned grid = (unsigned)append_blocks(g, ch.n_rows, q != nullptr);
   return with_type_and_dim(g, [&](auto t, auto d) {
     using T = decltype(t);
     auto go = [&](auto ps) {
