@@ -18,8 +18,15 @@ residual add and the next layer's bf16 input), both bf16 in, fp32 accumulation,
 bf16 out.  fp32 stacks use ``retro_project_f32`` (fp32 fused multiply-add
 chains on the unpacked weights, the output projection added into the residual
 stream in place).
-Feed-forward blocks and normalisation are left out: they do not touch the KV
-cache.
+Feed-forward blocks and their normalisation are left out: they do not touch the
+KV cache.
+
+With ``rotary`` queries and keys carry their positions: every window row's query
+and key is normalised (where a layer has ``q_norm`` / ``k_norm``) and rotated to the
+row's own position (``retro_rotate_qk``) before UpdateKV and the step.
+``prefill_chunk`` runs prompts, or chunks of them, through the stack: rotated
+append (``retro_append_kv_rotary``) and dense causal attention
+(``retro_chunk_attend``) in every layer, the large products on torch.matmul.
 """
 from __future__ import annotations
 
@@ -28,7 +35,7 @@ from typing import List, Optional, Sequence
 import torch
 
 from . import binding as B
-from .layer import RetroLayer
+from .layer import RetroLayer, RetroRotary
 
 
 class RetroDecoder:
@@ -42,10 +49,15 @@ class RetroDecoder:
     the products on torch.matmul (for comparison); with the library projections,
     ``fuse_update`` folds UpdateKV into the query / key / value launch
     (``retro_project_qkv_update``) instead of a ``retro_update_kv`` of its own.
+    ``rotary``: None, or a dict of ``rot_dim`` and optionally ``base``, ``interleaved``
+    and ``eps`` (RetroRotary); a layer's weights may then hold ``q_norm`` and ``k_norm``
+    ``[d]``.  Rotation goes between the projections and UpdateKV, which is then a
+    call of its own.
     """
 
     def __init__(self, weights: Sequence[dict], device: str = "cuda",
-                 library_projections: bool = True, fuse_update: bool = True, **layer_kw):
+                 library_projections: bool = True, fuse_update: bool = True,
+                 rotary: Optional[dict] = None, **layer_kw):
         self.device = torch.device(device)
         self.layers: List[RetroLayer] = [RetroLayer(device=device, **layer_kw)
                                          for _ in weights]
@@ -68,6 +80,22 @@ class RetroDecoder:
                 raise ValueError("projection shapes do not match the layer geometry")
             self.weights.append(dw)
         self.decoded = 0  # decode steps run so far
+        # norms and rotation: one table of angles for all layers
+        positions = lay.dims.max_pages * lay.P
+        opts = dict(rotary or {}, dtype=layer_kw.get("dtype", "bf16"), device=device)
+        rot_dim = opts.pop("rot_dim", 0)
+        if rotary is None and any(w.get(n) is not None for w in weights
+                                  for n in ("q_norm", "k_norm")):
+            raise ValueError("q_norm and k_norm need rotary (rot_dim 0: norms alone)")
+        self.rotated = rotary is not None
+        self.rotary: List[RetroRotary] = []
+        for w in weights:
+            table = self.rotary[0].table if self.rotary and rot_dim else None
+            self.rotary.append(RetroRotary(positions, rot_dim, table=table,
+                                           q_norm=w.get("q_norm"), k_norm=w.get("k_norm"), **opts))
+        if self.rotated:
+            # position of window row r less the tokens stored, row W the newest
+            self.window_offset = torch.arange(-self.W, 1, dtype=torch.int32, device=self.device)
         # bf16: library projections (weights pre-tiled; they need k % 1024 == 0 and
         # at most 112 rows)
         rows = self.batch * (self.W + 1)
@@ -94,7 +122,7 @@ class RetroDecoder:
             self.v = torch.zeros_like(self.k)
             self.k_new = torch.zeros(self.batch, self.hk, self.d, dtype=td, device=dev)
             self.v_new = torch.zeros_like(self.k_new)
-        self.fuse_update = self.fused and fuse_update
+        self.fuse_update = self.fused and fuse_update and not self.rotated
         # fp32: library projections on the unpacked weights (retro_project_f32)
         self.f32_library = library_projections and self.dtype == torch.float32
         if self.f32_library:
@@ -110,6 +138,33 @@ class RetroDecoder:
     def prefill(self, layer: int, seq: int, k, v, stream=None) -> None:
         """Prompt keys and values [n][h_k][d] of one sequence in one layer."""
         self.layers[layer].prefill(seq, k, v, stream)
+
+    def prefill_chunk(self, rows: Sequence[int], emb: torch.Tensor) -> torch.Tensor:
+        """Prompts, or their next chunks, through the whole stack on the current stream:
+        ``rows[b]`` tokens of every sequence, ``emb`` [sum of rows][d_model] on the device,
+        one sequence's rows behind the other's.  Returns the residual stream after the
+        last layer, [sum of rows][d_model] fp32.  May be called between decode steps."""
+        if emb.dim() != 2 or emb.shape[0] != sum(rows) or emb.shape[1] != self.d_model:
+            raise ValueError("emb must be [sum of rows][d_model]")
+        if any(lay._lens != self.layers[0]._lens for lay in self.layers):
+            raise ValueError("the layers hold different numbers of tokens")
+        chunk = self.layers[0].chunk(rows)
+        h = emb.to(device=self.device, dtype=torch.float32)
+        for lay, w, rot in zip(self.layers, self.weights, self.rotary):
+            x = h.to(self.dtype)
+            q = lay.append_chunk(self.decoded, chunk, rot, torch.matmul(x, w["wk"]),
+                                 torch.matmul(x, w["wv"]), torch.matmul(x, w["wq"]))
+            lay.chunk_ws = self.layers[0].chunk_ws  # one for all, used in turn
+            o = lay.attend_chunk(chunk, q)
+            h = h + torch.matmul(o.view(-1, self.hq * self.d), w["wo"]).float()
+        return h
+
+    def _rotate_window(self, lay, rot, q, k) -> None:
+        """Window rows' queries and keys to their positions, in place (rows in front of a
+        sequence's first token stay as they are: no query or key is read there)."""
+        rows = self.batch * (self.W + 1)
+        B.retro_rotate_qk(lay.dims, rot.struct, self.window_pos, rows, q, self.hq * self.d, k,
+                          self.hk * self.d, q, k)
 
     def n_update(self) -> int:
         """Past rows re-embedded this step: the decoded ones among the W."""
@@ -130,16 +185,20 @@ class RetroDecoder:
         if tuple(emb_window.shape) != (b, rows, self.d_model):
             raise ValueError("emb_window must be [batch][W+1][d_model]")
         n_upd = self.n_update()
+        if self.rotated:
+            self.window_pos = self.layers[0].seq_lens[:, None] + self.window_offset
         if self.fused:
             return self._step_fused(t, emb_window, n_upd, trace)
         if self.f32_library:
             return self._step_f32(t, emb_window, n_upd, trace)
         h = emb_window.to(device=self.device, dtype=torch.float32)
-        for lay, w in zip(self.layers, self.weights):
+        for lay, w, rot in zip(self.layers, self.weights, self.rotary):
             x = h.to(self.dtype)
             q = torch.matmul(x, w["wq"]).view(b, rows, self.hq, self.d)
             k = torch.matmul(x, w["wk"]).view(b, rows, self.hk, self.d)
             v = torch.matmul(x, w["wv"]).view(b, rows, self.hk, self.d)
+            if self.rotated:
+                self._rotate_window(lay, rot, q, k)
             if n_upd > 0:
                 lay.update_kv(k[:, W - n_upd:W], v[:, W - n_upd:W])
             lay.step(t, q, k[:, W], v[:, W])
@@ -159,11 +218,13 @@ class RetroDecoder:
         b, rows, W = self.batch, self.W + 1, self.W
         nq, nkv, r = self.hq * self.d, self.hk * self.d, self.batch * (self.W + 1)
         self.h.copy_(emb_window)
-        for lay, w in zip(self.layers, self.weights):
+        for lay, w, rot in zip(self.layers, self.weights, self.rotary):
             h_in = self.h.clone() if trace is not None else None
             B.retro_project_f32(self.h, r, self.d_model, w["wq"], nq, self.q)
             B.retro_project_f32(self.h, r, self.d_model, w["wk"], nkv, self.k)
             B.retro_project_f32(self.h, r, self.d_model, w["wv"], nkv, self.v)
+            if self.rotated:
+                self._rotate_window(lay, rot, self.q, self.k)
             if n_upd > 0:
                 lay.update_kv(self.k[:, W - n_upd:W], self.v[:, W - n_upd:W])
             lay.step(t, self.q, self.k[:, W], self.v[:, W])
@@ -181,7 +242,7 @@ class RetroDecoder:
         nq, nkv = self.hq * self.d, self.hk * self.d
         self.h.copy_(emb_window)
         self.x.copy_(emb_window)
-        for lay, (pq, po) in zip(self.layers, self.packed):
+        for lay, (pq, po), rot in zip(self.layers, self.packed, self.rotary):
             h_in = self.h.clone() if trace is not None else None
             x_in = self.x.clone() if trace is not None else None
             if self.fuse_update:
@@ -191,6 +252,8 @@ class RetroDecoder:
             else:
                 B.retro_project_qkv(self.x, b * rows, self.d_model, pq, nq, nkv, self.q, self.k,
                                     self.v)
+                if self.rotated:
+                    self._rotate_window(lay, rot, self.q, self.k)
                 if n_upd > 0:
                     lay.update_kv(self.k[:, W - n_upd:W], self.v[:, W - n_upd:W])
                 k_new, v_new = self.k[:, W], self.v[:, W]

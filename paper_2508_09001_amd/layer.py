@@ -6,8 +6,9 @@ include/retro.h.
 """
 from __future__ import annotations
 
+import contextlib
 import math
-from typing import Optional
+from typing import Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -15,6 +16,66 @@ from . import binding as B
 
 _TORCH_DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
 _RETRO_DTYPE = {"bf16": B.RETRO_BF16, "f32": B.RETRO_F32}
+
+
+class RetroRotary:
+    """Norms and rotation of a layer's queries and keys (``retro_rotary`` in the header).
+
+    ``positions``: tokens that a position may reach, ``max_pages * page_size`` for
+    ``append_chunk``; ``rot_dim``: the leading elements of a head that rotate (0: none),
+    paired with those ``rot_dim / 2`` further on or, ``interleaved``, with their
+    neighbours; ``q_norm`` / ``k_norm``: weights ``[d]`` of root-mean-square norms, or
+    None.  ``table``: cosines and sines ``[positions][rot_dim / 2][2]`` fp32 of the
+    caller's own, shared between layers (None: made from ``base``)."""
+
+    def __init__(self, positions: int, rot_dim: int, base: float = 10000.0,
+                 interleaved: bool = False, q_norm=None, k_norm=None, eps: float = 1e-6,
+                 dtype: str = "bf16", device: str = "cuda", table: Optional[torch.Tensor] = None):
+        self.device = torch.device(device)
+
+        def weight(w):
+            if w is None:
+                return None
+            if not isinstance(w, torch.Tensor):
+                w = torch.from_numpy(w)
+            return w.to(device=self.device, dtype=_TORCH_DTYPE[dtype]).contiguous()
+
+        self.q_norm, self.k_norm = weight(q_norm), weight(k_norm)
+        self.table = table
+        if rot_dim and table is None:
+            self.table = torch.empty(positions, rot_dim // 2, 2, dtype=torch.float32,
+                                     device=self.device)
+            with _on(self.device):
+                B.retro_rotary_table(self.table, positions, rot_dim, base)
+        elif rot_dim:
+            if tuple(table.shape) != (positions, rot_dim // 2, 2) or \
+               table.dtype != torch.float32 or not table.is_contiguous():
+                raise ValueError("table must be [positions][rot_dim / 2][2] fp32, contiguous")
+        self.struct = B.Rotary(B._ptr(self.table) if rot_dim else None,
+                               positions if rot_dim else 0, rot_dim, 1 if interleaved else 0, eps,
+                               B._ptr(self.q_norm), B._ptr(self.k_norm))
+
+
+class RetroChunk:
+    """A ragged batch of rows (``retro_chunk``): ``rows`` of each sequence, one sequence's
+    behind the other's, from position ``start`` on."""
+
+    def __init__(self, rows: Sequence[int], start: Sequence[int], device):
+        if len(rows) != len(start) or any(n < 0 for n in rows):
+            raise ValueError("rows and start must hold one entry per sequence")
+        self.rows, self.start = [int(n) for n in rows], [int(n) for n in start]
+        at = [0]
+        for n in self.rows:
+            at.append(at[-1] + n)
+        self.n_rows = at[-1]
+        both = torch.tensor(at + self.start, dtype=torch.int32).to(device)
+        self.row_start, self.start_pos = both[:len(at)], both[len(at):]
+        self.struct = B.Chunk(self.row_start.data_ptr(), self.start_pos.data_ptr(), self.n_rows)
+
+
+def _on(device: torch.device):
+    """The device current for the calls inside (they launch on the current one)."""
+    return torch.cuda.device(device) if device.index is not None else contextlib.nullcontext()
 
 
 class RetroLayer:
@@ -68,6 +129,7 @@ class RetroLayer:
         self.sel = B.Selection(self.selected.data_ptr(), self.mask.data_ptr(),
                                self.num_selected.data_ptr())
         self.ocache = B.OutputCache(self.o_cache.data_ptr(), self.lse_cache.data_ptr())
+        self.chunk_ws: Optional[torch.Tensor] = None  # of attend_chunk
         self._lens = [0] * batch  # host mirror of seq_lens, for prefill positions
 
     @classmethod
@@ -166,3 +228,96 @@ class RetroLayer:
         for b in range(self.batch):
             self._lens[b] += 1
         self._keep = (q_window, k_new, v_new)
+
+    # -- chunks of prompts, rotated positions -----------------------------------------
+    def _rows(self, x, heads: int) -> torch.Tensor:
+        """x [rows][heads][d] or [rows][heads * d] as it is where the library can read it
+        (rows may be strided: parts of one projection's output), else copied."""
+        if not isinstance(x, torch.Tensor):
+            x = torch.from_numpy(x)
+        if x.shape[0] * heads * self.d != x.numel():
+            raise ValueError(f"expected [rows][{heads}][{self.d}], got {tuple(x.shape)}")
+        x = x.to(device=self.device, dtype=self.dtype)
+        inner = x[:1].is_contiguous() if x.shape[0] else True
+        piece = 16 // x.element_size()
+        if not inner or x.data_ptr() % 16 or (x.shape[0] > 1 and
+                                              (x.stride(0) % piece or
+                                               x.stride(0) < heads * self.d)):
+            x = x.contiguous()
+        return x
+
+    def _stride(self, x: torch.Tensor, heads: int) -> int:
+        return x.stride(0) if x.shape[0] > 1 else heads * self.d
+
+    def chunk(self, rows: Sequence[int]) -> RetroChunk:
+        """The next ``rows[b]`` tokens of every sequence b, behind what it holds."""
+        if len(rows) != self.batch:
+            raise ValueError("rows must hold one entry per sequence")
+        return RetroChunk(rows, self._lens, self.device)
+
+    def rotate(self, rotary: RetroRotary, positions: torch.Tensor, q=None, k=None,
+               stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+        """Queries [rows][h_q][d] and keys [rows][h_k][d] (either may be None) normalised
+        and rotated to ``positions`` [rows] (int32, on the device), as new tensors."""
+        rows = int(positions.numel())
+        positions = positions.to(device=self.device, dtype=torch.int32).contiguous()
+        q = None if q is None else self._rows(q, self.hq)
+        k = None if k is None else self._rows(k, self.hk)
+        if any(x is not None and x.shape[0] != rows for x in (q, k)):
+            raise ValueError("one position per row")
+        # (rows of negative position are not written: they come out as zeros)
+        qo, ko = (None if x is None else
+                  torch.zeros(rows, h, self.d, dtype=self.dtype, device=self.device)
+                  for x, h in ((q, self.hq), (k, self.hk)))
+        with _on(self.device):
+            B.retro_rotate_qk(self.dims, rotary.struct, positions, rows,
+                              q, 0 if q is None else self._stride(q, self.hq),
+                              k, 0 if k is None else self._stride(k, self.hk), qo, ko, stream)
+        self._keep_rot = (positions, q, k, rotary)
+        return qo, ko
+
+    def append_chunk(self, step: int, chunk: RetroChunk, rotary: RetroRotary, k, v, q=None,
+                     stream=None) -> Optional[torch.Tensor]:
+        """Store the chunk's keys and values [rows][h_k][d], keys normalised and rotated on
+        the way; returns the queries q [rows][h_q][d], treated likewise (None without q)."""
+        k, v = self._rows(k, self.hk), self._rows(v, self.hk)
+        q = None if q is None else self._rows(q, self.hq)
+        if any(x is not None and x.shape[0] != chunk.n_rows for x in (q, k, v)):
+            raise ValueError("one row of q, k and v per row of the chunk")
+        if chunk.start != self._lens:
+            raise ValueError("the chunk does not begin where the sequences end")
+        out = None if q is None else torch.empty(chunk.n_rows, self.hq, self.d, dtype=self.dtype,
+                                                 device=self.device)
+        with _on(self.device):
+            B.retro_append_kv_rotary(self.dims, step, self.cache, chunk.struct, rotary.struct,
+                                     q, 0 if q is None else self._stride(q, self.hq),
+                                     k, self._stride(k, self.hk), v, self._stride(v, self.hk),
+                                     out, stream)
+        for b in range(self.batch):
+            self._lens[b] += chunk.rows[b]
+        self._keep_chunk = (q, k, v, chunk, rotary)
+        return out
+
+    def attend_chunk(self, chunk: RetroChunk, q, lse: bool = False, stream=None
+                     ) -> Union[torch.Tensor, Tuple[torch.Tensor, torch.Tensor]]:
+        """Dense causal attention of the chunk's (rotated) queries [rows][h_q][d] over
+        everything stored: outputs [rows][h_q][d], with ``lse`` also the natural
+        log-normalisers [rows][h_q] fp32."""
+        q = self._rows(q, self.hq)
+        if q.shape[0] != chunk.n_rows:
+            raise ValueError("one row of q per row of the chunk")
+        out = torch.empty(chunk.n_rows, self.hq, self.d, dtype=self.dtype, device=self.device)
+        z = torch.empty(chunk.n_rows, self.hq, dtype=torch.float32,
+                        device=self.device) if lse else None
+        need = B.retro_chunk_workspace_size(self.dims, chunk.n_rows)
+        if self.chunk_ws is None or self.chunk_ws.numel() < need:
+            # for as many rows as the cache has tokens, so that a captured call's
+            # workspace is not replaced by a larger one
+            most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G)
+            need = max(need, B.retro_chunk_workspace_size(self.dims, most))
+            self.chunk_ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
+        with _on(self.device):
+            B.retro_chunk_attend(self.dims, self.cache, chunk.struct, q, self._stride(q, self.hq),
+                                 out, z, self.chunk_ws, self.chunk_ws.numel(), stream)
+        self._keep_attend = (q, chunk)
+        return (out, z) if lse else out
