@@ -85,7 +85,7 @@ __device__ __forceinline__ Seq make_seq(Run run, int end, int G) {
 }
 __device__ __forceinline__ Seq load_seq(const AttendCall& a, int P, int b) {
   Seq s = make_seq(b < a.batch ? chunk_run(a.ch, b) : Run{0, 0, 0}, 0, a.G);
-  const int len = b < a.batch && s.rows ? a.seq_lens[b] : 0;
+  const int len = b < a.batch ? a.seq_lens[b] : 0;
   s.end = (int)min((int64_t)min(max(len, 0), s.run.pos + s.run.n), (int64_t)a.max_pages * P);
   return s;
 }
@@ -119,6 +119,12 @@ __device__ __forceinline__ int64_t wave_scan_i64(int64_t x) {
   x += dpp_i64<0x143, 0xC, false>(x);
   return x;
 }
+__device__ __forceinline__ int64_t read_lane(int64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(x >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t last_lane(int64_t x) { return read_lane(x, 63); }
 // Prefix sums of N values over the workgroup's threads, and their totals.
 template <int N>
 struct Scan {
@@ -146,6 +152,8 @@ __device__ __forceinline__ void block_scan(Scan<N>& s, int64_t (&scratch)[kScans
   __syncthreads();
 }
 
+// Up to 64 sequences every wavefront does by itself, a lane for each: no barrier, and
+// little code (a workgroup that runs once waits for much of it to be fetched).
 struct FindLds {
   int64_t scratch[kScans][kWaves];
   int64_t local, before;
@@ -169,9 +177,10 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
   enum { kLine, kSmall, kMany, kTiles };
   Scan<4> x;
   for (int j = 0; j < 4; ++j) x.of[j] = 0;
-  for (int b = tid; b < a.batch; b += kThreads) {
+  const bool wavefront = a.batch <= 64;
+  for (int b = wavefront ? tid & 63 : tid; b < a.batch; b += kThreads) {
     const Seq s = load_seq(a, P, b);
-    if (b < kThreads) L.first[b] = int4{s.run.row, s.run.n, s.run.pos, s.end};
+    if (b < kThreads) L.first[b] = int4{s.run.row, s.run.n, s.run.pos, s.end};  // (the same from every wavefront)
     const int64_t line = a.hk * s.place(s.tiles(kRowsFew), a.G);
     if (F32 || s.few) {
       x.of[kLine] += line;
@@ -182,7 +191,13 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
       x.of[kTiles] += tiles;
     }
   }
-  block_scan(x, L.scratch, tid);
+  if (wavefront) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.total[j] = last_lane(wave_scan_i64(x.of[j]));
+    __syncthreads();
+  } else {
+    block_scan(x, L.scratch, tid);
+  }
   const int64_t n = gridDim.x, many = x.total[kMany], tiles = x.total[kTiles];
   Cut c;
   c.all_line = F32 || (many < 5 * n && 8 * tiles < n && many > 16 * tiles);
@@ -199,6 +214,20 @@ template <typename Count, typename Other>
 __device__ __forceinline__ bool find_seq(const AttendCall& a, int P, int64_t u, FindLds& L, int tid,
                                          Count&& count, Other&& other, Seq& seq, int& b, int64_t& local,
                                          int64_t& before) {
+  if (a.batch <= 64) {
+    const int lane = tid & 63;
+    const Seq s = first_seq(L, min(lane, a.batch - 1), a.G);
+    const int64_t n = lane < a.batch ? count(s) : 0, f = lane < a.batch ? other(s) : 0;
+    const int64_t upto = wave_scan_i64(n);
+    const uint64_t past = wave_ballot(upto > u);
+    if (!past) return false;
+    b = __builtin_ctzll(past);
+    local = u - (read_lane(upto, b) - read_lane(n, b));
+    before = read_lane(wave_scan_i64(f) - f, b);
+    auto of_b = [&](int v) { return __builtin_amdgcn_readlane(v, b); };
+    seq = make_seq(Run{of_b(s.run.row), of_b(s.run.n), of_b(s.run.pos)}, of_b(s.end), a.G);
+    return true;
+  }
   int64_t base = 0, obase = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
     const Seq s = b0 ? load_seq(a, P, b0 + tid)
@@ -261,10 +290,13 @@ struct Shape {
   static __device__ __forceinline__ int fv(int d) { return d / (16 / CPV) % CPV; }
 };
 
-// Joining parts.  32 rows: what several groups of lanes have of a row's parts.
+// Joining parts.  32 rows: weights of some parts, what rows have so far, and several
+// groups of lanes' sums.
+constexpr int kJoinFew = 64;
 struct JoinLds {
   f32x4 o[kThreads];
-  float m[kThreads], l[kThreads];
+  float w[kJoinFew][kRowsFew];
+  float m[kRowsFew], sum[kRowsFew], keep[kRowsFew];
 };
 // Many rows: some parts' maxima, later their weights, and sums; what the rows have so far.
 constexpr int kJoinParts = 16;
@@ -525,19 +557,28 @@ struct Rows {
 
   // O^T += V^T P^T of one tile.  Masked: values of slots that hold no token of the
   // sequence (stored: tokens of it from this tile's first key on) are taken as zero.
-  template <bool MASK>
+  // SPLIT: a bf16 weight is given as two, what the first one's rounding leaves and it.
+  template <bool MASK, bool SPLIT>
   __device__ __forceinline__ void values(int at, const f32x16& p, int stored, uint32_t bad) {
     constexpr int STEPS = 32 / (2 * S::E);  // key pieces of a lane half
 #pragma unroll
     for (int t = 0; t < STEPS; ++t) {
       const int piece = 2 * t;  // (+ half) of the tile; pieces of a page: CPV
       const int more = at + piece / S::CPV * (int)(D * P * sizeof(T));
-      [[maybe_unused]] bf16x8 w;
+      [[maybe_unused]] bf16x8 w, rest;
       if constexpr (sizeof(T) == 2) {
         u32x4 x;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = pack_bf16(p[8 * t + 2 * e], p[8 * t + 2 * e + 1]);
         w = __builtin_bit_cast(bf16x8, x);
+        if constexpr (SPLIT) {
+          u32x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            y[e] = pack_bf16(p[8 * t + 2 * e] - __uint_as_float(x[e] << 16),
+                             p[8 * t + 2 * e + 1] - __uint_as_float(x[e] & 0xffff0000u));
+          rest = __builtin_bit_cast(bf16x8, y);
+        }
       }
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
@@ -557,6 +598,9 @@ struct Rows {
         if constexpr (sizeof(T) == 2) {
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w, acc[i], 0,
                                                            0, 0);
+          if constexpr (SPLIT)
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), rest, acc[i],
+                                                             0, 0, 0);
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -607,77 +651,121 @@ __device__ __forceinline__ bool last_part(int32_t* counter, int parts, int* flag
   return *flag != 0;
 }
 
-// Joins the parts of R of a tile's 32 rows: slot(p) is part p's result.  D / 4 lanes
-// take a row; where there are fewer rows than lanes for it, several groups of
-// lanes share a row's parts.  done(row, l, m, d, o): four elements from d on.
+// Joins the parts of R of a tile's 32 rows: slot(p) is part p's result.  16 lanes a
+// row take the maxima and sums of 64 parts; then all threads the outputs, 16 bytes
+// each, where there are fewer rows than threads for it several groups of them a
+// share of the parts each.  done(row, m, l, d, o): four elements from d on.
 template <int D, typename Slot, typename Done>
-__device__ __forceinline__ void join_few(JoinLds& L, int R, int parts, float c, int tid,
-                                           Slot&& slot, Done&& done) {
-  constexpr int LPR = D / 4, SUB = kThreads / LPR, AHEAD = 8;
-  const int sub = tid / LPR, d = tid % LPR * 4;
-  const int groups = max(SUB / R, 1), per = SUB / groups;  // rows at a time
-  for (int r0 = 0; r0 < R; r0 += per) {
-    const int row = r0 + sub % per, grp = sub / per;
-    const bool on = row < R && sub < per * groups;
-    float m = -INFINITY, l = 0.f;
-    f32x4 o{0.f, 0.f, 0.f, 0.f};
-    if (on)
-      for (int p0 = grp; p0 < parts; p0 += AHEAD * groups) {
-        f32x4 x[AHEAD];
-        float pm[AHEAD], pl[AHEAD];
+__device__ __forceinline__ void join_few(JoinLds& L, int R, int parts, float c, int tid, Slot&& slot,
+                                         Done&& done) {
+  constexpr int LPR = D / 4, PER = kThreads / LPR;       // rows at a time
+  constexpr int ITEMS = kRowsFew / PER;                  // rows of a thread: row0 + i * PER
+  const int d = tid % LPR * 4, sub = tid / LPR;
+  int shift = 0;                                         // 2^shift groups share the parts
+  while ((R << (shift + 1)) <= PER) ++shift;
+  const int groups = 1 << shift, grp = sub & (groups - 1), row0 = sub >> shift;
+  f32x4 o[ITEMS];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-          const int p = p0 + i * groups;
-          const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(min(p, parts - 1)));
-          x[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (row * D + d) * 4, 0, kCpolSc1));
-          pm[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (kRowsFew * D + row) * 4, 0, kCpolSc1));
-          pl[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (kRowsFew * (D + 1) + row) * 4, 0, kCpolSc1));
-          if (p >= parts) pm[i] = -INFINITY;
-        }
-        float mn = m;
+  for (int i = 0; i < ITEMS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (tid < kRowsFew) {
+    L.m[tid] = -INFINITY;
+    L.sum[tid] = 0.f;
+  }
+  __syncthreads();
+  for (int q0 = 0; q0 < parts; q0 += kJoinFew) {
+    const int np = min(parts - q0, kJoinFew);
+    {
+      const int row = tid / 16, j = tid % 16;  // kThreads / 16 == kRowsFew
+      float pm[kJoinFew / 16], pl[kJoinFew / 16];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) mn = fmaxf(mn, pm[i]);
-        const float mu = mn == -INFINITY ? 0.f : mn;
-        const float keep = __builtin_amdgcn_exp2f((m - mu) * c);
-        l *= keep;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] *= keep;
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-          if (p0 + i * groups >= parts) continue;
-          const float e = __builtin_amdgcn_exp2f((pm[i] - mu) * c);
-          l = __builtin_fmaf(e, pl[i], l);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[i][j], o[j]);
-        }
-        m = mn;
+      for (int i = 0; i < kJoinFew / 16; ++i) {
+        const int p = j + 16 * i;
+        const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(q0));
+        // (a part's place behind the first one's, in bytes)
+        const int at = (int)((const char*)slot(q0 + min(p, np - 1)) - (const char*)slot(q0));
+        pm[i] = __uint_as_float(
+            __builtin_amdgcn_raw_buffer_load_b32(r, at + (kRowsFew * D + row) * 4, 0, kCpolSc1));
+        pl[i] = __uint_as_float(
+            __builtin_amdgcn_raw_buffer_load_b32(r, at + (kRowsFew * (D + 1) + row) * 4, 0, kCpolSc1));
+        if (p >= np || row >= R) pm[i] = -INFINITY;
       }
-    if (groups > 1) {
-      L.o[tid] = o;
-      L.m[tid] = m;
-      L.l[tid] = l;
-      __syncthreads();
-      if (on && grp == 0) {
-        float mn = m;
-        for (int g = 1; g < groups; ++g) mn = fmaxf(mn, L.m[tid + g * per * LPR]);
-        const float mu = mn == -INFINITY ? 0.f : mn;
-        l = 0.f;
-        o = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int g = 0; g < groups; ++g) {
-          const int t = tid + g * per * LPR;
-          const float e = __builtin_amdgcn_exp2f((L.m[t] - mu) * c);
-          l = __builtin_fmaf(e, L.l[t], l);
+      float m = L.m[row];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, L.o[t][j], o[j]);
+      for (int i = 0; i < kJoinFew / 16; ++i) m = fmaxf(m, pm[i]);
+      m = fmaxf(m, dpp_f<kDppXor1>(m));
+      m = fmaxf(m, dpp_f<kDppXor2>(m));
+      m = fmaxf(m, dpp_f<kDppHalfMirror>(m));
+      m = fmaxf(m, dpp_f<kDppMirror>(m));
+      const float mu = m == -INFINITY ? 0.f : m, keep = __builtin_amdgcn_exp2f((L.m[row] - mu) * c);
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kJoinFew / 16; ++i) {
+        const int p = j + 16 * i;
+        const float w = __builtin_amdgcn_exp2f((pm[i] - mu) * c);
+        if (p < np) {
+          sum = __builtin_fmaf(w, row < R ? pl[i] : 0.f, sum);
+          L.w[p][row] = w;
         }
-        m = mn;
+      }
+      sum += dpp_f<kDppXor1>(sum);
+      sum += dpp_f<kDppXor2>(sum);
+      sum += dpp_f<kDppHalfMirror>(sum);
+      sum += dpp_f<kDppMirror>(sum);
+      if (j == 0) {
+        L.sum[row] = __builtin_fmaf(L.sum[row], keep, sum);
+        L.m[row] = m;
+        L.keep[row] = keep;
       }
     }
-    if (on && grp == 0) done(row, m, l, d, o);
+    __syncthreads();
+    constexpr int AHEAD = 8;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] *= L.keep[min(row0 + i * PER, R - 1)];
+    for (int p0 = grp; p0 < np; p0 += AHEAD * groups) {
+      f32x4 x[AHEAD][ITEMS];
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(q0));
+        const int at = (int)((const char*)slot(q0 + min(p0 + j * groups, np - 1)) - (const char*)slot(q0));
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+          x[j][i] = __builtin_bit_cast(
+              f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                         r, at + (min(row0 + i * PER, R - 1) * D + d) * 4, 0, kCpolSc1));
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        if (p0 + j * groups >= np) continue;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          const float w = L.w[p0 + j * groups][min(row0 + i * PER, R - 1)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][e] = __builtin_fmaf(w, x[j][i][e], o[i][e]);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  if (groups > 1) {  // (then R <= PER, and a thread has one row)
+    L.o[tid] = o[0];
+    __syncthreads();
+    if (grp == 0)
+      for (int g = 1; g < groups; ++g) {
+        const f32x4 y = L.o[tid + g * LPR];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[0][e] += y[e];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    const int row = row0 + i * PER;
+    if (grp == 0 && row < R) done(row, L.m[row], L.sum[row], d, o[i]);
   }
 }
 
-  // a sequence's pages: page i's number if it is mapped, else page 0 (never counted)
+// a sequence's pages: page i's number if it is mapped, else page 0 (never counted)
   struct Pages {
     const int32_t* table;
     int last, num_phys;
@@ -893,7 +981,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
             rows.weights(sc, rows.follow(sc));
             if (next < key_end) wait_loads<S::LOADS>();
             else wait_loads<0>();
-            rows.template values<true>(0, sc[0], s.end - key, bad);
+            // (and neither does the weights' second half: 0.0022 -> 0.0017 off 64 bits)
+            rows.template values<true, true>(0, sc[0], s.end - key, bad);
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
             if (next < key_end) issue(vh, vs, next, vcopy, vxor);
             bad = bad_next;
@@ -1105,7 +1194,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
             rows.weights(sa, rows.follow(sa));
 #pragma unroll
             for (int i = 0; i < S::NB; ++i)
-              rows.template values<true>(i * S::TILE, sa[i], s.end - key - 32 * i, bad >> (i * 32 / P));
+              rows.template values<true, false>(i * S::TILE, sa[i], s.end - key - 32 * i, bad >> (i * 32 / P));
           }
           if (key + S::KEYS <= lim1)
 #pragma unroll

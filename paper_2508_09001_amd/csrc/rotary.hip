@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   // a page's workgroups are neighbours: they read and write neighbouring memory
   const int kinds = q ? 2 * g.hk : g.hk, kind = blockIdx.x % kinds;
   const int b = find_page(ch, g.batch, PS, lane, blockIdx.x / kinds, run, page);
-  if (b < 0) return;
+  if (b < 0 || page < 0 || page >= run_pages(run, PS)) return;
   const int lp0 = run.pos / PS, lp = lp0 + page;
   // slots of this page that the run fills, and the row of slot 0
   const int s0 = page ? 0 : run.pos - lp * PS;

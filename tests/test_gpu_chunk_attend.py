@@ -184,6 +184,33 @@ def test_many_sequences(dtype):
     Batch(dtype, 2, 2, 64, 16, seqs, seed=6).run().check()
 
 
+def test_more_sequences_than_threads():
+    rng = np.random.default_rng(15)
+    seqs = [(int(rng.integers(0, 3)), int(rng.integers(0, 40))) for _ in range(1100)]
+    seqs[700], seqs[1050] = (90, 200), (1, 3000)
+    Batch("bf16", 1, 4, 64, 16, seqs, seed=16).run().check()
+
+
+def test_one_workspace_for_calls_of_other_dims():
+    batches = [Batch("bf16", 2, 4, 128, 16, [(1, 3000), (40, 700)], seed=17), Batch("f32", 3, 1, 64, 32, [(100, 900)], seed=18),
+               Batch("bf16", 8, 4, 64, 16, [(400, 2000)], seed=19)]
+    ws = torch.zeros(max(b.ws_bytes for b in batches), dtype=torch.uint8, device="cuda")
+    for b in batches * 3:
+        b.ws, b.ws_bytes = ws, ws.numel()
+        b.out.fill_(5.0)
+        b.lse.fill_(5.0)
+        b.run().check()
+
+
+def test_results_in_place_of_the_queries():
+    b = Batch("bf16", 8, 4, 128, 16, [(300, 2000), (1, 700)], seed=20).run()
+    q = b.q.contiguous().clone()
+    b.B.retro_chunk_attend(b.dims, b.cache, b.chunk, q, q.stride(0), q, None, b.ws, b.ws_bytes)
+    rows = slice(b.front, b.front + b.rows)
+    assert torch.equal(q.view_as(b.out)[rows], b.out[rows])
+    assert torch.equal(q[: b.front], b.q[: b.front])
+
+
 @pytest.mark.parametrize("hk,seqs", [(2, [(1, 3000), (100, 700)]), (8, [(1, 3000), (400, 2000)])])
 def test_no_lse_and_same_results_again(hk, seqs):
     b = Batch("bf16", hk, 4, 128, 16, seqs, seed=7).run()
