@@ -172,7 +172,7 @@ __device__ __forceinline__ Seq first_seq(const FindLds& L, int b, int G) {
 // tokens 34 and 47, 128 at 4000 49 and 57; but 256 at 2000 53 and 50, 512 at 4000 136
 // and 69, 128 rows of a new prompt 33 and 21.  fp32 tiles always are of 32 rows: its
 // matrix instructions are 16 times slower, and the reading does not show.
-template <bool F32>
+template <bool MANY>
 __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, int tid) {
   enum { kLine, kSmall, kMany, kTiles };
   Scan<4> x;
@@ -182,7 +182,7 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
     const Seq s = load_seq(a, P, b);
     if (b < kThreads) L.first[b] = int4{s.run.row, s.run.n, s.run.pos, s.end};  // (the same from every wavefront)
     const int64_t line = a.hk * s.place(s.tiles(kRowsFew), a.G);
-    if (F32 || s.few) {
+    if (!MANY || s.few) {
       x.of[kLine] += line;
     } else {
       const int64_t tiles = (int64_t)a.hk * s.tiles(kRowsMany);
@@ -200,7 +200,7 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
   }
   const int64_t n = gridDim.x, many = x.total[kMany], tiles = x.total[kTiles];
   Cut c;
-  c.all_line = F32 || (many < 5 * n && 8 * tiles < n && many > 16 * tiles);
+  c.all_line = !MANY || (many < 5 * n && 8 * tiles < n && many > 16 * tiles);
   c.line = x.total[kLine] + (c.all_line ? x.total[kSmall] : 0);
   c.many = c.all_line ? 0 : many;
   c.share = max((c.line + n - 1) / n, (int64_t)kMinFew);
@@ -672,8 +672,23 @@ __device__ __forceinline__ void join_few(JoinLds& L, int R, int parts, float c, 
     L.sum[tid] = 0.f;
   }
   __syncthreads();
+  constexpr int AHEAD = 8;
+  f32x4 x[AHEAD][ITEMS];
+  auto load = [&](int q0, int np, int p0) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(q0));
+      const int at = (int)((const char*)slot(q0 + min(p0 + j * groups, np - 1)) - (const char*)slot(q0));
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i)
+        x[j][i] = __builtin_bit_cast(
+            f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                       r, at + (min(row0 + i * PER, R - 1) * D + d) * 4, 0, kCpolSc1));
+    }
+  };
   for (int q0 = 0; q0 < parts; q0 += kJoinFew) {
     const int np = min(parts - q0, kJoinFew);
+    load(q0, np, grp);  // on the way while the weights are made
     {
       const int row = tid / 16, j = tid % 16;  // kThreads / 16 == kRowsFew
       float pm[kJoinFew / 16], pl[kJoinFew / 16];
@@ -718,23 +733,12 @@ __device__ __forceinline__ void join_few(JoinLds& L, int R, int parts, float c, 
       }
     }
     __syncthreads();
-    constexpr int AHEAD = 8;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] *= L.keep[min(row0 + i * PER, R - 1)];
     for (int p0 = grp; p0 < np; p0 += AHEAD * groups) {
-      f32x4 x[AHEAD][ITEMS];
-#pragma unroll
-      for (int j = 0; j < AHEAD; ++j) {
-        const __amdgpu_buffer_rsrc_t r = coherent_rsrc(slot(q0));
-        const int at = (int)((const char*)slot(q0 + min(p0 + j * groups, np - 1)) - (const char*)slot(q0));
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-          x[j][i] = __builtin_bit_cast(
-              f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                         r, at + (min(row0 + i * PER, R - 1) * D + d) * 4, 0, kCpolSc1));
-      }
+      if (p0 != grp) load(q0, np, p0);
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j) {
         if (p0 + j * groups >= np) continue;
@@ -860,7 +864,9 @@ __device__ __forceinline__ void join_many(JoinManyLds& L, int R, int parts, floa
 
 // ---- kernel ------------------------------------------------------------------------------
 
-template <typename T, int D, int P>
+// MANY: with tiles of many rows.  Without them the same line of tiles of 32 rows is
+// walked in less code and registers (one token at 32K: 38.8 -> 32.6 us).
+template <typename T, int D, int P, bool MANY>
 __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   using S = Shape<T, D, P>;
   using R_t = Rows<T, D, P>;
@@ -869,7 +875,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   const int tid = thread_index();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t st = lds_address(&L.u);
-  const Cut cut = make_cut<sizeof(T) == 4>(a, P, L.find, tid);
+  const Cut cut = make_cut<MANY>(a, P, L.find, tid);
   const int64_t page_bytes = (int64_t)P * D * sizeof(T), phys_bytes = page_bytes * a.hk;
   // a lane's place within a copy of keys, and of values: pieces in their LDS order
   uint32_t kcopy, vcopy;
@@ -1057,7 +1063,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   };
 
   // ---- many rows
-  auto many_rows = [&]() {
+  [[maybe_unused]] auto many_rows = [&]() {
     constexpr int PS = S::KEYS / P;  // pages of a stage
     const int most = (int)cut.part;
     auto parts_of = [&](int steps) { return (steps + most - 1) / most; };
@@ -1237,15 +1243,18 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
 
   // Reading the cache for few rows leaves the matrix cores idle and the other way
   // round: every other workgroup of an XCD begins with the one, the rest with the other.
-  const bool turn = blockIdx.x >> 3 & 1;
+  [[maybe_unused]] const bool turn = blockIdx.x >> 3 & 1;
+  if constexpr (MANY) {
 #pragma unroll 1
-  for (int i = 0; i < 2; ++i) {
-    if ((i == 0) != turn) {
-      if constexpr (sizeof(T) == 2)
+    for (int i = 0; i < 2; ++i) {
+      if ((i == 0) != turn) {
         if (cut.many) many_rows();
-    } else {
-      if (cut.line) few_rows();
+      } else {
+        if (cut.line) few_rows();
+      }
     }
+  } else {
+    if (cut.line) few_rows();
   }
 }
 
@@ -1305,8 +1314,20 @@ hipError_t launch_chunk_attend(const Geometry& g, const retro_kv_cache& c, const
                      g.max_pages,
                      g.num_phys,
                      g.sm_scale};
+  // The host does not know the lengths.  Where every sequence has a row, one can have
+  // no more than this many: few enough for tiles of 32 rows only.  (Where most have none
+  // after all, a long chunk of a few rows more than that takes longer, no worse.)
+  const bool many = g.dtype == RETRO_BF16 && ((int64_t)ch.n_rows - g.batch + 1) * g.G > 4 * kRowsFew;
   auto go = [&](auto t, auto d, auto ps) {
-    chunk_attend_kernel<decltype(t), decltype(d)::value, decltype(ps)::value><<<kCus, kThreads, 0, s>>>(a);
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value, P = decltype(ps)::value;
+    if constexpr (sizeof(T) == 2) {
+      if (many) {
+        chunk_attend_kernel<T, D, P, true><<<kCus, kThreads, 0, s>>>(a);
+        return hipGetLastError();
+      }
+    }
+    chunk_attend_kernel<T, D, P, false><<<kCus, kThreads, 0, s>>>(a);
     return hipGetLastError();
   };
   auto with_page = [&](auto t, auto d) {
