@@ -22,6 +22,14 @@
 // workspace, written and read past the L2s of the XCDs, and the workgroup that
 // finishes the last one joins them.
 //
+// Measured (bf16, 8 KV heads of 4 query heads of 128): a prompt of 8192 tokens 483 to
+// 505 us (1.09 to 1.14 PFLOP/s), 1024 rows at 131K 1.82 to 1.87 ms (1.17 to 1.20), where a
+// product of 16384^3 reaches 1.37: the matrix units are busy 64 % of the cycles at 1.75
+// GHz, which is where such products hold the clock too, and leaving out any one part
+// of the loop (exponentials, LDS reads, copies, maxima, sums) gains 4 to 9 %.  16 tokens
+// at 8K to 32K, 1.15 GB: 187 us, 6.15 TB/s, the rate of a plain read.  Short calls wait for
+// one memory round trip after the other: 12 us for a token at 100.
+//
 // Pages lie in LDS as in memory, cut into 16-byte pieces whose order within a
 // row is xored with the row's number, so that the 16 lanes of a read fall into 16
 // different groups of banks; the copy engine writes LDS in order and reads
