@@ -443,7 +443,7 @@ retro_status retro_project_f32(const float* x, int32_t rows, int32_t k, const fl
  * a ragged batch of rows with both applied on the way, and the attention of these
  * rows over everything stored.  Of retro_dims these calls use batch,
  * num_kv_heads, group, head_dim, page_size, max_pages, num_phys_pages, dtype and
- * sm_scale.  Rows are tokens: queries [rows][h_q][d], keys and values
+ * sm_scale (the others have to be valid).  Rows are tokens: queries [rows][h_q][d], keys and values
  * [rows][h_k][d] in dtype, where `*_stride` elements lie between the rows of an
  * input (parts of one projection's output: its row length; else heads * d).
  * Outputs are contiguous.  Every pointer is a device address, 16-byte aligned
@@ -531,12 +531,14 @@ retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, 
  * first (retro_append_kv_rotary, retro_prefill_kv, retro_append_kv_tokens); one row per
  * sequence is dense decoding.  Tokens of pages that are not mapped are left out.
  * Products and sums in fp32; for bf16 the softmax weights are rounded to bf16 for
- * their product with the values (sums and log-normalisers take the unrounded ones).
+ * their product with the values, where a sequence has few rows as two bf16 halves
+ * (sums and log-normalisers take the unrounded ones).
  * NaN and infinities as in retro_decode_attend: a NaN score, or one of +inf,
- * makes its row NaN; a NaN or infinite value of a stored token can reach every
- * row of its sequence and KV head in the same call; slots past seq_lens never count, whatever
- * they hold.  Reads the cache only.  n_rows == 0 does nothing; more than 65535
- * sequences, or n_rows * h_q * d >= 2^40, is RETRO_EUNSUPPORTED. */
+ * makes its row NaN; a NaN or infinite value of a stored token can make every
+ * row of its sequence and KV head in the same call NaN, also rows in front of it;
+ * slots past seq_lens never count, whatever they hold.  Reads the cache only.
+ * n_rows == 0 does nothing; n_rows * h_q * d >= 2^40 or n_rows * G >= 2^31 is
+ * RETRO_EUNSUPPORTED. */
 retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* cache,
                                 const retro_chunk* chunk, const void* q, int64_t q_stride,
                                 void* out, float* lse, void* workspace, size_t ws_bytes,

@@ -13,8 +13,8 @@
 //     other way): the wavefronts take 32 keys in turn, each through LDS of its own,
 //     without barriers, and join their (maximum, sum, output) at the end; bound by
 //     reading the cache;
-//   - many rows: 32 of 256 rows each, all over the same 64 keys (fp32: 32), which
-//     are copied into LDS for all, one stage ahead; bound by the matrix cores.
+//   - many rows (bf16): 32 of 256 rows each, all over the same 64 keys, which are
+//     copied into LDS for all, one stage ahead; bound by the matrix cores.
 // The work is laid out on the device, from the arrays of the call, by every
 // workgroup for itself: the steps of all tiles of 32 rows are one line, cut into
 // equal shares wherever that falls; tiles of many rows are cut along the keys
@@ -22,9 +22,9 @@
 // workspace, written and read past the L2s of the XCDs, and the workgroup that
 // finishes the last one joins them.
 //
-// Measured (bf16, 8 KV heads of 4 query heads of 128): a prompt of 8192 tokens 483 to
-// 505 us (1.09 to 1.14 PFLOP/s), 1024 rows at 131K 1.82 to 1.87 ms (1.17 to 1.20), where a
-// product of 16384^3 reaches 1.37: the matrix units are busy 64 % of the cycles at 1.75
+// Measured (bf16, 8 KV heads of 4 query heads of 128; several cards): a prompt of 8192
+// tokens 483 to 546 us (1.01 to 1.14 PFLOP/s), 1024 rows at 131K 1.82 to 2.03 ms (1.08 to
+// 1.20), where a product of 16384^3 reaches 1.37: the matrix units are busy 64 % of the cycles at 1.75
 // GHz, which is where such products hold the clock too, and leaving out any one part
 // of the loop (exponentials, LDS reads, copies, maxima, sums) gains 4 to 9 %.  16 tokens
 // at 8K to 32K, 1.15 GB: 187 us, 6.15 TB/s, the rate of a plain read.  Short calls wait for
@@ -285,7 +285,7 @@ struct Shape {
   static constexpr int CPR = D / E;              // pieces of a key row
   static constexpr int CPV = P / E;              // pieces of a value row (one element of d of a page)
   static constexpr int TILE = KB * D * sizeof(T);  // bytes of a tile's keys (and of its values)
-  static constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;  // keys of a shared stage
+  static constexpr int KEYS = 64;                // keys of a shared stage
   static constexpr int NB = KEYS / KB;
   static constexpr int STAGE = 2 * NB * TILE;    // bytes of a stage: keys, then values
   static constexpr int LOADS = TILE / 1024;      // wavefront copies of a tile's keys (or values)
@@ -505,11 +505,12 @@ struct Rows {
   // read four pieces ahead.  (sched_barrier: the compiler keeps this order.)
   template <int NB>
   __device__ __forceinline__ void weave(f32x16 (&s)[NB], f32x16 (&next)[NB], float mc) {
+    static_assert(sizeof(T) == 2, "tiles of many rows are bf16");
     constexpr int SE = 16 / (32 / (2 * S::E));   // scores of a lane that a step of values takes
     constexpr int NS = NB * S::QC, STEPS = NB * 16 / SE, TOTAL = NS + STEPS * DT;
     constexpr int AHEAD = 4, EL = NB * 16, SPAN = TOTAL - DT;
     u32x4 buf[AHEAD + 1];
-    [[maybe_unused]] bf16x8 w;
+    bf16x8 w;
     auto fetch = [&](int i) {
       if (i < NS) return lds_piece<T>(koff[i / NB] + i % NB * S::TILE);
       const int st = (i - NS) / DT, dt = (i - NS) % DT;          // step, 32 elements of d
@@ -529,32 +530,18 @@ struct Rows {
         if (i < NB)
 #pragma unroll
           for (int e = 0; e < 16; ++e) n[e] = 0.f;
-        if constexpr (sizeof(T) == 2) {
-          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
-                                                      __builtin_bit_cast(bf16x8, q[i / NB]), n, 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            n = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(q[i / NB][e]),
-                                                     n, 0, 0, 0);
-        }
+        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                    __builtin_bit_cast(bf16x8, q[i / NB]), n, 0, 0, 0);
       } else {
         const int st = (i - NS) / DT, dt = (i - NS) % DT, e0 = st * SE;
-        if constexpr (sizeof(T) == 2) {
-          if (dt == 0) {
-            u32x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              y[e] = pack_bf16(s[e0 / 16][e0 % 16 + 2 * e], s[e0 / 16][e0 % 16 + 2 * e + 1]);
-            w = __builtin_bit_cast(bf16x8, y);
-          }
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), w, acc[dt], 0, 0, 0);
-        } else {
+        if (dt == 0) {
+          u32x4 y;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), s[e0 / 16][e0 % 16 + e],
-                                                           acc[dt], 0, 0, 0);
+            y[e] = pack_bf16(s[e0 / 16][e0 % 16 + 2 * e], s[e0 / 16][e0 % 16 + 2 * e + 1]);
+          w = __builtin_bit_cast(bf16x8, y);
         }
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), w, acc[dt], 0, 0, 0);
       }
 #pragma unroll
       for (int e = min(i * EL / SPAN, EL); e < min((i + 1) * EL / SPAN, EL); ++e)
@@ -563,10 +550,10 @@ struct Rows {
     }
   }
 
-  // O^T += V^T P^T of one tile.  Masked: values of slots that hold no token of the
-  // sequence (stored: tokens of it from this tile's first key on) are taken as zero.
+  // O^T += V^T P^T of one tile.  Values of slots that hold no token of the sequence
+  // (stored: tokens of it from this tile's first key on) are taken as zero.
   // SPLIT: a bf16 weight is given as two, what the first one's rounding leaves and it.
-  template <bool MASK, bool SPLIT>
+  template <bool SPLIT>
   __device__ __forceinline__ void values(int at, const f32x16& p, int stored, uint32_t bad) {
     constexpr int STEPS = 32 / (2 * S::E);  // key pieces of a lane half
 #pragma unroll
@@ -591,17 +578,15 @@ struct Rows {
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
         u32x4 v = lds_piece<T>(voff[piece % S::CPV / 2] + (more + i * (int)(32 * P * sizeof(T))));
-        if constexpr (MASK) {
-          const int k = S::E * (piece + half);
-          const int n = bad >> (k / P) & 1 ? 0 : stored - k;  // elements that count
-          if constexpr (sizeof(T) == 2) {
+        const int k = S::E * (piece + half);
+        const int n = bad >> (k / P) & 1 ? 0 : stored - k;  // elements that count
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              v[e] &= (n > 2 * e ? 0xffffu : 0u) | (n > 2 * e + 1 ? 0xffff0000u : 0u);
-          } else {
+          for (int e = 0; e < 4; ++e)
+            v[e] &= (n > 2 * e ? 0xffffu : 0u) | (n > 2 * e + 1 ? 0xffff0000u : 0u);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = n > e ? v[e] : 0u;
-          }
+          for (int e = 0; e < 4; ++e) v[e] = n > e ? v[e] : 0u;
         }
         if constexpr (sizeof(T) == 2) {
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w, acc[i], 0,
@@ -996,7 +981,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
             if (next < key_end) wait_loads<S::LOADS>();
             else wait_loads<0>();
             // (and neither does the weights' second half: 0.0022 -> 0.0017 off 64 bits)
-            rows.template values<true, true>(0, sc[0], s.end - key, bad);
+            rows.template values<true>(0, sc[0], s.end - key, bad);
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
             if (next < key_end) issue(vh, vs, next, vcopy, vxor);
             bad = bad_next;
@@ -1071,7 +1056,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   };
 
   // ---- many rows
-  [[maybe_unused]] auto many_rows = [&]() {
+  [[maybe_unused]] auto many_rows = [&](auto) {  // (generic: compiled where it is called)
     constexpr int PS = S::KEYS / P;  // pages of a stage
     const int most = (int)cut.part;
     auto parts_of = [&](int steps) { return (steps + most - 1) / most; };
@@ -1208,7 +1193,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
             rows.weights(sa, rows.follow(sa));
 #pragma unroll
             for (int i = 0; i < S::NB; ++i)
-              rows.template values<true, false>(i * S::TILE, sa[i], s.end - key - 32 * i, bad >> (i * 32 / P));
+              rows.template values<false>(i * S::TILE, sa[i], s.end - key - 32 * i, bad >> (i * 32 / P));
           }
           if (key + S::KEYS <= lim1)
 #pragma unroll
@@ -1256,7 +1241,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       if ((i == 0) != turn) {
-        if (cut.many) many_rows();
+        if (cut.many) many_rows(0);
       } else {
         if (cut.line) few_rows();
       }

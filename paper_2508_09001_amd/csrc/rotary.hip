@@ -6,7 +6,7 @@
 // (interleaved) or in two lanes rot_dim / 2 elements apart, which exchange their
 // pieces as read (four words instead of eight products).  Norm, rotation and
 // everything between stay in fp32 and are rounded once.  Bound by HBM: every
-// vector is read once and written once, at 4.3 to 4.7 TB/s where a plain copy
+// vector is read once and written once, at 4.6 to 4.7 TB/s where a plain copy
 // reaches 4.8; by the launch for a few rows.
 #include "roles.h"
 #include "rotary.h"
@@ -272,10 +272,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   int page;
   // a page's workgroups are neighbours on one XCD: they read and write neighbouring
   // memory, and the same angles (21828 rows, 554 MB: 142 us as a row of all pages for
-  // each head, 129 as neighbours on all XCDs, 125 on one)
-  const int unit = xcd_remap(blockIdx.x, gridDim.x);
-  const int kinds = q ? 2 * g.hk : g.hk, kind = unit % kinds;
-  const int b = find_page(ch, g.batch, PS, lane, unit / kinds, run, page);
+  // each head, 129 as neighbours on all XCDs, 119 on one)
+  const int kinds = q ? 2 * g.hk : g.hk, i = blockIdx.x >> 3, kind = i % kinds;
+  const int b = find_page(ch, g.batch, PS, lane, i / kinds * 8 + (blockIdx.x & 7), run, page);
   if (b < 0 || page < 0 || page >= run_pages(run, PS)) return;
   const int lp0 = run.pos / PS, lp = lp0 + page;
   // slots of this page that the run fills, and the row of slot 0
@@ -405,9 +404,11 @@ int64_t rotate_blocks(const Geometry& g, int rows, bool q, bool k) {
   return (rows * ((heads + vpw - 1) / vpw) + 3) / 4;
 }
 
-// every sequence's pages, at most n / P + 2 of each, times the workgroups of a page
+// every sequence's pages, at most n / P + 2 of each, in eights (an XCD's workgroups are
+// every eighth), times the workgroups of a page
 int64_t append_blocks(const Geometry& g, int n_rows, bool q) {
-  return (n_rows / g.P + 2 * (int64_t)std::min(g.batch, n_rows)) * (q ? 2 : 1) * g.hk;
+  const int64_t pages = n_rows / g.P + 2 * (int64_t)std::min(g.batch, n_rows);
+  return (pages + 7) / 8 * 8 * (q ? 2 : 1) * g.hk;
 }
 
 }  // namespace
@@ -441,14 +442,14 @@ hipError_t launch_rotate_qk(const Geometry& g, const retro_rotary& r, const int3
 }
 
 bool append_rotary_supported(const Geometry& g, int n_rows) {
-  return append_blocks(g, n_rows, true) < ((int64_t)1 << 31) - 8;
+  return append_blocks(g, n_rows, true) < (int64_t)1 << 31;
 }
 
 hipError_t launch_append_rotary(const Geometry& g, int step, const retro_kv_cache& c,
                                 const retro_chunk& ch, const retro_rotary& r, const void* q,
                                 int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, void* q_out, hipStream_t s) {
-  const unsigned grid = (unsigned)((append_blocks(g, ch.n_rows, q != nullptr) + 7) / 8 * 8);
+  const unsigned grid = (unsigned)append_blocks(g, ch.n_rows, q != nullptr);
   return with_type_and_dim(g, [&](auto t, auto d) {
     using T = decltype(t);
     auto go = [&](auto ps) {
