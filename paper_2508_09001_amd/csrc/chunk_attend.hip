@@ -49,7 +49,7 @@ constexpr int kRowsFew = 32;             // rows of a unit in the first way
 constexpr int kRowsMany = 32 * kWaves;   // and in the second
 constexpr int kCus = 256;
 constexpr int kMinMany = 8, kMinFew = 4; // least steps of 64 keys of a part
-constexpr int kScans = 4;                // prefix sums made together
+constexpr int kScans = 6;                // prefix sums made together
 
 struct AttendCall {
   retro_chunk ch;
@@ -182,26 +182,30 @@ __device__ __forceinline__ Seq first_seq(const FindLds& L, int b, int G) {
 // matrix instructions are 16 times slower, and the reading does not show.
 template <bool MANY>
 __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, int tid) {
-  enum { kLine, kSmall, kMany, kTiles };
-  Scan<4> x;
-  for (int j = 0; j < 4; ++j) x.of[j] = 0;
+  enum { kLine, kLineTiles, kSmall, kSmallTiles, kMany, kTiles, kSums };
+  static_assert(kSums <= kScans, "sums made together");
+  Scan<kSums> x;
+  for (int j = 0; j < kSums; ++j) x.of[j] = 0;
   const bool wavefront = a.batch <= 64;
   for (int b = wavefront ? tid & 63 : tid; b < a.batch; b += kThreads) {
     const Seq s = load_seq(a, P, b);
     if (b < kThreads) L.first[b] = int4{s.run.row, s.run.n, s.run.pos, s.end};  // (the same from every wavefront)
-    const int64_t line = a.hk * s.place(s.tiles(kRowsFew), a.G);
+    const int small = s.tiles(kRowsFew);
+    const int64_t line = a.hk * s.place(small, a.G);
     if (!MANY || s.few) {
       x.of[kLine] += line;
+      x.of[kLineTiles] += (int64_t)a.hk * small;
     } else {
       const int64_t tiles = (int64_t)a.hk * s.tiles(kRowsMany);
       x.of[kSmall] += line;
+      x.of[kSmallTiles] += (int64_t)a.hk * small;
       x.of[kMany] += tiles * s.steps();
       x.of[kTiles] += tiles;
     }
   }
   if (wavefront) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x.total[j] = last_lane(wave_scan_i64(x.of[j]));
+    for (int j = 0; j < kSums; ++j) x.total[j] = last_lane(wave_scan_i64(x.of[j]));
     __syncthreads();
   } else {
     block_scan(x, L.scratch, tid);
@@ -211,8 +215,23 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
   c.all_line = !MANY || (many < 5 * n && 8 * tiles < n && many > 16 * tiles);
   c.line = x.total[kLine] + (c.all_line ? x.total[kSmall] : 0);
   c.many = c.all_line ? 0 : many;
-  c.share = max((c.line + n - 1) / n, (int64_t)kMinFew);
-  c.part = (int)min(max((c.line + c.many + n - 1) / n, (int64_t)kMinMany), (int64_t)1 << 30);
+  // (tiles shorter than four steps are a share each: one after the other they would take
+  // as many round trips: 33 sequences of 33 tokens 22 us, 13 so)
+  const int64_t of_line = x.total[kLineTiles] + (c.all_line ? x.total[kSmallTiles] : 0);
+  const int64_t least = of_line ? min((c.line + of_line - 1) / of_line, (int64_t)kMinFew) : 1;
+  c.share = max((c.line + n - 1) / n, least);
+  // A part's most steps: all workgroups' share, but no less than that gives every
+  // workgroup one part where there are fewer tiles than workgroups (of tiles of unlike
+  // lengths every other one has a part more; of like ones all have as many): a second
+  // round of some costs as much as one of all.  1332 rows of 8 KV heads and two
+  // sequences at 420 tokens 82 -> 52 us.
+  int64_t part = (c.line + c.many + n - 1) / n;
+  if (MANY && c.many && tiles <= n) {
+    part = max(part, (c.many + n - tiles / 2 - 1) / (n - tiles / 2));
+    const int64_t steps = (c.many + tiles - 1) / tiles;
+    if ((steps + part - 1) / part * tiles > n) part = (steps + n / tiles - 1) / (n / tiles);
+  }
+  c.part = (int)min(max(part, (int64_t)kMinMany), (int64_t)1 << 30);
   return c;
 }
 
@@ -904,7 +923,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   // ---- tiles of 32 rows: this workgroup's share of the line of steps
   auto few_rows = [&]() {
     constexpr int PT = 32 / P;  // pages of a tile
-    const int64_t mine = (int64_t)blockIdx.x * cut.share, upto = min(mine + cut.share, cut.line);
+    // (from the last workgroup on: the first ones take the tiles of many rows, if there are few)
+    const int64_t me = kCus - 1 - blockIdx.x, mine = me * cut.share, upto = min(mine + cut.share, cut.line);
     for (int64_t pos = mine; pos < upto;) {
       int b = 0;
       int64_t local = 0, before;
@@ -1005,7 +1025,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         barrier();
         // a part: slot 2 k of workgroup k for what its share begins with, 2 k + 1 for what it ends with
         const bool whole = n == length;
-        const int64_t k = blockIdx.x;
+        const int64_t k = me;
         auto slot = [&](int64_t i) { return a.few + i * slot_floats(kRowsFew, D); };
         const __amdgpu_buffer_rsrc_t part = coherent_rsrc(slot(2 * k + (pos != mine)));
         for (int i = tid; i < nr * (D / 4); i += kThreads) {
