@@ -93,6 +93,7 @@ class RetroDecoder:
             table = self.rotary[0].table if self.rotary and rot_dim else None
             self.rotary.append(RetroRotary(positions, rot_dim, table=table,
                                            q_norm=w.get("q_norm"), k_norm=w.get("k_norm"), **opts))
+            lay.check_rotary(self.rotary[-1])
         if self.rotated:
             # position of window row r less the tokens stored, row W the newest
             self.window_offset = torch.arange(-self.W, 1, dtype=torch.int32, device=self.device)
@@ -143,7 +144,11 @@ class RetroDecoder:
         """Prompts, or their next chunks, through the whole stack on the current stream:
         ``rows[b]`` tokens of every sequence, ``emb`` [sum of rows][d_model] on the device,
         one sequence's rows behind the other's.  Returns the residual stream after the
-        last layer, [sum of rows][d_model] fp32.  May be called between decode steps."""
+        last layer, [sum of rows][d_model] fp32.  Between decode steps too where W is 0;
+        with W > 0 a step's window rows are the tokens of the steps before it, so that
+        prompts come before the first one (ValueError otherwise)."""
+        if self.W and self.decoded:
+            raise ValueError("with a window, prompts come before the first decode step")
         if emb.dim() != 2 or emb.shape[0] != sum(rows) or emb.shape[1] != self.d_model:
             raise ValueError("emb must be [sum of rows][d_model]")
         if any(lay._lens != self.layers[0]._lens for lay in self.layers):

@@ -230,6 +230,39 @@ class RetroLayer:
         self._keep = (q_window, k_new, v_new)
 
     # -- chunks of prompts, rotated positions -----------------------------------------
+    # (one at a time, like every other call of a layer; with `stream` the copies that
+    # an input needs and the new tensors are that stream's too)
+    @contextlib.contextmanager
+    def _on_stream(self, stream, *inputs):
+        """Work of a call on the cache's device and on `stream` (None: the current one)."""
+        with torch.cuda.device(self.seq_lens.device):
+            if stream is None:
+                yield
+                return
+            s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+            with torch.cuda.stream(s):
+                yield
+            for x in inputs:  # may be freed by the caller before `stream` has read them
+                if isinstance(x, torch.Tensor) and x.is_cuda:
+                    x.record_stream(s)
+
+    def check_rotary(self, rotary: RetroRotary) -> None:
+        """ValueError unless the norms' weights and the table are this layer's to read."""
+        for w in (rotary.q_norm, rotary.k_norm):
+            if w is not None and (tuple(w.shape) != (self.d,) or w.dtype != self.dtype or
+                                  w.device.type != self.device.type):
+                raise ValueError(f"norm weights must be [{self.d}] {self.dtype} on {self.device}")
+        if rotary.table is not None and rotary.table.device.type != self.device.type:
+            raise ValueError(f"the table must be on {self.device}")
+
+    def _check_chunk(self, chunk: RetroChunk) -> None:
+        if len(chunk.rows) != self.batch:
+            raise ValueError("the chunk must hold one entry per sequence")
+        if chunk.row_start.device.type != self.device.type:
+            raise ValueError(f"the chunk must be on {self.device}")
+        if chunk.n_rows > self.batch * self.dims.max_pages * self.P:
+            raise ValueError("the chunk has more rows than the cache has tokens")
+
     def _rows(self, x, heads: int) -> torch.Tensor:
         """x [rows][heads][d] or [rows][heads * d] as it is where the library can read it
         (rows may be strided: parts of one projection's output), else copied."""
@@ -260,16 +293,17 @@ class RetroLayer:
         """Queries [rows][h_q][d] and keys [rows][h_k][d] (either may be None) normalised
         and rotated to ``positions`` [rows] (int32, on the device), as new tensors."""
         rows = int(positions.numel())
-        positions = positions.to(device=self.device, dtype=torch.int32).contiguous()
-        q = None if q is None else self._rows(q, self.hq)
-        k = None if k is None else self._rows(k, self.hk)
-        if any(x is not None and x.shape[0] != rows for x in (q, k)):
-            raise ValueError("one position per row")
-        # (rows of negative position are not written: they come out as zeros)
-        qo, ko = (None if x is None else
-                  torch.zeros(rows, h, self.d, dtype=self.dtype, device=self.device)
-                  for x, h in ((q, self.hq), (k, self.hk)))
-        with _on(self.device):
+        self.check_rotary(rotary)
+        with self._on_stream(stream, positions, q, k):
+            positions = positions.to(device=self.device, dtype=torch.int32).contiguous()
+            q = None if q is None else self._rows(q, self.hq)
+            k = None if k is None else self._rows(k, self.hk)
+            if any(x is not None and x.shape[0] != rows for x in (q, k)):
+                raise ValueError("one position per row")
+            # (rows of negative position are not written: they come out as zeros)
+            qo, ko = (None if x is None else
+                      torch.zeros(rows, h, self.d, dtype=self.dtype, device=self.device)
+                      for x, h in ((q, self.hq), (k, self.hk)))
             B.retro_rotate_qk(self.dims, rotary.struct, positions, rows,
                               q, 0 if q is None else self._stride(q, self.hq),
                               k, 0 if k is None else self._stride(k, self.hk), qo, ko, stream)
@@ -280,15 +314,17 @@ class RetroLayer:
                      stream=None) -> Optional[torch.Tensor]:
         """Store the chunk's keys and values [rows][h_k][d], keys normalised and rotated on
         the way; returns the queries q [rows][h_q][d], treated likewise (None without q)."""
-        k, v = self._rows(k, self.hk), self._rows(v, self.hk)
-        q = None if q is None else self._rows(q, self.hq)
-        if any(x is not None and x.shape[0] != chunk.n_rows for x in (q, k, v)):
-            raise ValueError("one row of q, k and v per row of the chunk")
+        self.check_rotary(rotary)
+        self._check_chunk(chunk)
         if chunk.start != self._lens:
             raise ValueError("the chunk does not begin where the sequences end")
-        out = None if q is None else torch.empty(chunk.n_rows, self.hq, self.d, dtype=self.dtype,
-                                                 device=self.device)
-        with _on(self.device):
+        with self._on_stream(stream, k, v, q, chunk.row_start):
+            k, v = self._rows(k, self.hk), self._rows(v, self.hk)
+            q = None if q is None else self._rows(q, self.hq)
+            if any(x is not None and x.shape[0] != chunk.n_rows for x in (q, k, v)):
+                raise ValueError("one row of q, k and v per row of the chunk")
+            out = None if q is None else torch.empty(chunk.n_rows, self.hq, self.d,
+                                                     dtype=self.dtype, device=self.device)
             B.retro_append_kv_rotary(self.dims, step, self.cache, chunk.struct, rotary.struct,
                                      q, 0 if q is None else self._stride(q, self.hq),
                                      k, self._stride(k, self.hk), v, self._stride(v, self.hk),
@@ -303,20 +339,21 @@ class RetroLayer:
         """Dense causal attention of the chunk's (rotated) queries [rows][h_q][d] over
         everything stored: outputs [rows][h_q][d], with ``lse`` also the natural
         log-normalisers [rows][h_q] fp32."""
-        q = self._rows(q, self.hq)
-        if q.shape[0] != chunk.n_rows:
-            raise ValueError("one row of q per row of the chunk")
-        out = torch.empty(chunk.n_rows, self.hq, self.d, dtype=self.dtype, device=self.device)
-        z = torch.empty(chunk.n_rows, self.hq, dtype=torch.float32,
-                        device=self.device) if lse else None
-        need = B.retro_chunk_workspace_size(self.dims, chunk.n_rows)
-        if self.chunk_ws is None or self.chunk_ws.numel() < need:
-            # for as many rows as the cache has tokens, so that a captured call's
-            # workspace is not replaced by a larger one
-            most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G)
-            need = max(need, B.retro_chunk_workspace_size(self.dims, most))
-            self.chunk_ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
-        with _on(self.device):
+        self._check_chunk(chunk)
+        with self._on_stream(stream, q, chunk.row_start):
+            q = self._rows(q, self.hq)
+            if q.shape[0] != chunk.n_rows:
+                raise ValueError("one row of q per row of the chunk")
+            out = torch.empty(chunk.n_rows, self.hq, self.d, dtype=self.dtype, device=self.device)
+            z = torch.empty(chunk.n_rows, self.hq, dtype=torch.float32,
+                            device=self.device) if lse else None
+            need = B.retro_chunk_workspace_size(self.dims, chunk.n_rows)
+            if self.chunk_ws is None or self.chunk_ws.numel() < need:
+                # for as many rows as the cache has tokens, so that a captured call's
+                # workspace is not replaced by a larger one
+                most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G)
+                need = max(need, B.retro_chunk_workspace_size(self.dims, most))
+                self.chunk_ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
             B.retro_chunk_attend(self.dims, self.cache, chunk.struct, q, self._stride(q, self.hq),
                                  out, z, self.chunk_ws, self.chunk_ws.numel(), stream)
         self._keep_attend = (q, chunk)

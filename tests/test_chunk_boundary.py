@@ -109,3 +109,45 @@ def test_chunk_attend(B):
     with pytest.raises(B.RetroError):
         B.retro_chunk_workspace_size(d, -1)
     assert lib.retro_chunk_workspace_size(C.byref(d), 5, None) == INVALID
+
+
+def test_layer_refuses_what_its_kernels_would_misread(B):
+    """Weights of another length or type, tables and chunks on the wrong device, of
+    another batch or past the cache: refused before anything is read."""
+    import torch
+    from paper_2508_09001_amd.layer import RetroChunk, RetroLayer, RetroRotary
+    lay = RetroLayer(batch=2, num_kv_heads=1, group=2, head_dim=64, page_size=16, budget=16, window=0,
+                     max_pages=2, device="cpu")
+    x, one = torch.zeros(2, 64), torch.ones(64)
+    good = RetroRotary(32, 0, k_norm=one, device="cpu")
+    lay.check_rotary(good)
+    bad = [RetroRotary(32, 0, device="cpu", **kw)
+           for kw in (dict(q_norm=torch.ones(32)), dict(k_norm=torch.ones(128)), dict(k_norm=one, dtype="f32"))]
+    elsewhere = RetroRotary(32, 64, device="cpu", table=torch.zeros(32, 32, 2, device="meta"))
+    for rot in bad + [elsewhere]:
+        with pytest.raises(ValueError):
+            lay.rotate(rot, torch.arange(2), k=x)
+        with pytest.raises(ValueError):
+            lay.append_chunk(0, lay.chunk((1, 1)), rot, x, x)
+    q = torch.zeros(2, 2, 64)
+    for ch in (RetroChunk((2,), (0,), "cpu"), RetroChunk((1, 1), (0, 0), "meta")):
+        with pytest.raises(ValueError):
+            lay.attend_chunk(ch, q)
+        with pytest.raises(ValueError):
+            lay.append_chunk(0, ch, good, x, x)
+    with pytest.raises(ValueError):   # 65 rows, 64 tokens
+        lay.attend_chunk(lay.chunk((32, 33)), torch.zeros(65, 2, 64))
+
+
+def test_decoder_refuses_prompts_between_the_steps_of_a_window(B):
+    import torch
+    from paper_2508_09001_amd.decode import RetroDecoder
+    w = dict(wq=torch.zeros(128, 128), wk=torch.zeros(128, 64), wv=torch.zeros(128, 64), wo=torch.zeros(128, 128))
+    kw = dict(batch=1, num_kv_heads=1, group=2, head_dim=64, page_size=16, budget=16, max_pages=2, device="cpu",
+              library_projections=False, rotary=dict(rot_dim=0))
+    dec = RetroDecoder([w], window=2, **kw)
+    dec.decoded = 1
+    with pytest.raises(ValueError, match="window"):
+        dec.prefill_chunk((1,), torch.zeros(1, 128))
+    with pytest.raises(ValueError):   # a norm's weights of another length
+        RetroDecoder([dict(w, q_norm=torch.ones(32))], window=0, **kw)

@@ -193,3 +193,36 @@ def test_layer_calls_take_views_and_lists():
     lays[0].append(1, torch.zeros(2, hk, d), torch.zeros(2, hk, d))
     with pytest.raises(ValueError):   # the sequences have grown since
         lays[0].append_chunk(0, ch, rot, qkv[0, :1, :hk * d], qkv[0, :1, :hk * d])
+
+
+def test_layer_calls_on_another_stream_while_the_current_one_is_busy():
+    """Copies of strided inputs, new tensors and the workspace's zeros are work of the
+    call's stream, not of the current one, which sleeps for some milliseconds meanwhile."""
+    from paper_2508_09001_amd.layer import RetroChunk, RetroLayer, RetroRotary
+    hk, G, d, P, mp, n = 2, 4, 128, 16, 96, 40
+    rot = RetroRotary(mp * P, d)
+    # (transposed and fp32: copied by every call)
+    qkv = [torch.randn(m, heads * d, device="cuda").t().contiguous().t()
+           for m in (1400, n) for heads in (hk, hk, hk * G)]
+    chunks = [RetroChunk((1400,), (0,), "cuda"), RetroChunk((n,), (1400,), "cuda")]
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    lays = [RetroLayer(batch=1, num_kv_heads=hk, group=G, head_dim=d, page_size=P, budget=P, window=0, max_pages=mp)
+            for _ in range(2)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def calls(lay, stream):
+        for ch, (k, v, q) in zip(chunks, (qkv[:3], qkv[3:])):
+            q = lay.append_chunk(0, ch, rot, k, v, q, stream=stream)
+            o, z = lay.attend_chunk(ch, q, lse=True, stream=stream)
+        return q, o, z, lay.rotate(rot, pos, q=qkv[5], stream=stream)[0]
+
+    want = calls(lays[0], None)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    got = calls(lays[1], side)
+    side.synchronize()
+    with torch.cuda.stream(side):
+        same = [bool(torch.equal(a, b)) for a, b in zip(got, want)]
+    assert same == [True] * 4
+    torch.cuda.synchronize()
