@@ -49,6 +49,11 @@ constexpr int kRowsFew = 32;             // rows of a unit in the first way
 constexpr int kRowsMany = 32 * kWaves;   // and in the second
 constexpr int kCus = 256;
 constexpr int kMinMany = 8, kMinFew = 4; // least steps of 64 keys of a part
+// What a step of a tile costs a workgroup while others do the other kind: 0.8 and 2.1 us
+// alone, each longer beside the other (us with 2 to 5, 1 to 2 and 3 to 5: a chunk of 100
+// rows beside 15 tokens at 4K to 16K 153, 148, 139; of 256 beside 32 at 2K to 8K 145, 145,
+// 166; of 1024 beside 63 at 0.5K to 2K 126, 134, 113)
+constexpr int64_t kFewCost = 1, kManyCost = 2;
 constexpr int kScans = 6;                // prefix sums made together
 
 struct AttendCall {
@@ -103,9 +108,18 @@ struct Cut {
   bool all_line;      // no tiles of many rows
   int64_t line;       // steps of all tiles of 32 rows, of all KV heads
   int64_t share;      // a workgroup's share of them
+  int64_t first, long_share;  // the first ones', that have no tile of many rows
   int64_t many;       // steps of all tiles of many rows
   int part;           // most steps of a part of such a tile
   __device__ __forceinline__ bool on_line(const Seq& s) const { return s.few || all_line; }
+  // where workgroup k's share of the line begins, and whose share a step is in
+  __device__ __forceinline__ int64_t begin(int64_t k) const {
+    return min(k, first) * long_share + max(k - first, (int64_t)0) * share;
+  }
+  __device__ __forceinline__ int64_t owner(int64_t step) const {
+    const int64_t past = step - first * long_share;
+    return past < 0 ? step / long_share : first + past / share;
+  }
   __device__ __forceinline__ int64_t line_of(const Seq& s, const AttendCall& a) const {
     return on_line(s) ? a.hk * s.place(s.tiles(kRowsFew), a.G) : 0;
   }
@@ -220,16 +234,38 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
   const int64_t of_line = x.total[kLineTiles] + (c.all_line ? x.total[kSmallTiles] : 0);
   const int64_t least = of_line ? min((c.line + of_line - 1) / of_line, (int64_t)kMinFew) : 1;
   c.share = max((c.line + n - 1) / n, least);
-  // A part's most steps: all workgroups' share, but no less than that gives every
-  // workgroup one part where there are fewer tiles than workgroups (of tiles of unlike
-  // lengths every other one has a part more; of like ones all have as many): a second
-  // round of some costs as much as one of all.  1332 rows of 8 KV heads and two
+  c.first = c.long_share = 0;
+  // A part's most steps: all workgroups' share of the work, but no less than that gives
+  // every workgroup one part where there are fewer tiles than workgroups (of tiles of
+  // unlike lengths every other one has a part more; of like ones all have as many): a
+  // second round of some costs as much as one of all.  1332 rows of 8 KV heads and two
   // sequences at 420 tokens 82 -> 52 us.
-  int64_t part = (c.line + c.many + n - 1) / n;
+  int64_t part = (kManyCost * c.many + kFewCost * c.line + kManyCost * n - 1) / (kManyCost * n);
   if (MANY && c.many && tiles <= n) {
+    const int64_t work = part;
     part = max(part, (c.many + n - tiles / 2 - 1) / (n - tiles / 2));
     const int64_t steps = (c.many + tiles - 1) / tiles;
     if ((steps + part - 1) / part * tiles > n) part = (steps + n / tiles - 1) / (n / tiles);
+    part = max(part, (int64_t)kMinMany);
+    if (c.line) {
+      // The workgroups without a part take as much more of the line, so that some read
+      // while others multiply (us, against equal shares of the line: a chunk of 256 rows
+      // beside 32 tokens at 2K to 8K 215 -> 145, of 100 beside 15 at 4K to 16K 253 -> 148).
+      Scan<1> y;
+      y.of[0] = 0;
+      for (int b = wavefront ? tid & 63 : tid; b < a.batch; b += kThreads) {
+        const Seq s = b < kThreads ? first_seq(L, b, a.G) : load_seq(a, P, b);
+        if (!s.few) y.of[0] += (int64_t)a.hk * s.tiles(kRowsMany) * ((s.steps() + part - 1) / part);
+      }
+      if (wavefront) y.total[0] = last_lane(wave_scan_i64(y.of[0]));
+      else block_scan(y, L.scratch, tid);
+      c.first = max(n - y.total[0], (int64_t)0);
+      if (c.first) {
+        c.long_share = max(min((kManyCost * work + kFewCost - 1) / kFewCost, (c.line + c.first - 1) / c.first), least);
+        const int64_t left = max(c.line - c.first * c.long_share, (int64_t)0);
+        c.share = max((left + n - c.first - 1) / max(n - c.first, (int64_t)1), least);
+      }
+    }
   }
   c.part = (int)min(max(part, (int64_t)kMinMany), (int64_t)1 << 30);
   return c;
@@ -924,7 +960,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   auto few_rows = [&]() {
     constexpr int PT = 32 / P;  // pages of a tile
     // (from the last workgroup on: the first ones take the tiles of many rows, if there are few)
-    const int64_t me = kCus - 1 - blockIdx.x, mine = me * cut.share, upto = min(mine + cut.share, cut.line);
+    const int64_t me = kCus - 1 - blockIdx.x, mine = cut.begin(me), upto = min(cut.begin(me + 1), cut.line);
     for (int64_t pos = mine; pos < upto;) {
       int b = 0;
       int64_t local = 0, before;
@@ -1056,12 +1092,12 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         }
         if (!whole) {
           // the tile's steps are start .. start + length - 1 of the line
-          const int64_t start = pos - step0, k0 = start / cut.share;
-          const int parts = (int)((start + length - 1) / cut.share - k0) + 1;
+          const int64_t start = pos - step0, k0 = cut.owner(start);
+          const int parts = (int)(cut.owner(start + length - 1) - k0) + 1;
           if (last_part(a.counters + k0, parts, &L.last, tid))
             join_few<D>(
                 L.u.join, nr, parts, rows.c, tid,
-                [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != k0 * cut.share)); },
+                [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != cut.begin(k0))); },
                 [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, rho0 + row, m, l, d, o); });
         }
         barrier();
