@@ -345,7 +345,11 @@ struct Shape {
   static constexpr int STAGE = 2 * NB * TILE;    // bytes of a stage: keys, then values
   static constexpr int LOADS = TILE / 1024;      // wavefront copies of a tile's keys (or values)
   static constexpr int PPP = P * D * (int)sizeof(T) / 1024;  // copies of a page
-  static constexpr int OWN = TILE <= 8192 ? kWaves : kWaves / 2;  // wavefronts in the first way
+  // In the first way a wavefront has one buffer for a tile's keys and one for its values,
+  // or where that is too much LDS (fp32 of d 128) one for both in turn, the other
+  // wavefront of the SIMD multiplying meanwhile (us, against two for half as many
+  // wavefronts: 1024 rows at 1024 328 -> 266, a token at 32K 80 -> 64).
+  static constexpr bool ONE = TILE > 8192;
   static constexpr int OROW = D + 4;             // row of the joining buffer
   static constexpr int QC = CPR / 2;             // pieces of a row per lane half
   // order of a key row's pieces, and of a value row's
@@ -373,8 +377,8 @@ struct ChunkLds {
   using S = Shape<T, D, P>;
   union {
     char stage[2][S::STAGE];
-    char own[S::OWN][2 * S::TILE];
-    float o[S::OWN][kRowsFew][S::OROW];
+    char own[kWaves][(S::ONE ? 1 : 2) * S::TILE];
+    float o[kWaves][kRowsFew][S::OROW];
     JoinLds join;
     JoinManyLds join_many;
   } u;
@@ -605,8 +609,27 @@ struct Rows {
     }
   }
 
-  // O^T += V^T P^T of one tile.  Values of slots that hold no token of the sequence
-  // (stored: tokens of it from this tile's first key on) are taken as zero.
+  // Zeroes an fp32 tile's values of slots that hold no token of the sequence (stored:
+  // tokens of it from this tile's first key on), each lane those that it will read.
+  __device__ __forceinline__ void clear(int stored, uint32_t bad) const {
+#pragma unroll
+    for (int piece = 0; piece < 32 / S::E; piece += 2) {
+      const int k = S::E * (piece + half), n = bad >> (k / P) & 1 ? 0 : stored - k;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        const uint32_t at = voff[piece % S::CPV / 2] + (piece / S::CPV * D + i * 32) * P * sizeof(T);
+        u32x4 v = lds_piece<T>(at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = n > e ? v[e] : 0u;
+        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = v;
+      }
+    }
+  }
+
+  // O^T += V^T P^T of one tile.  bf16 values of slots that hold no token are taken as
+  // zero here: an AND beside each of few matrix instructions, hidden by the memory
+  // (fp32, with four times as many and each four times as long, would wait for them:
+  // 1024 rows at 1024, d 128, 370 -> 328 us without).
   // SPLIT: a bf16 weight is given as two, what the first one's rounding leaves and it.
   template <bool SPLIT>
   __device__ __forceinline__ void values(int at, const f32x16& p, int stored, uint32_t bad) {
@@ -634,16 +657,11 @@ struct Rows {
       for (int i = 0; i < DT; ++i) {
         u32x4 v = lds_piece<T>(voff[piece % S::CPV / 2] + (more + i * (int)(32 * P * sizeof(T))));
         const int k = S::E * (piece + half);
-        const int n = bad >> (k / P) & 1 ? 0 : stored - k;  // elements that count
+        [[maybe_unused]] const int n = bad >> (k / P) & 1 ? 0 : stored - k;  // elements that count
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             v[e] &= (n > 2 * e ? 0xffffu : 0u) | (n > 2 * e + 1 ? 0xffff0000u : 0u);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = n > e ? v[e] : 0u;
-        }
-        if constexpr (sizeof(T) == 2) {
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w, acc[i], 0,
                                                            0, 0);
           if constexpr (SPLIT)
@@ -1000,7 +1018,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         int lim;
         const T* qrow = row_at(s, h, rho0 + (lane & 31), live, lim);
         rows.start(qrow, live, lim);
-        const uint32_t ks = st + wave * 2 * S::TILE, vs = ks + S::TILE;
+        const int all_see = min(s.run.pos + rho0 / a.G, s.end - 1);  // last token that every row sees
+        const uint32_t ks = st + wave * (int)sizeof(L.u.own[0]), vs = S::ONE ? ks : ks + S::TILE;
         rows.read_from(ks, vs);
         // copies a tile's keys or values; which of its pages are not mapped
         auto issue = [&](const char* base, uint32_t to, int key, uint32_t off, auto x) {
@@ -1020,26 +1039,33 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
           return bits;
         };
         int key = key_begin + wave * 32;
-        if (wave < S::OWN && key < key_end) {
+        if (key < key_end) {
           uint32_t bad = issue(kh, ks, key, kcopy, kxor);
-          issue(vh, vs, key, vcopy, vxor);
-          for (; key < key_end; key += S::OWN * 32) {
-            const int next = key + S::OWN * 32;
+          if constexpr (!S::ONE) issue(vh, vs, key, vcopy, vxor);
+          for (; key < key_end; key += kWaves * 32) {
+            const int next = key + kWaves * 32;
             f32x16 sc[1];
-            wait_loads<S::LOADS>();
+            wait_loads<S::ONE ? 0 : S::LOADS>();
             sc[0] = rows.scores(0);
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
             uint32_t bad_next = 0;
-            if (next < key_end) bad_next = issue(kh, ks, next, kcopy, kxor);
-            // (masking every tile costs nothing here: the wavefront waits for memory)
-            rows.mask(sc, key, bad);
+            if constexpr (S::ONE) issue(vh, vs, key, vcopy, vxor);
+            else if (next < key_end) bad_next = issue(kh, ks, next, kcopy, kxor);
+            // (masking every tile costs nothing for bf16: the wavefront waits for memory)
+            const bool clean = sizeof(T) == 4 && !bad && key + 31 <= all_see;
+            if (!clean) rows.mask(sc, key, bad);
             rows.weights(sc, rows.follow(sc));
-            if (next < key_end) wait_loads<S::LOADS>();
+            if (!S::ONE && next < key_end) wait_loads<S::LOADS>();
             else wait_loads<0>();
             // (and neither does the weights' second half: 0.0022 -> 0.0017 off 64 bits)
+            if constexpr (sizeof(T) == 4)
+              if (!clean) rows.clear(s.end - key, bad);
             rows.template values<true>(0, sc[0], s.end - key, bad);
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-            if (next < key_end) issue(vh, vs, next, vcopy, vxor);
+            if (next < key_end) {
+              if constexpr (S::ONE) bad_next = issue(kh, ks, next, kcopy, kxor);
+              else issue(vh, vs, next, vcopy, vxor);
+            }
             bad = bad_next;
           }
         }
@@ -1051,7 +1077,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
           L.m[wave][r] = rows.m;
           L.l[wave][r] = rows.l;
         }
-        if (wave < S::OWN && r < nr)
+        if (r < nr)
 #pragma unroll
           for (int i = 0; i < R_t::DT; ++i)
 #pragma unroll
@@ -1068,12 +1094,12 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
           const int row = i / (D / 4), d = i % (D / 4) * 4;
           float m = -INFINITY;
 #pragma unroll
-          for (int w = 0; w < S::OWN; ++w) m = fmaxf(m, L.m[w][row]);
+          for (int w = 0; w < kWaves; ++w) m = fmaxf(m, L.m[w][row]);
           const float mu = m == -INFINITY ? 0.f : m;
           float l = 0.f;
           f32x4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int w = 0; w < S::OWN; ++w) {
+          for (int w = 0; w < kWaves; ++w) {
             const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * rows.c);
             const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
             l = __builtin_fmaf(e, L.l[w][row], l);
