@@ -391,7 +391,7 @@ auto with_type_and_dim(const Geometry& g, F f) {
 
 // Groups of heads per wavefront: one where there are few rows (64 rows of 40 heads: 4.0
 // us), five where the wavefronts fill the GPU many times over (8192 rows of 40 heads, 172
-// MB: 60 us with one, 54, 52, 49, 48 and 48 with 2, 3, 4, 5 and 8; 40 us, 4.3 TB/s, with
+// MB: 60 us with one, 54, 52, 49, 48 and 48 with 2, 3, 4, 5 and 8; 36.5 us, 4.7 TB/s, with
 // the outputs written past the L2s).
 constexpr int kManyGroups = 5;
 int rotate_groups(const Geometry& g, int rows, bool q, bool k) {
