@@ -280,3 +280,29 @@ def test_another_stream(hk, seqs):
     b.B.retro_chunk_attend(b.dims, b.cache, b.chunk, b.q, b.q.stride(0), b.out, b.lse, b.ws, b.ws_bytes, stream=s)
     s.synchronize()
     assert torch.equal(b.out, want) and torch.equal(b.lse, z)
+
+
+# chunks of many rows beside other sequences' tokens: the workgroups without a part of the
+# former take longer shares of the latter, all of them or not; more sequences than a
+# wavefront has lanes, and than a workgroup has threads
+MIXED = [
+    ([(256, 3000)], 12, 4000, 8, 4, 128, 16),
+    ([(300, 900), (1, 77), (150, 400)], 80, 700, 8, 4, 64, 32),
+    ([(120, 130)], 560, 60, 8, 4, 64, 16),
+    ([(700, 700)], 5, 5000, 4, 8, 128, 32),
+    ([(130, 2100), (70, 5)], 20, 3000, 8, 4, 128, 16),
+]
+
+
+@pytest.mark.parametrize("chunks,tokens,ctx,hk,G,d,P", MIXED, ids=[str(i) for i in range(len(MIXED))])
+def test_chunks_beside_tokens(chunks, tokens, ctx, hk, G, d, P):
+    rng = np.random.default_rng(tokens)
+    seqs = [(1, int(rng.integers(0, ctx))) for _ in range(tokens)]
+    seqs[3:3] = chunks
+    b = Batch("bf16", hk, G, d, P, seqs, seed=tokens).run()
+    b.check()
+    out, z = b.out.clone(), b.lse.clone()
+    for _ in range(3):
+        b.out.fill_(5.0)
+        b.run()
+        assert torch.equal(b.out, out) and torch.equal(b.lse, z)
