@@ -159,7 +159,8 @@ class RetroDecoder:
             x = h.to(self.dtype)
             q = lay.append_chunk(self.decoded, chunk, rot, torch.matmul(x, w["wk"]),
                                  torch.matmul(x, w["wv"]), torch.matmul(x, w["wq"]))
-            lay.chunk_ws = self.layers[0].chunk_ws  # one for all, used in turn
+            if lay.chunk_ws is None:
+                lay.chunk_ws = self.layers[0].chunk_ws  # one for all, used in turn
             o = lay.attend_chunk(chunk, q)
             h = h + torch.matmul(o.view(-1, self.hq * self.d), w["wo"]).float()
         return h

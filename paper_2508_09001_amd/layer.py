@@ -288,6 +288,26 @@ class RetroLayer:
             raise ValueError("rows must hold one entry per sequence")
         return RetroChunk(rows, self._lens, self.device)
 
+    def _chunk_workspace(self) -> torch.Tensor:
+        if self.chunk_ws is None:
+            # (a captured fill would clear the counts at replays only, not for the calls
+            # in front of the first one)
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("reserve_chunks comes before a captured attend_chunk")
+            # for as many rows as the cache has tokens: never replaced by a larger one
+            most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G)
+            self.chunk_ws = torch.zeros(B.retro_chunk_workspace_size(self.dims, most),
+                                        dtype=torch.uint8, device=self.device)
+        return self.chunk_ws
+
+    def reserve_chunks(self) -> None:
+        """Makes the workspace of ``attend_chunk``, ready for every stream when this returns.
+        The first ``attend_chunk`` makes it too, except where it is captured into a graph
+        (RuntimeError): a program that captures calls this first."""
+        with torch.cuda.device(self.seq_lens.device):
+            self._chunk_workspace()
+            torch.cuda.current_stream().synchronize()
+
     def rotate(self, rotary: RetroRotary, positions: torch.Tensor, q=None, k=None,
                stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
         """Queries [rows][h_q][d] and keys [rows][h_k][d] (either may be None) normalised
@@ -338,7 +358,7 @@ class RetroLayer:
                      ) -> Union[torch.Tensor, Tuple[torch.Tensor, torch.Tensor]]:
         """Dense causal attention of the chunk's (rotated) queries [rows][h_q][d] over
         everything stored: outputs [rows][h_q][d], with ``lse`` also the natural
-        log-normalisers [rows][h_q] fp32."""
+        log-normalisers [rows][h_q] fp32.  Captured into a graph: after ``reserve_chunks``."""
         self._check_chunk(chunk)
         with self._on_stream(stream, q, chunk.row_start):
             q = self._rows(q, self.hq)
@@ -347,14 +367,8 @@ class RetroLayer:
             out = torch.empty(chunk.n_rows, self.hq, self.d, dtype=self.dtype, device=self.device)
             z = torch.empty(chunk.n_rows, self.hq, dtype=torch.float32,
                             device=self.device) if lse else None
-            need = B.retro_chunk_workspace_size(self.dims, chunk.n_rows)
-            if self.chunk_ws is None or self.chunk_ws.numel() < need:
-                # for as many rows as the cache has tokens, so that a captured call's
-                # workspace is not replaced by a larger one
-                most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G)
-                need = max(need, B.retro_chunk_workspace_size(self.dims, most))
-                self.chunk_ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            ws = self._chunk_workspace()
             B.retro_chunk_attend(self.dims, self.cache, chunk.struct, q, self._stride(q, self.hq),
-                                 out, z, self.chunk_ws, self.chunk_ws.numel(), stream)
+                                 out, z, ws, ws.numel(), stream)
         self._keep_attend = (q, chunk)
         return (out, z) if lse else out

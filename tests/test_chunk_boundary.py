@@ -151,3 +151,27 @@ def test_decoder_refuses_prompts_between_the_steps_of_a_window(B):
         dec.prefill_chunk((1,), torch.zeros(1, 128))
     with pytest.raises(ValueError):   # a norm's weights of another length
         RetroDecoder([dict(w, q_norm=torch.ones(32))], window=0, **kw)
+
+
+def _small_layer(**kw):
+    from paper_2508_09001_amd.layer import RetroLayer
+    args = dict(batch=2, num_kv_heads=1, group=2, head_dim=64, page_size=16, budget=16, window=0, max_pages=2,
+                device="cpu")
+    args.update(kw)
+    return RetroLayer(**args)
+
+
+def test_workspace_is_not_made_inside_a_capture(B, monkeypatch):
+    """Its fill would only be recorded: an eager call before the first replay would count
+    parts from whatever the memory held."""
+    import torch
+    lay = _small_layer()
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="reserve_chunks"):
+        lay._chunk_workspace()
+    assert lay.chunk_ws is None
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    ws = lay._chunk_workspace()
+    assert (ws == 0).all() and ws.numel() == B.retro_chunk_workspace_size(lay.dims, 64)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    assert lay._chunk_workspace() is ws

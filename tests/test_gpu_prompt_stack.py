@@ -226,3 +226,31 @@ def test_layer_calls_on_another_stream_while_the_current_one_is_busy():
         same = [bool(torch.equal(a, b)) for a, b in zip(got, want)]
     assert same == [True] * 4
     torch.cuda.synchronize()
+
+
+def test_captured_layer_attention_between_eager_calls():
+    """A layer's attend_chunk captured after reserve_chunks: eager calls before the first
+    replay, between replays and of other shapes use the same workspace."""
+    from paper_2508_09001_amd.layer import RetroChunk, RetroLayer, RetroRotary
+    hk, G, d, P, mp, n = 2, 4, 128, 16, 96, 40
+    lay = RetroLayer(batch=1, num_kv_heads=hk, group=G, head_dim=d, page_size=P, budget=P, window=0, max_pages=mp)
+    k, v = (torch.randn(1400 + n, hk, d).bfloat16().cuda() for _ in range(2))
+    lay.append_chunk(0, lay.chunk((1400 + n,)), RetroRotary(mp * P, 0), k, v)
+    q = torch.randn(n, hk * G, d).bfloat16().cuda()
+    ch, one = RetroChunk((n,), (1400,), "cuda"), RetroChunk((1,), (1400,), "cuda")
+    fresh = RetroLayer(batch=1, num_kv_heads=hk, group=G, head_dim=d, page_size=P, budget=P, window=0, max_pages=mp)
+    for name in ("k_cache", "v_cache", "digest", "seq_lens", "last_loaded"):
+        getattr(fresh, name).copy_(getattr(lay, name))
+    want = [x.clone() for c in (ch, one) for x in fresh.attend_chunk(c, q[:c.n_rows], lse=True)]
+    lay.reserve_chunks()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, z = lay.attend_chunk(ch, q, lse=True)
+    for _ in range(3):
+        eager = [x for c in (ch, one) for x in lay.attend_chunk(c, q[:c.n_rows], lse=True)]
+        assert all(torch.equal(a, b) for a, b in zip(eager, want))
+        o.fill_(5.0)
+        z.fill_(5.0)
+        graph.replay()
+        assert torch.equal(o, want[0]) and torch.equal(z, want[1])
+        torch.cuda.synchronize()
