@@ -146,14 +146,15 @@ class RetroDecoder:
         one sequence's rows behind the other's.  Returns the residual stream after the
         last layer, [sum of rows][d_model] fp32.  Between decode steps too where W is 0;
         with W > 0 a step's window rows are the tokens of the steps before it, so that
-        prompts come before the first one (ValueError otherwise)."""
+        prompts come before the first one (ValueError otherwise, and for rows that a
+        sequence has no room for)."""
         if self.W and self.decoded:
             raise ValueError("with a window, prompts come before the first decode step")
         if emb.dim() != 2 or emb.shape[0] != sum(rows) or emb.shape[1] != self.d_model:
             raise ValueError("emb must be [sum of rows][d_model]")
-        if any(lay._lens != self.layers[0]._lens for lay in self.layers):
-            raise ValueError("the layers hold different numbers of tokens")
         chunk = self.layers[0].chunk(rows)
+        for lay in self.layers:  # before any of them has changed
+            lay.check_append(chunk)
         h = emb.to(device=self.device, dtype=torch.float32)
         for lay, w, rot in zip(self.layers, self.weights, self.rotary):
             x = h.to(self.dtype)

@@ -263,6 +263,15 @@ class RetroLayer:
         if chunk.n_rows > self.batch * self.dims.max_pages * self.P:
             raise ValueError("the chunk has more rows than the cache has tokens")
 
+    def check_append(self, chunk: RetroChunk) -> None:
+        """ValueError unless the chunk's rows are the next tokens and have room."""
+        self._check_chunk(chunk)
+        if chunk.start != self._lens:
+            raise ValueError("the chunk does not begin where the sequences end")
+        room = self.dims.max_pages * self.P
+        if any(n and at + n > room for n, at in zip(chunk.rows, chunk.start)):
+            raise ValueError(f"a sequence holds at most {room} tokens")
+
     def _rows(self, x, heads: int) -> torch.Tensor:
         """x [rows][heads][d] or [rows][heads * d] as it is where the library can read it
         (rows may be strided: parts of one projection's output), else copied."""
@@ -335,9 +344,7 @@ class RetroLayer:
         """Store the chunk's keys and values [rows][h_k][d], keys normalised and rotated on
         the way; returns the queries q [rows][h_q][d], treated likewise (None without q)."""
         self.check_rotary(rotary)
-        self._check_chunk(chunk)
-        if chunk.start != self._lens:
-            raise ValueError("the chunk does not begin where the sequences end")
+        self.check_append(chunk)
         with self._on_stream(stream, k, v, q, chunk.row_start):
             k, v = self._rows(k, self.hk), self._rows(v, self.hk)
             q = None if q is None else self._rows(q, self.hq)

@@ -175,3 +175,30 @@ def test_workspace_is_not_made_inside_a_capture(B, monkeypatch):
     assert (ws == 0).all() and ws.numel() == B.retro_chunk_workspace_size(lay.dims, 64)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
     assert lay._chunk_workspace() is ws
+
+
+@pytest.mark.parametrize("held,rows", [((0, 0), (33, 0)), ((0, 0), (0, 33)), ((32, 5), (1, 3)), ((20, 0), (13, 32))])
+def test_rows_that_a_sequence_has_no_room_for(B, held, rows):
+    """Room for 32 tokens each: refused before a layer changes, whatever the total."""
+    import torch
+    from paper_2508_09001_amd.decode import RetroDecoder
+    from paper_2508_09001_amd.layer import RetroRotary
+    lay = _small_layer()
+    lay._lens = list(held)
+    x = torch.zeros(sum(rows), 64)
+    with pytest.raises(ValueError, match="at most 32 tokens"):
+        lay.append_chunk(0, lay.chunk(rows), RetroRotary(32, 0, device="cpu"), x, x)
+    assert lay._lens == list(held)
+    lay._lens = [0, 32]
+    lay.check_append(lay.chunk((32, 0)))    # (up to the end, and none for a full one)
+    w = dict(wq=torch.zeros(128, 128), wk=torch.zeros(128, 64), wv=torch.zeros(128, 64), wo=torch.zeros(128, 128))
+    dec = RetroDecoder([w, w], batch=2, num_kv_heads=1, group=2, head_dim=64, page_size=16, budget=16, max_pages=2,
+                       window=0, device="cpu", library_projections=False)
+    for la in dec.layers:
+        la._lens = list(held)
+    with pytest.raises(ValueError, match="at most 32 tokens"):
+        dec.prefill_chunk(rows, torch.zeros(sum(rows), 128))
+    assert all(la._lens == list(held) for la in dec.layers)
+    dec.layers[1]._lens = [7, 0]            # layers that differ: before the first one changes
+    with pytest.raises(ValueError, match="where the sequences end"):
+        dec.prefill_chunk((0, 0), torch.zeros(0, 128))
