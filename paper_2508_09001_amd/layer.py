@@ -109,6 +109,9 @@ class RetroLayer:
         if page_table is None:
             page_table = torch.arange(batch * max_pages, dtype=torch.int32).view(batch, max_pages)
         self.page_table = page_table.to(device=dev, dtype=torch.int32).contiguous()
+        # version of the table with every page mapped, so that no row is dropped (None: not so)
+        full = bool(((page_table >= 0) & (page_table < num_phys_pages)).all())
+        self._full_table = self._table_version() if full else None
         self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=dev)
         self.last_loaded = torch.full((batch, hk, max_pages), -1, dtype=torch.int32, device=dev)
         self.selected = torch.full((batch, hk, self.k_max), -1, dtype=torch.int32, device=dev)
@@ -141,6 +144,13 @@ class RetroLayer:
                     reuse_interval=getattr(spec, "reuse_interval", 0))
         args.update(kw)
         return cls(**args)
+
+    def _table_version(self) -> Optional[int]:
+        return None if self.page_table.is_inference() else self.page_table._version
+
+    def _may_drop(self) -> bool:
+        """Whether the device may have dropped rows that ``_lens`` counts."""
+        return self._full_table is None or self._full_table != self._table_version()
 
     def _dev(self, x) -> torch.Tensor:
         if not isinstance(x, torch.Tensor):
@@ -263,9 +273,19 @@ class RetroLayer:
         if chunk.n_rows > self.batch * self.dims.max_pages * self.P:
             raise ValueError("the chunk has more rows than the cache has tokens")
 
+    def read_lens(self) -> None:
+        """Takes over the sequences' lengths from the device, which is waited for.  ``chunk``
+        does it where it has to; a program calls it after replays of captured calls, which
+        the layer does not see, or writes to the table past its tensor."""
+        if self.seq_lens.is_cuda:
+            torch.cuda.synchronize(self.seq_lens.device)
+        self._lens = self.seq_lens.tolist()
+
     def check_append(self, chunk: RetroChunk) -> None:
         """ValueError unless the chunk's rows are the next tokens and have room."""
         self._check_chunk(chunk)
+        if chunk.start != self._lens and self._may_drop():
+            self.read_lens()  # (rows may have been dropped here as in the chunk's layer)
         if chunk.start != self._lens:
             raise ValueError("the chunk does not begin where the sequences end")
         room = self.dims.max_pages * self.P
@@ -292,9 +312,13 @@ class RetroLayer:
         return x.stride(0) if x.shape[0] > 1 else heads * self.d
 
     def chunk(self, rows: Sequence[int]) -> RetroChunk:
-        """The next ``rows[b]`` tokens of every sequence b, behind what it holds."""
+        """The next ``rows[b]`` tokens of every sequence b, behind what it holds: as counted
+        by the calls of this layer, or where pages are or were not mapped (the device drops
+        rows there) as on the device, which is waited for."""
         if len(rows) != self.batch:
             raise ValueError("rows must hold one entry per sequence")
+        if self._may_drop():
+            self.read_lens()
         return RetroChunk(rows, self._lens, self.device)
 
     def _chunk_workspace(self) -> torch.Tensor:
@@ -342,7 +366,8 @@ class RetroLayer:
     def append_chunk(self, step: int, chunk: RetroChunk, rotary: RetroRotary, k, v, q=None,
                      stream=None) -> Optional[torch.Tensor]:
         """Store the chunk's keys and values [rows][h_k][d], keys normalised and rotated on
-        the way; returns the queries q [rows][h_q][d], treated likewise (None without q)."""
+        the way; returns the queries q [rows][h_q][d], treated likewise (None without q).
+        Rows of a page that is not mapped are dropped, with those behind them."""
         self.check_rotary(rotary)
         self.check_append(chunk)
         with self._on_stream(stream, k, v, q, chunk.row_start):

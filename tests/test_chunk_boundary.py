@@ -202,3 +202,26 @@ def test_rows_that_a_sequence_has_no_room_for(B, held, rows):
     dec.layers[1]._lens = [7, 0]            # layers that differ: before the first one changes
     with pytest.raises(ValueError, match="where the sequences end"):
         dec.prefill_chunk((0, 0), torch.zeros(0, 128))
+
+
+def test_chunks_begin_where_the_device_stopped(B):
+    """Rows of pages that are not mapped are dropped on the device: the next chunk begins
+    at its lengths, in every layer, not at what the calls counted."""
+    import torch
+    from paper_2508_09001_amd.layer import RetroChunk
+    table = torch.tensor([[0, -1], [2, 3]])
+    lays = [_small_layer(page_table=table), _small_layer(page_table=table), _small_layer(num_phys_pages=3),
+            _small_layer(), _small_layer()]
+    lays[3].page_table[0, 1] = 9
+    for lay in lays:
+        lay._lens = [20, 7]                           # (counted)
+        lay.seq_lens.copy_(torch.tensor([16, 7]))     # (stored)
+    for lay in lays[:4]:
+        assert lay.chunk((0, 1)).start == [16, 7]
+    lays[0]._lens = [20, 7]
+    lays[0].check_append(RetroChunk((0, 1), (16, 7), "cpu"))    # another layer's chunk
+    assert lays[4].chunk((0, 1)).start == [20, 7]     # every page mapped: as counted, nothing waited for
+    lays[4].read_lens()
+    assert lays[4].chunk((0, 1)).start == [16, 7]
+    with torch.inference_mode():
+        assert _small_layer().chunk((1, 1)).start == [0, 0]

@@ -254,3 +254,30 @@ def test_captured_layer_attention_between_eager_calls():
         graph.replay()
         assert torch.equal(o, want[0]) and torch.equal(z, want[1])
         torch.cuda.synchronize()
+
+
+def test_chunks_after_rows_that_were_dropped():
+    """A page that is not mapped ends a sequence's append; once it is, the next chunk goes
+    on from there, as in a layer that never had the gap."""
+    from paper_2508_09001_amd.layer import RetroLayer, RetroRotary
+    hk, G, d, P, mp = 2, 2, 64, 16, 4
+    pt = torch.arange(2 * mp).view(2, mp)
+    gap = pt.clone()
+    gap[0, 1] = -1
+    kw = dict(batch=2, num_kv_heads=hk, group=G, head_dim=d, page_size=P, budget=P, window=0, max_pages=mp)
+    lay, ref = RetroLayer(page_table=gap, **kw), RetroLayer(page_table=pt, **kw)
+    rot = RetroRotary(mp * P, d)
+    k, v = (torch.randn(2, 40, hk, d).bfloat16().cuda() for _ in range(2))
+
+    def call(la, frm, to):
+        ch = la.chunk([b - a for a, b in zip(frm, to)])
+        assert ch.start == list(frm)
+        la.append_chunk(0, ch, rot, *(torch.cat([x[0, frm[0]:to[0]], x[1, frm[1]:to[1]]]) for x in (k, v)))
+
+    call(lay, (0, 0), (20, 9))
+    assert lay.seq_lens.tolist() == [16, 9]
+    lay.page_table[0, 1] = 1
+    call(lay, (16, 9), (40, 30))
+    call(ref, (0, 0), (40, 30))
+    for name in ("k_cache", "v_cache", "digest", "seq_lens"):
+        assert torch.equal(getattr(lay, name), getattr(ref, name)), name
