@@ -258,18 +258,19 @@ class RetroLayer:
 
     def check_rotary(self, rotary: RetroRotary) -> None:
         """ValueError unless the norms' weights and the table are this layer's to read."""
+        device = self.seq_lens.device
         for w in (rotary.q_norm, rotary.k_norm):
             if w is not None and (tuple(w.shape) != (self.d,) or w.dtype != self.dtype or
-                                  w.device.type != self.device.type):
-                raise ValueError(f"norm weights must be [{self.d}] {self.dtype} on {self.device}")
-        if rotary.table is not None and rotary.table.device.type != self.device.type:
-            raise ValueError(f"the table must be on {self.device}")
+                                  w.device != device):
+                raise ValueError(f"norm weights must be [{self.d}] {self.dtype} on {device}")
+        if rotary.table is not None and rotary.table.device != device:
+            raise ValueError(f"the table must be on {device}")
 
     def _check_chunk(self, chunk: RetroChunk) -> None:
         if len(chunk.rows) != self.batch:
             raise ValueError("the chunk must hold one entry per sequence")
-        if chunk.row_start.device.type != self.device.type:
-            raise ValueError(f"the chunk must be on {self.device}")
+        if chunk.row_start.device != self.seq_lens.device:
+            raise ValueError(f"the chunk must be on {self.seq_lens.device}")
         if chunk.n_rows > self.batch * self.dims.max_pages * self.P:
             raise ValueError("the chunk has more rows than the cache has tokens")
 
@@ -319,7 +320,7 @@ class RetroLayer:
             raise ValueError("rows must hold one entry per sequence")
         if self._may_drop():
             self.read_lens()
-        return RetroChunk(rows, self._lens, self.device)
+        return RetroChunk(rows, self._lens, self.seq_lens.device)
 
     def _chunk_workspace(self) -> torch.Tensor:
         if self.chunk_ws is None:

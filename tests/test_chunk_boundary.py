@@ -225,3 +225,25 @@ def test_chunks_begin_where_the_device_stopped(B):
     assert lays[4].chunk((0, 1)).start == [16, 7]
     with torch.inference_mode():
         assert _small_layer().chunk((1, 1)).start == [0, 0]
+
+
+def test_tensors_of_another_gpu_are_refused(B):
+    """Of the same kind of device, but not the layer's: its kernels would read them there."""
+    import torch
+    from types import SimpleNamespace as NS
+    gpu = [torch.device("cuda", i) for i in (0, 1)]
+
+    def weights(dev):
+        return NS(shape=(64,), dtype=torch.bfloat16, device=dev)
+
+    lay = _small_layer()
+    lay.device, lay.seq_lens = torch.device("cuda"), NS(device=gpu[0])
+    lay.check_rotary(NS(q_norm=weights(gpu[0]), k_norm=weights(gpu[0]), table=NS(device=gpu[0])))
+    for kw in (dict(q_norm=weights(gpu[1])), dict(k_norm=weights(gpu[1])), dict(table=NS(device=gpu[1]))):
+        with pytest.raises(ValueError, match="cuda:0"):
+            lay.check_rotary(NS(**dict(dict(q_norm=None, k_norm=None, table=None), **kw)))
+    with pytest.raises(ValueError, match="cuda:0"):
+        lay._check_chunk(NS(rows=[1, 1], n_rows=2, row_start=NS(device=gpu[1])))
+    meta = _small_layer(device="meta")      # (a layer's own chunk: on its device, whichever is current)
+    meta.device = torch.device("cpu")
+    assert meta.chunk((1, 1)).row_start.device == meta.seq_lens.device
