@@ -328,8 +328,10 @@ class RetroLayer:
             # in front of the first one)
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("reserve_chunks comes before a captured attend_chunk")
-            # for as many rows as the cache has tokens: never replaced by a larger one
-            most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G)
+            # for as many rows as the tables have tokens, or the largest call: never replaced
+            # by a larger one
+            most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G,
+                       ((1 << 40) - 1) // (self.hq * self.d))
             self.chunk_ws = torch.zeros(B.retro_chunk_workspace_size(self.dims, most),
                                         dtype=torch.uint8, device=self.device)
         return self.chunk_ws

@@ -247,3 +247,14 @@ def test_tensors_of_another_gpu_are_refused(B):
     meta = _small_layer(device="meta")      # (a layer's own chunk: on its device, whichever is current)
     meta.device = torch.device("cpu")
     assert meta.chunk((1, 1)).row_start.device == meta.seq_lens.device
+
+
+@pytest.mark.parametrize("kw", [dict(batch=512, num_kv_heads=8, group=16, head_dim=128, max_pages=8192),
+                                dict(batch=1024, num_kv_heads=1, group=16, max_pages=16384),
+                                dict(batch=8191, num_kv_heads=8, group=4, head_dim=128, max_pages=2048)])
+def test_tables_of_more_tokens_than_a_call_has_rows(B, kw, monkeypatch):
+    """The workspace is for the largest call where the tables have room for more rows."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    lay = _small_layer(device="meta", num_phys_pages=4096, **kw)
+    assert lay._chunk_workspace().numel() >= B.retro_chunk_workspace_size(lay.dims, 100000)
