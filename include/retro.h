@@ -537,8 +537,8 @@ retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, 
  * makes its row NaN; a NaN or infinite value of a stored token can make every
  * row of its sequence and KV head in the same call NaN, also rows in front of it;
  * slots past seq_lens never count, whatever they hold.  Reads the cache only.
- * n_rows == 0 does nothing; n_rows * h_q * d >= 2^40 or n_rows * G >= 2^31 is
- * RETRO_EUNSUPPORTED. */
+ * n_rows == 0 does nothing; n_rows * h_q * d >= 2^40 or n_rows * G >= 2^31 - 256
+ * is RETRO_EUNSUPPORTED. */
 retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* cache,
                                 const retro_chunk* chunk, const void* q, int64_t q_stride,
                                 void* out, float* lse, void* workspace, size_t ws_bytes,

@@ -1358,7 +1358,9 @@ Bounds bounds(const Geometry& g, int n_rows) {
 }  // namespace
 
 bool chunk_attend_supported(const Geometry& g, int n_rows) {
-  return (int64_t)n_rows * g.hq * g.D < (int64_t)1 << 40 && (int64_t)n_rows * g.G < (int64_t)1 << 31;
+  // (row numbers of a tile go up to one tile of many rows past the last row)
+  return (int64_t)n_rows * g.hq * g.D < (int64_t)1 << 40 &&
+         (int64_t)n_rows * g.G < ((int64_t)1 << 31) - kRowsMany;
 }
 
 size_t chunk_workspace(const Geometry& g, int n_rows) {

@@ -330,7 +330,7 @@ class RetroLayer:
                 raise RuntimeError("reserve_chunks comes before a captured attend_chunk")
             # for as many rows as the tables have tokens, or the largest call: never replaced
             # by a larger one
-            most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 1) // self.G,
+            most = min(self.batch * self.dims.max_pages * self.P, ((1 << 31) - 257) // self.G,
                        ((1 << 40) - 1) // (self.hq * self.d))
             self.chunk_ws = torch.zeros(B.retro_chunk_workspace_size(self.dims, most),
                                         dtype=torch.uint8, device=self.device)

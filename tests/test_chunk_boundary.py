@@ -258,3 +258,19 @@ def test_tables_of_more_tokens_than_a_call_has_rows(B, kw, monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     lay = _small_layer(device="meta", num_phys_pages=4096, **kw)
     assert lay._chunk_workspace().numel() >= B.retro_chunk_workspace_size(lay.dims, 100000)
+
+
+@pytest.mark.parametrize("G", [1, 7, 16])
+def test_rows_whose_numbers_pass_32_bits(B, G):
+    """Numbers of a tile's rows go up to 255 past the last row, and stay below 2^31."""
+    lib, n = B.load_library(), C.c_size_t(0)
+    d = _dims(B, batch=1, num_kv_heads=1, group=G, head_dim=64)
+    full = B.KVCache(*[A] * 6)
+    most = ((1 << 31) - 257) // G
+    assert lib.retro_chunk_workspace_size(C.byref(d), most, C.byref(n)) == OK
+    assert most * G - 1 + 256 < 1 << 31
+    for rows in (most + 1, ((1 << 31) - 1) // G):
+        assert lib.retro_chunk_workspace_size(C.byref(d), rows, C.byref(n)) == UNSUPPORTED
+        ch = B.Chunk(A + 64, A + 128, rows)
+        assert lib.retro_chunk_attend(C.byref(d), C.byref(full), C.byref(ch), A, G * 64, A, None, A, 1 << 40,
+                                      None) == UNSUPPORTED
