@@ -491,8 +491,9 @@ retro_status retro_rotary_table(float* table, int32_t positions, int32_t rot_dim
  * (then its output is not looked at).  q_out may be q, and k_out k, where their
  * strides are h_q * d and h_k * d.  A row of negative position is not written; the
  * rotated elements of one at or past rotary->positions become NaN.  positions may
- * be NULL where rot_dim is 0.  rows == 0 does nothing.  E.g. for the window rows
- * of a step: rotated queries for retro_step, rotated keys for retro_update_kv. */
+ * be NULL where rot_dim is 0.  rows == 0 does nothing; rows >= 2^31 - 4 is
+ * RETRO_EUNSUPPORTED.  E.g. for the window rows of a step: rotated queries for
+ * retro_step, rotated keys for retro_update_kv. */
 retro_status retro_rotate_qk(const retro_dims* dims, const retro_rotary* rotary,
                              const int32_t* positions, int32_t rows, const void* q,
                              int64_t q_stride, const void* k, int64_t k_stride, void* q_out,

@@ -421,7 +421,8 @@ hipError_t launch_rotary_table(float* table, int positions, int rot_dim, double 
 }
 
 bool rotate_qk_supported(const Geometry& g, int rows, bool q, bool k) {
-  return rotate_blocks(g, rows, q, k) < (int64_t)1 << 31;
+  // (the last workgroup's wavefronts go up to three rows past the last one)
+  return rotate_blocks(g, rows, q, k) < (int64_t)1 << 31 && rows < 0x7fffffff - 3;
 }
 
 hipError_t launch_rotate_qk(const Geometry& g, const retro_rotary& r, const int32_t* positions,

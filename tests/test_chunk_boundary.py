@@ -274,3 +274,11 @@ def test_rows_whose_numbers_pass_32_bits(B, G):
         ch = B.Chunk(A + 64, A + 128, rows)
         assert lib.retro_chunk_attend(C.byref(d), C.byref(full), C.byref(ch), A, G * 64, A, None, A, 1 << 40,
                                       None) == UNSUPPORTED
+
+
+def test_rotated_rows_whose_numbers_pass_32_bits(B):
+    """A wavefront's row goes up to three past the last one, and stays below 2^31."""
+    lib, r = B.load_library(), _rotary(B, rot_dim=64)
+    d = _dims(B, batch=1, num_kv_heads=1, group=1, head_dim=64)
+    for rows in ((1 << 31) - 4, (1 << 31) - 1):
+        assert lib.retro_rotate_qk(C.byref(d), C.byref(r), A, rows, None, 0, A, 64, None, A, None) == UNSUPPORTED
