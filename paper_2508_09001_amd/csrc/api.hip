@@ -589,7 +589,7 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
   if (!cache_ok(cache) || !chunk_ok(cache, chunk)) return RETRO_EINVAL;
   if (chunk->n_rows == 0) return RETRO_OK;
   if (!rows_ok(g, q, q_stride, g.hq) || !rows_ok(g, out, (int64_t)g.hq * g.D, g.hq) ||
-      !aligned16({cache->k_cache, cache->v_cache}))
+      (q == out && q_stride != (int64_t)g.hq * g.D) || !aligned16({cache->k_cache, cache->v_cache}))
     return RETRO_EINVAL;
   if (!retro::chunk_attend_supported(g, chunk->n_rows)) return RETRO_EUNSUPPORTED;
   if (!workspace || !aligned16({workspace}) || ws_bytes < retro::chunk_workspace(g, chunk->n_rows))

@@ -282,3 +282,13 @@ def test_rotated_rows_whose_numbers_pass_32_bits(B):
     d = _dims(B, batch=1, num_kv_heads=1, group=1, head_dim=64)
     for rows in ((1 << 31) - 4, (1 << 31) - 1):
         assert lib.retro_rotate_qk(C.byref(d), C.byref(r), A, rows, None, 0, A, 64, None, A, None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_attention_in_place_of_strided_queries(B, dtype):
+    """Outputs are contiguous: those of one row would lie in another's queries, unread yet."""
+    lib, d = B.load_library(), _dims(B, dtype=dtype)
+    cache, ch = B.KVCache(*[A] * 6), B.Chunk(A + 64, A + 128, 5)
+    assert lib.retro_chunk_attend(C.byref(d), C.byref(cache), C.byref(ch), A, 6144, A, None, None, 0, None) == INVALID
+    # (contiguous queries in place: on to the workspace)
+    assert lib.retro_chunk_attend(C.byref(d), C.byref(cache), C.byref(ch), A, 4096, A, None, None, 0, None) == WORKSPACE
