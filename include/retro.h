@@ -509,9 +509,8 @@ retro_status retro_rotate_qk(const retro_dims* dims, const retro_rotary* rotary,
  * initial -1).  The first row whose page is not mapped is dropped with every
  * later row of its sequence (slots past the new seq_lens, and digests and last_loaded of
  * pages past it, are then unspecified).  Queries are written for dropped rows
- * too (NaN past rotary->positions); q_out may be q where q_stride is h_q * d.  With
- * rot_dim > 0, rotary->positions must be at least max_pages * P (RETRO_EINVAL).
- * n_rows == 0 does nothing. */
+ * too (NaN past rotary->positions); q_out may be q where q_stride is h_q * d.  With rot_dim > 0, rotary->positions must be
+ * at least max_pages * P (RETRO_EINVAL).  n_rows == 0 does nothing. */
 retro_status retro_append_kv_rotary(const retro_dims* dims, int32_t step,
                                     const retro_kv_cache* cache, const retro_chunk* chunk,
                                     const retro_rotary* rotary, const void* q, int64_t q_stride,
@@ -530,8 +529,8 @@ retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, 
  *   out = sum_i softmax_i(sm_scale q . k_i) v_i,  lse = ln sum_i exp(sm_scale q . k_i)
  * out [n_rows][h_q][d] dtype, lse [n_rows][h_q] fp32 (may be NULL); out may be q where
  * q_stride is h_q * d (RETRO_EINVAL otherwise).  A row that no token is left for gives
- * (0, -inf).  The chunk's own keys and values are stored first
- * (retro_append_kv_rotary, retro_prefill_kv, retro_append_kv_tokens); one row per
+ * (0, -inf).  The chunk's own keys and values are stored
+ * first (retro_append_kv_rotary, retro_prefill_kv, retro_append_kv_tokens); one row per
  * sequence is dense decoding.  Tokens of pages that are not mapped are left out.
  * Products and sums in fp32; for bf16 the softmax weights are rounded to bf16 for
  * their product with the values, where a sequence has few rows as two bf16 halves

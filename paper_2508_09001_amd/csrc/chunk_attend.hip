@@ -405,12 +405,12 @@ __device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, u
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2 nt"
                  :
                  : "s"(to), "v"(offset), "s"(base)
-                 : "m0", "memory");
+                 : "memory");
   else
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2"
                  :
                  : "s"(to), "v"(offset), "s"(base)
-                 : "m0", "memory");
+                 : "memory");
 }
 // until at most N of the wavefront's loads and copies are in flight
 template <int N>
