@@ -472,11 +472,16 @@ typedef struct retro_rotary {
  * A sequence with start_pos[b] < 0 takes no part.  Rows that belong to no
  * sequence (in front of row_start[0], at or behind row_start[batch]) are not read
  * and their outputs stay as they were, so that a captured call can be replayed
- * for fewer rows.  n_rows: rows that the buffers hold; what reaches past it is cut. */
+ * for fewer rows.  n_rows: rows that the buffers hold; what reaches past it is cut.
+ * longest only helps retro_chunk_attend choose between two kernels that both take any
+ * lengths: results are right whatever it says, but where it is unknown every sequence is
+ * taken to have a row, and a chunk of a few hundred rows beside as many empty ranges may
+ * take twice as long. */
 typedef struct retro_chunk {
   const int32_t* row_start;  /* [batch + 1] */
   const int32_t* start_pos;  /* [batch]; not the cache's seq_lens array */
   int32_t n_rows;
+  int32_t longest;           /* most rows of a sequence, where the host knows; 0: unknown */
 } retro_chunk;
 
 /* Fills table [positions][rot_dim / 2][2] fp32 with cosine and sine of

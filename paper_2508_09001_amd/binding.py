@@ -66,7 +66,8 @@ class Rotary(C.Structure):
 
 
 class Chunk(C.Structure):
-    _fields_ = [("row_start", C.c_void_p), ("start_pos", C.c_void_p), ("n_rows", C.c_int32)]
+    _fields_ = [("row_start", C.c_void_p), ("start_pos", C.c_void_p), ("n_rows", C.c_int32),
+                ("longest", C.c_int32)]
 
 
 _lib = None

@@ -1370,6 +1370,23 @@ size_t chunk_workspace(const Geometry& g, int n_rows) {
   return kCounterBytes + ((floats * sizeof(float) + 255) & ~size_t(255));
 }
 
+namespace {
+
+// Whether the call gets the kernel that also takes tiles of many rows, which costs a
+// call without them 3 us and 5 to 18 % (a token each of 33 to 512 sequences at 60 to 8000
+// tokens).  The device knows the lengths; the host may know the longest one: up to 32 rows
+// there are no such tiles, and above 128 they are worth having (a chunk beside empty ranges,
+// us without and with them: 280 rows of 256 sequences at 4000 96 and 57, 540 of 512 at 4000
+// 146 and 69, at 0 52 and 31; 64 of 64 at 4000 34 and 37).  In between, and where it is
+// unknown, every sequence is taken to have a row, which bounds the longest.
+bool may_have_many(const retro_chunk& ch, int batch, int G) {
+  const int64_t longest = (int64_t)std::min(ch.longest, ch.n_rows) * G;
+  if (longest > 4 * kRowsFew) return true;
+  return ((int64_t)ch.n_rows - batch + 1) * G > 4 * kRowsFew && (longest == 0 || longest > kRowsFew);
+}
+
+}  // namespace
+
 hipError_t launch_chunk_attend(const Geometry& g, const retro_kv_cache& c, const retro_chunk& ch,
                                const void* q, int64_t q_stride, void* out, float* lse, void* ws,
                                hipStream_t s) {
@@ -1393,10 +1410,7 @@ hipError_t launch_chunk_attend(const Geometry& g, const retro_kv_cache& c, const
                      g.max_pages,
                      g.num_phys,
                      g.sm_scale};
-  // The host does not know the lengths.  Where every sequence has a row, one can have
-  // no more than this many: few enough for tiles of 32 rows only.  (Where most have none
-  // after all, a long chunk of a few rows more than that takes longer, no worse.)
-  const bool many = g.dtype == RETRO_BF16 && ((int64_t)ch.n_rows - g.batch + 1) * g.G > 4 * kRowsFew;
+  const bool many = g.dtype == RETRO_BF16 && may_have_many(ch, g.batch, g.G);
   auto go = [&](auto t, auto d, auto ps) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value, P = decltype(ps)::value;

@@ -70,7 +70,8 @@ class RetroChunk:
         self.n_rows = at[-1]
         both = torch.tensor(at + self.start, dtype=torch.int32).to(device)
         self.row_start, self.start_pos = both[:len(at)], both[len(at):]
-        self.struct = B.Chunk(self.row_start.data_ptr(), self.start_pos.data_ptr(), self.n_rows)
+        self.struct = B.Chunk(self.row_start.data_ptr(), self.start_pos.data_ptr(), self.n_rows,
+                              max(self.rows, default=0))
 
 
 def _on(device: torch.device):
