@@ -243,3 +243,54 @@ def test_captured_append_replayed_for_other_rows():
         assert torch.equal(qo[:sum(ns)], qr[:sum(ns)])
         for name in ("k_cache", "v_cache", "digest", "seq_lens", "last_loaded"):
             assert torch.equal(getattr(lay, name), getattr(ref, name)), name
+
+
+# more than 16384 times 64 / (lanes of a vector) heads: five groups of heads a wavefront,
+# the last of a row not full, queries and keys in one group, keys alone (of 20 places 5 or 9)
+@pytest.mark.parametrize("dtype,d,rot,interleaved,rows,hk,G,which", [
+    ("bf16", 128, 128, 0, 3001, 5, 4, "qk"), ("bf16", 128, 48, 1, 3001, 5, 4, "qk"),
+    ("f32", 128, 128, 0, 1501, 5, 4, "qk"), ("f32", 64, 64, 1, 2601, 5, 4, "qk"),
+    ("bf16", 64, 32, 0, 4501, 5, 4, "qk"), ("bf16", 128, 128, 0, 9001, 5, 4, "k"),
+    ("bf16", 128, 64, 0, 6001, 1, 8, "qk"), ("bf16", 128, 128, 1, 4201, 5, 4, "q"), ("f32", 128, 0, 0, 6001, 5, 1, "k")])
+def test_rotate_many_rows(dtype, d, rot, interleaved, rows, hk, G, which):
+    from paper_2508_09001_amd import binding as B
+    g = torch.Generator().manual_seed(rows)
+    hq, n = hk * G, 700
+    qkv = torch.randn(rows, (hq + 2 * hk) * d, generator=g).to(TD[dtype]).cuda()
+    pos = torch.randint(0, n, (rows,), generator=g, dtype=torch.int32)
+    pos[[1, rows - 1]] = -1          # not written
+    pos[[2, rows - 2]] = n           # past the table
+    live, past = pos >= 0, pos >= n
+    w = [(1 + 0.2 * torch.randn(d, generator=g)).to(TD[dtype]) for _ in range(2)]
+    wd, tab = [x.cuda() for x in w], R.table(n, rot, 1e4)
+    tab_d = torch.from_numpy(tab).cuda() if rot else None
+    r = B.Rotary(tab_d.data_ptr() if rot else None, n if rot else 0, rot, interleaved, 1e-6, *(x.data_ptr() for x in wd))
+    dims, posd, calls = _dims(B, dtype, d, hk, G), pos.cuda(), {}
+    for name, at, heads in (("q", 0, hq), ("k", hq * d, hk)):
+        if name in which:
+            x = qkv[:, at:at + heads * d]
+            calls[name] = (x, torch.full((rows + 1, heads, d), 5.0).to(TD[dtype]).cuda(), heads)
+
+    def call(src, stride, dst):
+        def arg(f, none):
+            return [f(i) if i in calls else none for i in ("q", "k")]
+        (q, k), (qs, ks), (qo, ko) = arg(src, None), arg(stride, 0), arg(dst, None)
+        B.retro_rotate_qk(dims, r, posd, rows, q, qs, k, ks, qo, ko)
+        torch.cuda.synchronize()
+
+    print(f"[rotate] {dtype} d={d} rot={rot} il={interleaved} rows={rows} hk={hk} G={G} {which}", flush=True)
+    call(lambda i: calls[i][0], lambda i: calls[i][0].stride(0), lambda i: calls[i][1])
+    own = {i: x.contiguous().clone() for i, (x, _, _) in calls.items()}
+    call(lambda i: own[i], lambda i: calls[i][2] * d, lambda i: own[i])      # in place
+    ok = live & ~past if rot else live
+    for (name, (x, o, heads)), weight in zip(calls.items(), [w["qk".index(i)] for i in calls]):
+        want, tol = R.turn(_f64(x[ok.cuda()].reshape(-1, heads, d)), _f64(weight), tab, pos[ok].numpy(), rot,
+                           interleaved, 1e-6, dtype)
+        _within(o[:rows][ok.cuda()], want, tol, name)
+        assert (o[rows] == 5.0).all() and (o[:rows][~live.cuda()] == 5.0).all()
+        if rot:
+            assert o[:rows][past.cuda()][..., :rot].isnan().all()
+            assert o[:rows][past.cuda()][..., rot:].isfinite().all()
+        same = own[name].view(rows, heads, d)
+        assert torch.equal(same[ok.cuda()], o[:rows][ok.cuda()])
+        assert torch.equal(same[~live.cuda()], x.reshape(rows, heads, d)[~live.cuda()])
