@@ -317,3 +317,26 @@ def test_results_do_not_depend_on_the_longest_run_given(seqs, longest):
     b = Batch("bf16", 2, 4, 128, 16, seqs, seed=21)
     b.chunk.longest = longest
     b.run().check()
+
+
+# more tiles of 256 rows than workgroups (387, 296 and 404): those of the second round are dealt
+# backwards, cut or not
+@pytest.mark.parametrize("seqs,hk,G,d,P", [([(1040, 0), (500, 300)], 9, 7, 64, 32),
+                                           ([(1100, 0), (60, 9000)], 8, 8, 128, 16),
+                                           ([(900, 200), (700, 0), (1, 3000)], 4, 16, 128, 32)], ids=["0", "1", "2"])
+def test_more_tiles_of_many_rows_than_workgroups(seqs, hk, G, d, P):
+    Batch("bf16", hk, G, d, P, seqs, seed=22).run().check()
+
+
+# a tile or a few of 256 rows under long contexts: some 160, 88, 26 and 59 parts each
+@pytest.mark.parametrize("seqs,hk,G,d,P", [([(64, 82000)], 1, 4, 64, 16), ([(64, 44800)], 2, 4, 128, 16),
+                                           ([(60, 12800)], 4, 8, 128, 32),
+                                           ([(70, 6000), (64, 30000), (1, 900)], 2, 4, 64, 32)], ids=["0", "1", "2", "3"])
+def test_tiles_of_many_rows_in_many_parts(seqs, hk, G, d, P):
+    b = Batch("bf16", hk, G, d, P, seqs, seed=23).run()
+    b.check()
+    out, z = b.out.clone(), b.lse.clone()
+    for _ in range(3):   # (the counts are back at zero)
+        b.out.fill_(5.0)
+        b.run()
+        assert torch.equal(b.out, out) and torch.equal(b.lse, z)
