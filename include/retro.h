@@ -538,8 +538,10 @@ retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, 
  * first (retro_append_kv_rotary, retro_prefill_kv, retro_append_kv_tokens); one row per
  * sequence is dense decoding.  Tokens of pages that are not mapped are left out.
  * Products and sums in fp32; for bf16 the softmax weights are rounded to bf16 for
- * their product with the values, where a sequence has few rows as two bf16 halves
- * (sums and log-normalisers take the unrounded ones).
+ * their product with the values (2^-8 of a weight at most), where a sequence has few
+ * rows as two bf16 halves (sums and log-normalisers take the unrounded ones).  Which of
+ * the two a sequence of more than 32 / G rows gets, and the order of its sums, depend on
+ * the call's other sequences too; the same call gives the same bits.
  * NaN and infinities as in retro_decode_attend: a NaN score, or one of +inf,
  * makes its row NaN; a NaN or infinite value of a stored token can make every
  * row of its sequence and KV head in the same call NaN, also rows in front of it;

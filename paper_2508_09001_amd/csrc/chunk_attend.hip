@@ -25,7 +25,7 @@
 //
 // Measured (bf16, 8 KV heads of 4 query heads of 128; several cards): a prompt of 8192
 // tokens 483 to 546 us (1.01 to 1.14 PFLOP/s), 1024 rows at 131K 1.82 to 2.03 ms (1.08 to
-// 1.20), where a product of 16384^3 reaches 1.37: the matrix units are busy 64 % of the cycles at 1.75
+// 1.20), where a product of 16384^3 reaches 1.33 to 1.37: the matrix units are busy 64 % of the cycles at 1.75
 // GHz, which is where such products hold the clock too, and leaving out any one part
 // of the loop (exponentials, LDS reads, copies, maxima, sums) gains 4 to 9 %.  16 tokens
 // at 8K to 32K, 1.15 GB: 187 us, 6.15 TB/s, the rate of a plain read.  Short calls wait for
@@ -633,6 +633,9 @@ struct Rows {
   // (fp32, with four times as many and each four times as long, would wait for them:
   // 1024 rows at 1024, d 128, 370 -> 328 us without).
   // SPLIT: a bf16 weight is given as two, what the first one's rounding leaves and it.
+  // Tiles of many rows, bound by the matrix units, take the rounded one alone: with
+  // both 8192 rows 502 -> 690 us and 1024 at 131K 1857 -> 2593, for outputs of 2000 rows
+  // 1.9e-4 -> 1.5e-4 off 64 bits (root mean squares; of the outputs 0.09).
   template <bool SPLIT>
   __device__ __forceinline__ void values(int at, const f32x16& p, int stored, uint32_t bad) {
     constexpr int STEPS = 32 / (2 * S::E);  // key pieces of a lane half
@@ -695,6 +698,29 @@ __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d)
 __device__ __forceinline__ float natural_lse(float m, float l, float scale) {
   return l == 0.f ? -INFINITY : __builtin_fmaf(m, scale, __builtin_amdgcn_logf(l) * kLn2);
 }
+
+// A sequence's pages: page i's number if it is mapped, else page 0 (never counted).
+struct Pages {
+  const int32_t* table;
+  int last, num_phys;
+  __device__ __forceinline__ int operator()(int i, bool& bad) const {
+    const int id = sload(table + min(i, last));
+    bad = id < 0 || id >= num_phys;
+    return bad ? 0 : id;
+  }
+  // pages without a mapping among n (those past the end are cut by lengths)
+  template <int N>
+  __device__ __forceinline__ uint32_t bad(int page0) const {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      bool b;
+      (*this)(page0 + i, b);
+      bits |= (uint32_t)b << i;
+    }
+    return bits;
+  }
+};
 
 // ---- parts -------------------------------------------------------------------------------
 
@@ -836,29 +862,6 @@ __device__ __forceinline__ void join_few(JoinLds& L, int R, int parts, float c, 
     if (grp == 0 && row < R) done(row, L.m[row], L.sum[row], d, o[i]);
   }
 }
-
-// a sequence's pages: page i's number if it is mapped, else page 0 (never counted)
-  struct Pages {
-    const int32_t* table;
-    int last, num_phys;
-    __device__ __forceinline__ int operator()(int i, bool& bad) const {
-      const int id = sload(table + min(i, last));
-      bad = id < 0 || id >= num_phys;
-      return bad ? 0 : id;
-    }
-    // pages without a mapping among n (those past the end are cut by lengths)
-    template <int N>
-    __device__ __forceinline__ uint32_t bad(int page0) const {
-      uint32_t bits = 0;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        bool b;
-        (*this)(page0 + i, b);
-        bits |= (uint32_t)b << i;
-      }
-      return bits;
-    }
-  };
 
 // The same for up to 256 rows: a slot is read by all threads at once, 16 bytes of up
 // to 16 rows each (D 128), which keeps 128 KB on the way.  (Row after row, eight parts
