@@ -68,6 +68,7 @@ class RetroChunk:
         for n in self.rows:
             at.append(at[-1] + n)
         self.n_rows = at[-1]
+        self.reach = max((p + n for n, p in zip(self.rows, self.start) if n), default=0)
         both = torch.tensor(at + self.start, dtype=torch.int32).to(device)
         self.row_start, self.start_pos = both[:len(at)], both[len(at):]
         self.struct = B.Chunk(self.row_start.data_ptr(), self.start_pos.data_ptr(), self.n_rows,
@@ -291,7 +292,7 @@ class RetroLayer:
         if chunk.start != self._lens:
             raise ValueError("the chunk does not begin where the sequences end")
         room = self.dims.max_pages * self.P
-        if any(n and at + n > room for n, at in zip(chunk.rows, chunk.start)):
+        if chunk.reach > room:
             raise ValueError(f"a sequence holds at most {room} tokens")
 
     def _rows(self, x, heads: int) -> torch.Tensor:
