@@ -340,3 +340,21 @@ def test_tiles_of_many_rows_in_many_parts(seqs, hk, G, d, P):
         b.out.fill_(5.0)
         b.run()
         assert torch.equal(b.out, out) and torch.equal(b.lse, z)
+
+
+def test_two_calls_at_once():
+    """On two streams, a workspace each: neither waits for the other nor changes its result."""
+    a, b = (Batch("bf16", hk, 4, 128, 16, seqs, seed=24) for hk, seqs in
+            ((8, [(500, 1500), (1, 2000)]), (2, [(1, 30000), (100, 700)])))
+    want = [(x.run().out.clone(), x.lse.clone()) for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for x in (a, b):
+        x.out.fill_(5.0)
+        x.lse.fill_(5.0)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, s in zip((a, b), streams):
+            x.B.retro_chunk_attend(x.dims, x.cache, x.chunk, x.q, x.q.stride(0), x.out, x.lse, x.ws, x.ws_bytes, stream=s)
+    torch.cuda.synchronize()
+    for x, (o, z) in zip((a, b), want):
+        assert torch.equal(x.out, o) and torch.equal(x.lse, z)

@@ -294,3 +294,18 @@ def test_rotate_many_rows(dtype, d, rot, interleaved, rows, hk, G, which):
         same = own[name].view(rows, heads, d)
         assert torch.equal(same[ok.cuda()], o[:rows][ok.cuda()])
         assert torch.equal(same[~live.cuda()], x.reshape(rows, heads, d)[~live.cuda()])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norms_alone_need_no_positions(dtype):
+    from paper_2508_09001_amd import binding as B
+    rows, hk, G, d = 9, 2, 3, 128
+    g = torch.Generator().manual_seed(6)
+    q, k = (torch.randn(rows, h, d, generator=g).to(TD[dtype]).cuda() for h in (hk * G, hk))
+    w = (1 + 0.2 * torch.randn(d, generator=g)).to(TD[dtype]).cuda()
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    B.retro_rotate_qk(_dims(B, dtype, d, hk, G), B.Rotary(None, 0, 0, 0, 1e-6, None, w.data_ptr()), None, rows,
+                      q, hk * G * d, k, hk * d, qo, ko)
+    assert torch.equal(qo, q)
+    want, tol = R.turn(_f64(k), _f64(w), None, None, 0, 0, 1e-6, dtype)
+    _within(ko, want, tol, "k")
