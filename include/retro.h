@@ -481,7 +481,7 @@ typedef struct retro_chunk {
   const int32_t* row_start;  /* [batch + 1] */
   const int32_t* start_pos;  /* [batch]; not the cache's seq_lens array */
   int32_t n_rows;
-  int32_t longest;           /* most rows of a sequence, where the host knows; 0: unknown */
+  int32_t longest;           /* most rows of a sequence, where the host knows; <= 0: unknown */
 } retro_chunk;
 
 /* Fills table [positions][rot_dim / 2][2] fp32 with cosine and sine of

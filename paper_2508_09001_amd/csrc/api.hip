@@ -511,8 +511,7 @@ bool rotary_ok(const Geometry& g, const retro_rotary* r) {
 }
 
 bool chunk_ok(const retro_kv_cache* cache, const retro_chunk* c) {
-  return c && c->row_start && c->start_pos && c->n_rows >= 0 && c->longest >= 0 &&
-         c->start_pos != cache->seq_lens;
+  return c && c->row_start && c->start_pos && c->n_rows >= 0 && c->start_pos != cache->seq_lens;
 }
 
 }  // namespace

@@ -1385,7 +1385,7 @@ namespace {
 bool may_have_many(const retro_chunk& ch, int batch, int G) {
   const int64_t longest = (int64_t)std::min(ch.longest, ch.n_rows) * G;
   if (longest > 4 * kRowsFew) return true;
-  return ((int64_t)ch.n_rows - batch + 1) * G > 4 * kRowsFew && (longest == 0 || longest > kRowsFew);
+  return ((int64_t)ch.n_rows - batch + 1) * G > 4 * kRowsFew && (longest <= 0 || longest > kRowsFew);
 }
 
 }  // namespace

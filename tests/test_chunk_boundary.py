@@ -300,9 +300,3 @@ def test_longest_run_of_a_chunk(B):
     assert RetroChunk([0] * 300 + [540, 1], [0] * 302, "cpu").struct.longest == 540
     assert RetroChunk([], [], "cpu").struct.longest == 0
     assert B.Chunk(A, A, 5).longest == 0        # unknown
-    lib, d = B.load_library(), _dims(B)
-    cache, ch = B.KVCache(*[A] * 6), B.Chunk(A + 64, A + 128, 5, -1)
-    assert lib.retro_chunk_attend(C.byref(d), C.byref(cache), C.byref(ch), A, 4096, A, None, A, 1 << 40,
-                                  None) == INVALID
-    assert lib.retro_append_kv_rotary(C.byref(d), 0, C.byref(cache), C.byref(ch), C.byref(_rotary(B)), A, 4096,
-                                      A, 1024, A, 1024, A, None) == INVALID

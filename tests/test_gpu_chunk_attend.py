@@ -310,7 +310,7 @@ def test_chunks_beside_tokens(chunks, tokens, ctx, hk, G, d, P):
 
 # one chunk in a table of slots of which the others are empty, short chunks in all of them,
 # and both: the kernel goes by the longest run, the results by none
-@pytest.mark.parametrize("longest", [0, 1, 7, 40, 300, 2**31 - 1])
+@pytest.mark.parametrize("longest", [-5, 0, 1, 7, 40, 300, 2**31 - 1])
 @pytest.mark.parametrize("seqs", [[(300, 500)] + [(0, 40)] * 299, [(7, 100)] * 60, [(40, 2500), (1, 9)] + [(0, 0)] * 60],
                          ids=["slots", "short", "mixed"])
 def test_results_do_not_depend_on_the_longest_run_given(seqs, longest):
