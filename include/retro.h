@@ -476,7 +476,7 @@ typedef struct retro_rotary {
  * longest only helps retro_chunk_attend choose between two kernels that both take any
  * lengths: results are right whatever it says, but where it is unknown every sequence is
  * taken to have a row, and a chunk of a few hundred rows beside as many empty ranges may
- * take twice as long. */
+ * take two to three times as long. */
 typedef struct retro_chunk {
   const int32_t* row_start;  /* [batch + 1] */
   const int32_t* start_pos;  /* [batch]; not the cache's seq_lens array */
