@@ -61,8 +61,8 @@ typedef enum {
 typedef enum { RETRO_F32 = 0, RETRO_BF16 = 1 } retro_dtype;
 
 /* Bits of retro_dims.flags.  0 lets retro_step choose its launches (the normal
- * case); the other bits select a launch sequence explicitly or test the failure
- * path, with the same results. */
+ * case); RETRO_FLAG_KV_MX4 says how the cache is held; the other bits select a launch
+ * sequence explicitly or test the failure path, with the same results. */
 typedef enum {
   /* retro_step: the page scores take a launch of their own even where the
    * scores, selection and attention fit in one launch */
@@ -72,7 +72,9 @@ typedef enum {
   RETRO_FLAG_SELECT_IN_SCORES = 2,
   /* tests of the failure path only: every bounded wait between the workgroups
    * of a launch gives up after a few polls, as if its producers never came */
-  RETRO_FLAG_TEST_WAIT_TIMEOUT = 4
+  RETRO_FLAG_TEST_WAIT_TIMEOUT = 4,
+  /* the cache's keys and values are held in 4 bits (see "The cache in 4 bits" below) */
+  RETRO_FLAG_KV_MX4 = 16
 } retro_flag;
 
 /* Problem statement of one layer.  Supported: head_dim 64 or 128; page_size
@@ -552,6 +554,39 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
                                 const retro_chunk* chunk, const void* q, int64_t q_stride,
                                 void* out, float* lse, void* workspace, size_t ws_bytes,
                                 void* stream);
+
+/* ---- The cache in 4 bits ---------------------------------------------------------
+ * With RETRO_FLAG_KV_MX4 in dims->flags a cache's keys and values are held in 4.25 bits
+ * an element (the elements and scales of the OCP Microscaling Formats specification's
+ * MXFP4), for 3.8 times the tokens in the same memory and as much less to read.  A head's vector is cut into blocks of 32 elements.
+ * A block has one exponent byte e and 32 codes: a sign bit and the magnitudes 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 in the order of the other three bits; an element stands for its code's
+ * value times 2^(e - 127), which is exact in bf16.  Storing an element x of dtype (a key
+ * as the other format would hold it, normalised, rotated and rounded):
+ *   with m the largest magnitude of the block and 2^f <= m < 2^(f + 1),
+ *   e = 127 + f - 2 for m < 1.75 * 2^f, one more from there on, cut to 2 .. 252;
+ *   the code is the one nearest to x / 2^(e - 127), of two equally near ones that with an
+ *   even last bit, and 6 for what lies beyond.
+ * A block with a NaN or an infinity gets e = 255: all of it stands for NaN.
+ * k_cache and v_cache are then bytes, [num_phys_pages][h_k][P d / 2 + P d / 32], a page of
+ * a KV head being its codes (element 2 i in the low half of a byte, 2 i + 1 in the high
+ * one), then its exponents:
+ *   keys    codes [P][d], exponents [P][d / 32]
+ *   values  codes [P / 4][16][4][d / 16]: of four tokens the 16 parts of the vector in
+ *           turn, of a part the tokens in turn; exponents [P / 4][d / 32][4]
+ * digest and the queries stay in dtype; a digest holds the minimum and maximum of what the
+ * page's keys stand for, so that pages are scored as they will be attended.
+ * retro_append_kv_rotary, retro_read_kv, retro_chunk_attend and retro_decode_attend take such dims, and so
+ * do the calls that touch neither keys nor values (retro_select_pages, retro_copy_scores,
+ * retro_merge_output_cache, retro_rotate_qk and the sizes); the others return RETRO_EUNSUPPORTED. */
+
+/* Rows of the cache as keys and values: row j of sequence b, as `chunk` lays them out, is
+ * the token at position start_pos[b] + j; k_out, v_out [n_rows][h_k][d] dtype (either may
+ * be NULL).  For every format of the cache.  Rows of positions at or past seq_lens[b], or
+ * whose page is not mapped, become zeros; rows that belong to no sequence stay as they
+ * were.  Reads the cache only.  n_rows == 0 does nothing. */
+retro_status retro_read_kv(const retro_dims* dims, const retro_kv_cache* cache,
+                           const retro_chunk* chunk, void* k_out, void* v_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,7 @@ RETRO_OK, RETRO_EINVAL, RETRO_EUNSUPPORTED, RETRO_EHIP, RETRO_EWORKSPACE, RETRO_
     0, -1, -2, -3, -4, -5
 RETRO_F32, RETRO_BF16 = 0, 1
 RETRO_FLAG_SEPARATE_SCORES, RETRO_FLAG_SELECT_IN_SCORES, RETRO_FLAG_TEST_WAIT_TIMEOUT = 1, 2, 4
+RETRO_FLAG_KV_MX4 = 16
 
 EXPORTED = ("retro_version", "retro_status_string", "retro_k_max", "retro_workspace_size",
             "retro_prefill_kv", "retro_append_kv", "retro_append_kv_tokens", "retro_update_kv",
@@ -28,7 +29,7 @@ EXPORTED = ("retro_version", "retro_status_string", "retro_k_max", "retro_worksp
             "retro_step_launches", "retro_attend_plan", "retro_pack_weight",
             "retro_project_qkv", "retro_project_qkv_update", "retro_project_out", "retro_project_f32",
             "retro_rotary_table", "retro_rotate_qk", "retro_append_kv_rotary",
-            "retro_chunk_workspace_size", "retro_chunk_attend")
+            "retro_chunk_workspace_size", "retro_chunk_attend", "retro_read_kv")
 
 
 class RetroError(RuntimeError):
@@ -128,6 +129,7 @@ def load_library(path: str = LIB_PATH):
         "retro_chunk_workspace_size": ([D, i32, C.POINTER(C.c_size_t)], C.c_int),
         "retro_chunk_attend": ([D, C.POINTER(KVCache), C.POINTER(Chunk), P, C.c_int64, P, P, P,
                                 C.c_size_t, P], C.c_int),
+        "retro_read_kv": ([D, C.POINTER(KVCache), C.POINTER(Chunk), P, P, P], C.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -364,3 +366,8 @@ def retro_chunk_attend(dims: Dims, cache: KVCache, chunk: Chunk, q, q_stride: in
                                              _ptr(q), q_stride, _ptr(out), _ptr(lse),
                                              _ptr(workspace), ws_bytes, _stream(stream)),
            "retro_chunk_attend")
+
+
+def retro_read_kv(dims: Dims, cache: KVCache, chunk: Chunk, k_out, v_out, stream=None) -> None:
+    _check(load_library().retro_read_kv(C.byref(dims), C.byref(cache), C.byref(chunk), _ptr(k_out),
+                                        _ptr(v_out), _stream(stream)), "retro_read_kv")

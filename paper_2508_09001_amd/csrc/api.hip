@@ -5,6 +5,7 @@
 #include <initializer_list>
 
 #include "internal.h"
+#include "mx4.h"
 #include "proj.h"
 #include "rotary.h"
 
@@ -39,7 +40,7 @@ retro_status make_geometry(const retro_dims* d, Geometry* g) {
   if (d->budget_permille < 0 || d->budget_permille > 1000) return RETRO_EINVAL;
   if (d->max_pages > 16384) return RETRO_EUNSUPPORTED;
   if (d->flags & ~(RETRO_FLAG_SEPARATE_SCORES | RETRO_FLAG_SELECT_IN_SCORES |
-                   RETRO_FLAG_TEST_WAIT_TIMEOUT))
+                   RETRO_FLAG_TEST_WAIT_TIMEOUT | RETRO_FLAG_KV_MX4))
     return RETRO_EINVAL;
   if ((int64_t)d->batch * d->num_kv_heads > 65535) return RETRO_EUNSUPPORTED;
 
@@ -150,6 +151,12 @@ retro_status prepare(const retro_dims* dims, int32_t step, Geometry* g) {
   return RETRO_OK;
 }
 
+bool aligned16(std::initializer_list<const void*> ps) {
+  uintptr_t bits = 0;
+  for (const void* p : ps) bits |= reinterpret_cast<uintptr_t>(p);
+  return (bits & 15u) == 0;
+}
+
 retro_status check_ws(const Geometry& g, void* ws, size_t ws_bytes) {
   if (!ws || ws_bytes < g.ws_total) return RETRO_EWORKSPACE;
   return RETRO_OK;
@@ -217,6 +224,7 @@ retro_status retro_prefill_kv(const retro_dims* dims, const retro_kv_cache* cach
   Geometry g;
   retro_status st = retro::make_geometry(dims, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || !k_src || !v_src) return RETRO_EINVAL;
   if (seq < 0 || seq >= g.batch || start_pos < 0 || n_tokens < 0) return RETRO_EINVAL;
   if ((int64_t)start_pos + n_tokens > (int64_t)g.max_pages * g.P) return RETRO_EINVAL;
@@ -229,6 +237,7 @@ retro_status retro_append_kv(const retro_dims* dims, int32_t step, const retro_k
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || !k_new || !v_new) return RETRO_EINVAL;
   return from_hip(retro::launch_append(g, step, *cache, k_new, v_new, (hipStream_t)stream));
 }
@@ -239,6 +248,7 @@ retro_status retro_append_kv_tokens(const retro_dims* dims, int32_t step,
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || n_tokens < 0) return RETRO_EINVAL;
   if (n_tokens == 0) return RETRO_OK;
   if (!k_new || !v_new) return RETRO_EINVAL;
@@ -252,6 +262,7 @@ retro_status retro_update_kv(const retro_dims* dims, const retro_kv_cache* cache
   Geometry g;
   retro_status st = make_geometry(dims, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || n_tokens < 0) return RETRO_EINVAL;
   if (n_tokens == 0) return RETRO_OK;
   if (!k_upd || !v_upd) return RETRO_EINVAL;
@@ -266,6 +277,7 @@ retro_status retro_project_qkv_update(const retro_dims* dims, const retro_kv_cac
   Geometry g;
   retro_status st = make_geometry(dims, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || !x || !w_packed || !q || !k_new || !v_new || k <= 0 ||
       n_update < 0 || n_update > g.W)
     return RETRO_EINVAL;
@@ -309,9 +321,12 @@ retro_status retro_decode_attend(const retro_dims* dims, int32_t step, const voi
   hipStream_t s = (hipStream_t)stream;
   float* o_ws = ws_at(workspace, g.ws_opart);
   float* l_ws = ws_at(workspace, g.ws_lpart);
-  const Geometry ga = retro::attend_geometry(g);
-  hipError_t e = retro::launch_attend(ga, step, q_window, *cache, *sel, nullptr, o_ws, l_ws,
-                                      (char*)workspace + g.ws_dummy, s);
+  const bool mx4 = retro::is_mx4(g);
+  if (mx4 && !aligned16({q_window, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
+  const Geometry ga = mx4 ? retro::mx4_window_geometry(g) : retro::attend_geometry(g);
+  hipError_t e = mx4 ? retro::launch_mx4_window(ga, step, q_window, *cache, *sel, o_ws, l_ws, s)
+                     : retro::launch_attend(ga, step, q_window, *cache, *sel, nullptr, o_ws, l_ws,
+                                            (char*)workspace + g.ws_dummy, s);
   if (e == hipSuccess)
     e = retro::launch_combine_merge(ga, step, 0, o_ws, l_ws, sel->num_selected, nullptr, nullptr,
                                     o_part, lse_part, nullptr, nullptr, nullptr, nullptr, s);
@@ -325,6 +340,7 @@ retro_status retro_decode_attend_partials(const retro_dims* dims, int32_t step,
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!q_window || !cache_ok(cache) || !sel_ok(sel)) return RETRO_EINVAL;
   if ((st = check_ws(g, workspace, ws_bytes)) != RETRO_OK) return st;
   return from_hip(retro::launch_attend(retro::attend_geometry(g), step, q_window, *cache, *sel,
@@ -339,6 +355,7 @@ retro_status retro_step_attend_partials(const retro_dims* dims, int32_t step,
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!q_window || !cache_ok(cache) || !sel_ok(sel)) return RETRO_EINVAL;
   if ((st = check_ws(g, workspace, ws_bytes)) != RETRO_OK) return st;
   if (!retro::attend_selects(g)) return RETRO_EUNSUPPORTED;
@@ -370,6 +387,7 @@ retro_status retro_attend_plan(const retro_dims* dims, int32_t selects, int32_t*
   if (!row_tiles || !splits) return RETRO_EINVAL;
   retro_status st = prepare(dims, 0, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   const Geometry ga = retro::attend_geometry(g, selects != 0);
   *row_tiles = ga.stream ? ga.tiles_per_group : 0;
   *splits = ga.n_splits;
@@ -381,6 +399,7 @@ retro_status retro_step_launches(const retro_dims* dims, int32_t* launches) {
   if (!launches) return RETRO_EINVAL;
   retro_status st = retro::make_geometry(dims, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   Geometry gp = g;
   gp.token_pending = 1;
   *launches = one_launch(gp) ? 1 : select_in_attention(gp) ? 3 : 4;
@@ -424,6 +443,7 @@ retro_status retro_step(const retro_dims* dims, int32_t step, const void* q_wind
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
+  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!q_window || !k_new || !v_new || !cache_ok(cache) || !sel_ok(sel) || !o_out || !lse_out)
     return RETRO_EINVAL;
   if (g.W > 0 && (!ocache || !ocache->o_cache || !ocache->lse_cache)) return RETRO_EINVAL;
@@ -491,12 +511,6 @@ retro_status retro_step(const retro_dims* dims, int32_t step, const void* q_wind
 }  // extern "C"
 
 namespace {
-
-bool aligned16(std::initializer_list<const void*> ps) {
-  uintptr_t bits = 0;
-  for (const void* p : ps) bits |= reinterpret_cast<uintptr_t>(p);
-  return (bits & 15u) == 0;
-}
 
 // an input of rows of `heads` vectors of d elements, whole 16-byte pieces
 bool rows_ok(const Geometry& g, const void* p, int64_t stride, int heads) {
@@ -569,6 +583,19 @@ retro_status retro_append_kv_rotary(const retro_dims* dims, int32_t step,
                                               k_stride, v, v_stride, q_out, (hipStream_t)stream));
 }
 
+retro_status retro_read_kv(const retro_dims* dims, const retro_kv_cache* cache,
+                           const retro_chunk* chunk, void* k_out, void* v_out, void* stream) {
+  Geometry g;
+  retro_status st = retro::make_geometry(dims, &g);
+  if (st != RETRO_OK) return st;
+  if (!cache_ok(cache) || !chunk_ok(cache, chunk)) return RETRO_EINVAL;
+  if (chunk->n_rows == 0) return RETRO_OK;
+  if ((!k_out && !v_out) || !aligned16({k_out, v_out, cache->k_cache, cache->v_cache}))
+    return RETRO_EINVAL;
+  if (!retro::read_kv_supported(g, chunk->n_rows)) return RETRO_EUNSUPPORTED;
+  return from_hip(retro::launch_read_kv(g, *cache, *chunk, k_out, v_out, (hipStream_t)stream));
+}
+
 retro_status retro_chunk_workspace_size(const retro_dims* dims, int32_t n_rows, size_t* bytes) {
   Geometry g;
   if (!bytes || n_rows < 0) return RETRO_EINVAL;
@@ -594,8 +621,8 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
   if (!retro::chunk_attend_supported(g, chunk->n_rows)) return RETRO_EUNSUPPORTED;
   if (!workspace || !aligned16({workspace}) || ws_bytes < retro::chunk_workspace(g, chunk->n_rows))
     return RETRO_EWORKSPACE;
-  return from_hip(retro::launch_chunk_attend(g, *cache, *chunk, q, q_stride, out, lse, workspace,
-                                             (hipStream_t)stream));
+  return from_hip((retro::is_mx4(g) ? retro::launch_mx4_attend : retro::launch_chunk_attend)(
+      g, *cache, *chunk, q, q_stride, out, lse, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

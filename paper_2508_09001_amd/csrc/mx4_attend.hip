@@ -1,0 +1,231 @@
+// Dense causal attention of a ragged batch of rows over a paged cache in 4 bits: what
+// chunk_attend.hip does over pages in dtype, with the same layout of the work
+// (chunk_work.h): the steps of all tiles of 32 rows form one line, cut into shares for
+// the workgroups, and the parts of a cut tile are joined by the workgroup that counts
+// itself last.  A workgroup's wavefronts take 32 tokens in turn, codes straight from the page into
+// registers (mx4_rows.h), and join their (maximum, sum, output) at the end of a tile.
+#include "chunk_work.h"
+#include "mx4_rows.h"
+
+namespace retro {
+namespace {
+
+template <int D>
+struct Mx4Lds {
+  static constexpr int OROW = D + 4;
+  union {
+    float o[kWaves][kRowsFew][OROW];
+    JoinLds join;
+  } u;
+  float m[kWaves][kRowsFew], l[kWaves][kRowsFew];
+  int last;
+  FindLds find;
+};
+
+template <typename T, int D, int P>
+__global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
+  __shared__ __attribute__((aligned(1024))) Mx4Lds<D> L;
+  const int tid = thread_index();
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Cut cut = make_cut<false>(a, P, L.find, tid);
+  constexpr int64_t kBlock = mx4_block_bytes(P, D);
+  const int64_t phys_bytes = kBlock * a.hk;
+  const float c = a.scale * kLog2e;
+
+  // the result of row rho of a sequence's rows for KV head h, four elements of d
+  auto finish = [&](const Seq& s, int h, int rho, float m, float l, int d, f32x4 o) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t at = (int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G;
+    store4((T*)a.out + at * D + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    if (d == 0 && a.lse) a.lse[at] = natural_lse(m, l, a.scale);
+  };
+
+  // The rows from rho0 on (nr of them) with the keys of [key_begin, key_end), this
+  // wavefront's share of them; results into LDS.
+  auto tile_of = [&](auto row_tiles, const Seq& s, int b, int h, int rho0, int nr, int key_begin, int key_end) {
+    constexpr int NR = decltype(row_tiles)::value;
+    const int lane = thread_index() & 63;
+    const Pages page_of{a.pt + (int64_t)b * a.max_pages, max((s.end + P - 1) / P - 1, 0), a.num_phys};
+    const char* kh = (const char*)a.kc + h * kBlock;
+    const char* vh = (const char*)a.vc + h * kBlock;
+    Mx4Rows<T, D, NR> rows;
+    rows.c = c;
+    int lim[NR];  // last token that the lane's row may see
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int rho = rho0 + 16 * n + (lane & 15), r = min(rho, s.rows - 1);
+      lim[n] = min(s.run.pos + r / a.G, s.end - 1);
+      rows.start(n, (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride + (int64_t)(h * a.G + r % a.G) * D,
+                 rho < s.rows, lane);
+    }
+    const int all_see = min(s.run.pos + rho0 / a.G, s.end - 1);  // last token that every row sees
+    const Mx4Places<D, P> at(lane);
+    // loads a tile; which of its halves lie in pages that are not mapped
+    auto load = [&](Mx4Tile<D>& x, int key) {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        bool bad;
+        const int64_t page = page_of((key + 16 * t) / P, bad) * phys_bytes;
+        bits |= (uint32_t)bad << t;
+        at.load(x, t, kh + page, vh + page, (key + 16 * t) % P);
+      }
+      return bits;
+    };
+    auto work = [&](Mx4Tile<D>& x, int key, uint32_t bad) {
+      const bool clean = !bad && key + 31 <= all_see;
+      if (!clean) {
+        const int first = key + 4 * (lane >> 4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          x.ve[t] = live_exponents(x.ve[t], bad >> t & 1 ? 0 : s.end - (first + 16 * t));
+      }
+      rows.step(x, [&](int n, f32x4(&sc)[2]) {
+        if (clean) return;
+        const int first = key + 4 * (lane >> 4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (first + 16 * t + e > lim[n] || (bad >> t & 1)) sc[t][e] = -INFINITY;
+      });
+    };
+    constexpr int kNext = 32 * kWaves;
+    int key = key_begin + wave * 32;
+    if (key < key_end) {
+      Mx4Tile<D> x, y;
+      uint32_t bx = load(x, key), by = 0;
+      for (;;) {
+        const bool more = key + kNext < key_end;
+        if (more) by = load(y, key + kNext);
+        work(x, key, bx);
+        if (!more) break;
+        key += kNext;
+        const bool again = key + kNext < key_end;
+        if (again) bx = load(x, key + kNext);
+        work(y, key, by);
+        if (!again) break;
+        key += kNext;
+      }
+    }
+    // results, for the join of the wavefronts
+    barrier();
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int r = 16 * n + (lane & 15);
+      const float l = col_sum4(rows.l[n]);
+      if (lane < 16) {
+        L.m[wave][r] = rows.m[n];
+        L.l[wave][r] = l;
+      }
+      if (r < nr)
+        rows.each(n, lane, [&](int d, f32x4 o) { *reinterpret_cast<f32x4*>(&L.u.o[wave][r][d]) = o; });
+    }
+  };
+
+  // this workgroup's share of the line of steps
+  const int64_t me = kCus - 1 - blockIdx.x, mine = cut.begin(me), upto = min(cut.begin(me + 1), cut.line);
+  for (int64_t pos = mine; pos < upto;) {
+    int b = 0;
+    int64_t local = 0, before;
+    Seq s;
+    find_seq(a, P, pos, L.find, tid, [&](const Seq& s) { return cut.line_of(s, a); },
+             [](const Seq&) { return (int64_t)0; }, s, b, local, before);
+    const int tiles = s.tiles(kRowsFew);
+    // its KV heads and their tiles, one after the other
+    const int64_t per_head = s.place(tiles, a.G);
+    int h = (int)(local / per_head), tile = 0;
+    local -= h * per_head;
+    for (int n = tiles; n > 1;) {  // the last tile that begins at or in front of local
+      const int half = n / 2;
+      if (s.place(tile + half, a.G) <= local) {
+        tile += half;
+        n -= half;
+      } else {
+        n = half;
+      }
+    }
+    int step0 = (int)(local - s.place(tile, a.G));
+    while (h < a.hk && pos < upto) {
+      const int rho0 = tile * kRowsFew, nr = min(s.rows - rho0, kRowsFew);
+      const int length = (int)(s.place(tile + 1, a.G) - s.place(tile, a.G));
+      const int n = (int)min((int64_t)(length - step0), upto - pos);
+      // (a place's last steps may lie behind the tile's end, in a sequence whose start_pos
+      // is out of range far behind: then nothing is read)
+      const int key_begin = min(step0, 1 << 24) * 64,
+                key_end = (int)min((int64_t)s.seen(rho0 + kRowsFew, a.G), ((int64_t)step0 + n) * 64);
+      if (nr <= 16) tile_of(std::integral_constant<int, 1>{}, s, b, h, rho0, nr, key_begin, key_end);
+      else tile_of(std::integral_constant<int, 2>{}, s, b, h, rho0, nr, key_begin, key_end);
+      barrier();
+      // a part: slot 2 k of workgroup k for what its share begins with, 2 k + 1 for what it ends with
+      const bool whole = n == length;
+      auto slot = [&](int64_t i) { return a.few + i * slot_floats(kRowsFew, D); };
+      const __amdgpu_buffer_rsrc_t part = coherent_rsrc(slot(2 * me + (pos != mine)));
+      for (int i = tid; i < nr * (D / 4); i += kThreads) {
+        const int row = i / (D / 4), d = i % (D / 4) * 4;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, L.m[w][row]);
+        const float mu = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * c);
+          const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
+          l = __builtin_fmaf(e, L.l[w][row], l);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
+        }
+        if (whole) {
+          finish(s, h, rho0 + row, m, l, d, o);
+        } else {
+          put_part(part, row * D + d, o);
+          if (d == 0) {
+            put_part(part, kRowsFew * D + row, m);
+            put_part(part, kRowsFew * (D + 1) + row, l);
+          }
+        }
+      }
+      if (!whole) {
+        // the tile's steps are start .. start + length - 1 of the line
+        const int64_t start = pos - step0, k0 = cut.owner(start);
+        const int parts = (int)(cut.owner(start + length - 1) - k0) + 1;
+        if (last_part(a.counters + k0, parts, &L.last, tid))
+          join_few<D>(
+              L.u.join, nr, parts, c, tid,
+              [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != cut.begin(k0))); },
+              [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, rho0 + row, m, l, d, o); });
+      }
+      barrier();
+      pos += n;
+      step0 = 0;
+      if (++tile == tiles) {
+        tile = 0;
+        ++h;
+      }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_mx4_attend(const Geometry& g, const retro_kv_cache& c, const retro_chunk& ch,
+                             const void* q, int64_t q_stride, void* out, float* lse, void* ws,
+                             hipStream_t s) {
+  const AttendCall a = attend_call(g, c, ch, q, q_stride, out, lse, ws);
+  auto go = [&](auto t, auto d, auto ps) {
+    mx4_attend_kernel<decltype(t), decltype(d)::value, decltype(ps)::value><<<kCus, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+  };
+  auto with_page = [&](auto t, auto d) {
+    return g.P == 16 ? go(t, d, std::integral_constant<int, 16>{})
+                     : go(t, d, std::integral_constant<int, 32>{});
+  };
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (g.dtype == RETRO_BF16) return g.D == 128 ? with_page(bf16_t{}, D128{}) : with_page(bf16_t{}, D64{});
+  return g.D == 128 ? with_page(float{}, D128{}) : with_page(float{}, D64{});
+}
+
+}  // namespace retro

@@ -8,7 +8,7 @@
 // everything between stay in fp32 and are rounded once.  Bound by HBM: every
 // vector is read once and written once, at 4.6 to 4.7 TB/s where a plain copy
 // reaches 4.8; by the launch for a few rows.
-#include "roles.h"
+#include "mx4.h"
 #include "rotary.h"
 
 namespace retro {
@@ -219,45 +219,53 @@ __global__ void __launch_bounds__(256) rotate_qk_kernel(
 
 // ---- append ------------------------------------------------------------------------
 
-// pages that a run touches
-__device__ __forceinline__ int run_pages(const Run& r, int P) {
-  if (r.n <= 0) return 0;
-  return (int)(((int64_t)r.pos + r.n - 1) / P) - r.pos / P + 1;
-}
-
-// The sequence that unit `u` of all sequences' pages belongs to, and the page
-// within its run; -1 behind the last.  Every wavefront finds it by itself.
-__device__ __forceinline__ int find_page(const retro_chunk& ch, int batch, int P, int lane, int u,
-                                         Run& run, int& page) {
-  int base = 0;
-  for (int b0 = 0; b0 < batch; b0 += 64) {
-    Run r{0, 0, 0};
-    if (b0 + lane < batch) r = chunk_run(ch, b0 + lane);
-    const int n = run_pages(r, P), upto = base + wave_inclusive_scan(n);
-    const uint64_t past = wave_ballot(upto > u);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      run.row = __builtin_amdgcn_readlane(r.row, l);
-      run.n = __builtin_amdgcn_readlane(r.n, l);
-      run.pos = __builtin_amdgcn_readlane(r.pos, l);
-      page = u - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
-      return b0 + l;
-    }
-    base = __builtin_amdgcn_readlane(upto, 63);
-  }
-  return -1;
-}
-
 constexpr int kAppendThreads = 128;
+
+// A lane's piece of a head's vector in codes; the lanes of a block together.
+template <typename T>
+struct Codes {
+  static constexpr int E = 16 / sizeof(T);
+  uint32_t codes;  // E of them
+  int e;
+  __device__ explicit Codes(u32x4 piece) {
+    float x[E];
+    unpack<T>(piece, x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = max(top, (uint32_t)dpp_i<kDppXor1>((int)top));
+    top = max(top, (uint32_t)dpp_i<kDppXor2>((int)top));
+    if constexpr (E == 4) top = max(top, (uint32_t)dpp_i<kDppHalfMirror>((int)top));
+    e = mx4_exponent(top);
+    // (a block that is NaN as a whole has codes like any other)
+    const float s = mx4_scale(e == kMx4NaN ? 127 : e);
+    codes = mx4_encode<0>(0, x[0], x[1], s);
+    codes = mx4_encode<1>(codes, x[2], x[3], s);
+    if constexpr (E == 8) {
+      codes = mx4_encode<2>(codes, x[4], x[5], s);
+      codes = mx4_encode<3>(codes, x[6], x[7], s);
+    }
+  }
+  __device__ void store(char* at) const {
+    if constexpr (E == 8) *reinterpret_cast<uint32_t*>(at) = codes;
+    else *reinterpret_cast<uint16_t*>(at) = (uint16_t)codes;
+  }
+  __device__ u32x4 values() const { return mx4_piece<T>(codes, mx4_scale(e)); }
+};
 
 // One workgroup per (page of a sequence's run, KV head) stores the page's new
 // keys (token-major) and values (d-major, transposed through LDS, whole 16-byte
 // pieces where the run covers them) and widens the digest; as many others turn
 // the queries of the page's rows, G heads each.  The positions come from
 // start_pos, so that one workgroup can advance seq_lens while the others run.
-template <typename T, int PS, int D>
+//
+// MX4: pages in 4 bits (mx4.h).  Keys are rounded to T as they would be stored, then
+// both to codes, a block by the lanes that hold it; codes and exponents go straight to
+// their places in the page (four tokens' values side by side, so that a wavefront writes
+// 256 bytes in a row), and the digest is that of the codes' values.
+template <typename T, int PS, int D, bool MX4>
 __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
-    Geometry g, int step, retro_chunk ch, retro_rotary r, T* __restrict__ kc, T* __restrict__ vc,
+    Geometry g, int step, retro_chunk ch, retro_rotary r, char* __restrict__ kc, char* __restrict__ vc,
     T* __restrict__ dg, const int32_t* __restrict__ pt, int32_t* __restrict__ seq_lens,
     int32_t* __restrict__ loaded, const T* q, int64_t q_stride, const T* __restrict__ k,
     int64_t k_stride, const T* __restrict__ v, int64_t v_stride, T* q_out) {
@@ -265,7 +273,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   constexpr int E = Tn::E, LPV = Tn::LPV;
   constexpr int ROW = D + E;  // padded LDS row
   __shared__ __attribute__((aligned(16))) T ks[PS * ROW];
-  __shared__ __attribute__((aligned(16))) T vs[PS * ROW];
+  __shared__ __attribute__((aligned(16))) T vs[MX4 ? E : PS * ROW];
   __shared__ int first_bad;
   const int tid = threadIdx.x, lane = tid & 63;
   Run run;
@@ -326,8 +334,10 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   if (lp >= g.max_pages) return;
   const int phys = pt[(int64_t)b * g.max_pages + lp];
   if (phys < 0 || phys >= g.num_phys) return;
-  const int64_t blk = ((int64_t)phys * g.hk + h) * PS * D;
   turn.weights(r.k_norm, wt);
+  const int64_t block = (int64_t)phys * g.hk + h;
+  constexpr int kBytes = MX4 ? mx4_block_bytes(PS, D) : PS * D * (int)sizeof(T);
+  char *const kblk = kc + block * kBytes, *const vblk = vc + block * kBytes;
   constexpr int NP = PS * LPV / kAppendThreads;  // passes over a page's rows
   u32x4 kr[NP], vr[NP];
 #pragma unroll
@@ -342,17 +352,36 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
     const int t = tid / LPV + i * (kAppendThreads / LPV);
     if (t < s0 || t >= s1) continue;
     turn.angles(lp * PS + t, a);
-    const u32x4 kt = turn(kr[i], r.k_norm != nullptr, wt, a, lane);
-    reinterpret_cast<u32x4*>(kc + blk + t * D)[turn.c] = kt;
+    u32x4 kt = turn(kr[i], r.k_norm != nullptr, wt, a, lane);
+    if constexpr (MX4) {
+      const Codes<T> kq(kt), vq(vr[i]);
+      const int n = E / 2, block = turn.c * E / 32, part = turn.c * E / (D / 16), in = turn.c * E % (D / 16);
+      kq.store(kblk + t * (D / 2) + turn.c * n);
+      char* group = vblk + t / 4 * (2 * D);
+      if constexpr (E <= D / 16) {
+        vq.store(group + (part * 4 + t % 4) * (D / 32) + in / 2);
+      } else {  // (two parts of four elements)
+        static_assert(E == 2 * (D / 16), "a piece is a part, or half of one, or two");
+        reinterpret_cast<uint16_t*>(group)[part * 4 + t % 4] = (uint16_t)vq.codes;
+        reinterpret_cast<uint16_t*>(group)[part * 4 + 4 + t % 4] = (uint16_t)(vq.codes >> 16);
+      }
+      if (turn.c * E % 32 == 0) {
+        kblk[PS * D / 2 + t * (D / 32) + block] = (char)kq.e;
+        vblk[PS * D / 2 + (t / 4 * (D / 32) + block) * 4 + t % 4] = (char)vq.e;
+      }
+      kt = kq.values();
+    } else {
+      reinterpret_cast<u32x4*>((T*)kblk + t * D)[turn.c] = kt;
+      *reinterpret_cast<u32x4*>(vs + t * ROW + turn.c * E) = vr[i];
+    }
     *reinterpret_cast<u32x4*>(ks + t * ROW + turn.c * E) = kt;
-    *reinterpret_cast<u32x4*>(vs + t * ROW + turn.c * E) = vr[i];
   }
   __syncthreads();
   // values: E consecutive tokens of one element of d per piece
-  for (int e = tid; e < D * (PS / E); e += kAppendThreads) {
+  for (int e = tid; !MX4 && e < D * (PS / E); e += kAppendThreads) {
     const int i = e / (PS / E), t0 = e % (PS / E) * E;
     if (t0 + E <= s0 || t0 >= s1) continue;
-    T* dst = vc + blk + (int64_t)i * PS + t0;
+    T* dst = (T*)vblk + (int64_t)i * PS + t0;
     T x[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) x[j] = vs[(t0 + j) * ROW + i];
@@ -404,11 +433,8 @@ int64_t rotate_blocks(const Geometry& g, int rows, bool q, bool k) {
   return (rows * ((heads + vpw - 1) / vpw) + 3) / 4;
 }
 
-// every sequence's pages, at most n / P + 2 of each, in eights (an XCD's workgroups are
-// every eighth), times the workgroups of a page
 int64_t append_blocks(const Geometry& g, int n_rows, bool q) {
-  const int64_t pages = n_rows / g.P + 2 * (int64_t)std::min(g.batch, n_rows);
-  return (pages + 7) / 8 * 8 * (q ? 2 : 1) * g.hk;
+  return page_blocks(g, n_rows, (q ? 2 : 1) * g.hk);
 }
 
 }  // namespace
@@ -451,14 +477,19 @@ hipError_t launch_append_rotary(const Geometry& g, int step, const retro_kv_cach
                                 int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                 int64_t v_stride, void* q_out, hipStream_t s) {
   const unsigned grid = (unsigned)append_blocks(g, ch.n_rows, q != nullptr);
+  const bool mx4 = is_mx4(g);
   return with_type_and_dim(g, [&](auto t, auto d) {
     using T = decltype(t);
-    auto go = [&](auto ps) {
-      append_rotary_kernel<T, decltype(ps)::value, decltype(d)::value><<<grid, kAppendThreads, 0, s>>>(
-          g, step, ch, r, (T*)c.k_cache, (T*)c.v_cache, (T*)c.digest, c.page_table, c.seq_lens,
-          c.last_loaded, (const T*)q, q_stride, (const T*)k, k_stride, (const T*)v, v_stride,
-          (T*)q_out);
+    auto with_format = [&](auto ps, auto in_4_bits) {
+      append_rotary_kernel<T, decltype(ps)::value, decltype(d)::value, decltype(in_4_bits)::value>
+          <<<grid, kAppendThreads, 0, s>>>(
+              g, step, ch, r, (char*)c.k_cache, (char*)c.v_cache, (T*)c.digest, c.page_table, c.seq_lens,
+              c.last_loaded, (const T*)q, q_stride, (const T*)k, k_stride, (const T*)v, v_stride,
+              (T*)q_out);
       return hipGetLastError();
+    };
+    auto go = [&](auto ps) {
+      return mx4 ? with_format(ps, std::true_type{}) : with_format(ps, std::false_type{});
     };
     return g.P == 16 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 32>{});
   });
