@@ -68,18 +68,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
   auto kxor = [](int i) { return (uint32_t)S::fk(i * kRowsPerCopy & 31) << 4; };
   auto vxor = [](int i) { return S::CPV == 8 ? (uint32_t)(i & 1) << 6 : 0u; };
 
-  auto pages_of = [&](const Seq& s, int b) {
-    return Pages{a.pt + (int64_t)b * a.max_pages, max((s.end + P - 1) / P - 1, 0), a.num_phys};
-  };
-  // row rho of a sequence's rows for KV head h (the last one for those behind it)
-  auto row_at = [&](const Seq& s, int h, int rho, bool& live, int& lim) {
-    live = rho < s.rows;
-    const int r = min(rho, s.rows - 1);
-    lim = min(s.run.pos + r / a.G, s.end - 1);
-    return (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride +
-           (int64_t)(h * a.G + r % a.G) * D;
-  };
-  // the result of such a row, four elements of d
+  // the result of row rho of a sequence's rows for KV head h, four elements of d
   auto finish = [&](const Seq& s, int h, int rho, float m, float l, int d, f32x4 o) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t at = (int64_t)(s.run.row + rho / a.G) * a.hq + h * a.G + rho % a.G;
@@ -98,7 +87,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
       Seq s;
       find_seq(a, P, pos, L.find, tid, [&](const Seq& s) { return cut.line_of(s, a); },
                [](const Seq&) { return (int64_t)0; }, s, b, local, before);
-      const Pages page_of = pages_of(s, b);
+      const Pages page_of = pages_of<P>(a, s, b);
       const int tiles = s.tiles(kRowsFew);
       // its KV heads and their tiles, one after the other
       const int64_t per_head = s.place(tiles, a.G);
@@ -129,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
         rows.init(lane, a.scale);
         bool live;
         int lim;
-        const T* qrow = row_at(s, h, rho0 + (lane & 31), live, lim);
+        const T* qrow = row_at<T, D>(a, s, h, rho0 + (lane & 31), live, lim);
         rows.start(qrow, live, lim);
         const int all_see = min(s.run.pos + rho0 / a.G, s.end - 1);  // last token that every row sees
         const uint32_t ks = st + wave * (int)sizeof(L.u.own[0]), vs = S::ONE ? ks : ks + S::TILE;
@@ -250,185 +239,6 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
     }
   };
 
-  // ---- many rows
-  [[maybe_unused]] auto many_rows = [&](auto) {  // (generic: compiled where it is called)
-    constexpr int PS = S::KEYS / P;  // pages of a stage
-    const int most = (int)cut.part;
-    auto parts_of = [&](int steps) { return (steps + most - 1) / most; };
-    for (int64_t round = 0;; ++round) {
-      // longest first; every other round backwards, eight neighbours (one per XCD) together
-      int64_t k = blockIdx.x;
-      if (round & 1) k = (int64_t)(gridDim.x / 8 - 1 - k / 8) * 8 + k % 8;
-      int b;
-      int64_t u, before;
-      Seq s;
-      if (!find_seq(a, P, round * gridDim.x + k, L.find, tid,
-                    [&](const Seq& s) {
-                      return s.few ? 0 : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
-                    },
-                    [&](const Seq& s) {
-                      return s.few || s.steps() <= most
-                                 ? 0
-                                 : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
-                    },
-                    s, b, u, before))
-        break;
-      const int un = __builtin_amdgcn_readfirstlane((int)u);
-      // KV head fastest (a head's units meet in one L2), then row tiles, last first
-      const int tiles = s.tiles(kRowsMany);
-      const int h = un % a.hk, part = un / a.hk / tiles, back = un / a.hk % tiles;
-      const int tile = tiles - 1 - back;
-      const int R = min(s.rows - tile * kRowsMany, kRowsMany);
-      const int end = s.seen(tile * kRowsMany + R, a.G);   // tokens that the tile sees
-      const int steps = max((end + 63) / 64, 1), parts = parts_of(steps);
-      if (part >= parts) continue;
-      const int per = (steps + parts - 1) / parts;
-      const int key_begin = part * per * 64, key_end = min(end, (part + 1) * per * 64);
-      const Pages page_of = pages_of(s, b);
-      const char* kh = (const char*)a.kc + h * page_bytes;
-      const char* vh = (const char*)a.vc + h * page_bytes;
-      const int lane = thread_index() & 63;
-      R_t rows;
-      rows.init(lane, a.scale);
-      const int rho0 = tile * kRowsMany + wave * 32;
-      const bool any = rho0 < s.rows;
-      bool live;
-      int lim;
-      const T* qrow = row_at(s, h, rho0 + (lane & 31), live, lim);
-      rows.start(qrow, live, lim);
-      rows.read_from(st, st + S::NB * S::TILE);
-      // Every row sees the tokens up to the first row's; stages behind them, and all
-      // where a page is not mapped, are masked.  No row of the wavefront sees past lim1.
-      const int np = (key_end + P - 1) / P;
-      bool missing = false;
-      for (int i = key_begin / P + tid; i < np; i += kThreads) {
-        const int id = page_of.table[i];
-        missing |= id < 0 || id >= a.num_phys;
-      }
-      const int seen = __syncthreads_or(missing) ? 0 : min(s.run.pos + tile * kRowsMany / a.G, s.end - 1) + 1;
-      const int lim1 =
-          any ? min(s.run.pos + min(rho0 + 31, s.rows - 1) / a.G, s.end - 1) : -1;
-      constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
-      static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
-      const int first = wave * MINE;
-      auto page_at = [&](int key) {  // of the wavefront's copies of the stage from this key on
-        bool bad;
-        return page_of(key / P + first / S::PPP, bad);
-      };
-      uint32_t to = st;
-      auto copy_keys = [&](int page) {
-        const char* src = kh + page * phys_bytes + first % S::PPP * 1024;
-#pragma unroll
-        for (int i = 0; i < MINE; ++i)
-          copy_to_lds<false>(src + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
-      };
-      auto copy_values = [&](int page) {
-        const char* src = vh + page * phys_bytes + first % S::PPP * 1024;
-#pragma unroll
-        for (int i = 0; i < MINE; ++i)
-          copy_to_lds<false>(src + i * 1024, vcopy ^ vxor(first + i),
-                      to + S::NB * S::TILE + (first + i) * 1024);
-      };
-      // A stage of LDS holds 64 keys' values and the next 64 keys: while the weights of
-      // one are taken, the scores of the next are made.
-      int key = key_begin, page = 0, page_next = 0;
-      int32_t by = S::STAGE;  // to the other stage
-      // in front of the work on the stage at `key`: its copies are there, the next one's begin
-      auto turn = [&]() {
-        wait_loads<0>();
-        barrier();
-        to += by;
-        if (key + S::KEYS < key_end) copy_values(page);
-        if (key + 2 * S::KEYS < key_end) copy_keys(page_next);
-        page = page_next;
-        page_next = page_at(key + 3 * S::KEYS);
-      };
-      auto next_stage = [&]() {
-        rows.move_by(by);
-        by = -by;
-        key += S::KEYS;
-      };
-      if (key_begin < key_end) {
-        f32x16 sa[S::NB], sb[S::NB];
-        page = page_at(key);
-        page_next = page_at(key + S::KEYS);
-        copy_keys(page);
-        to += by;
-        copy_values(page);
-        if (key + S::KEYS < key_end) copy_keys(page_next);
-        page = page_next;
-        page_next = page_at(key + 2 * S::KEYS);
-        wait_loads<MINE>();
-        barrier();
-#pragma unroll
-        for (int i = 0; i < S::NB; ++i) sa[i] = rows.scores(i * S::TILE);
-        rows.move_by(by);
-        by = -by;
-        // stages that no mask touches, up to the last but one
-        const int clean = min(seen / S::KEYS * S::KEYS, key_end - S::KEYS);
-        auto step = [&](f32x16(&cur)[S::NB], f32x16(&next)[S::NB]) {
-          turn();
-          rows.weave(cur, next, rows.follow(cur));
-          next_stage();
-        };
-        while (key + S::KEYS < clean) {
-          step(sa, sb);
-          step(sb, sa);
-        }
-        if (key < clean) {
-          step(sa, sb);
-#pragma unroll
-          for (int i = 0; i < S::NB; ++i) sa[i] = sb[i];
-        }
-        while (key < key_end) {
-          turn();
-          if (key <= lim1) {
-            const uint32_t bad = page_of.template bad<PS>(key / P);
-            rows.mask(sa, key, bad);
-            rows.weights(sa, rows.follow(sa));
-#pragma unroll
-            for (int i = 0; i < S::NB; ++i)
-              rows.template values<false>(i * S::TILE, sa[i], s.end - key - 32 * i, bad >> (i * 32 / P));
-          }
-          if (key + S::KEYS <= lim1)
-#pragma unroll
-            for (int i = 0; i < S::NB; ++i) sa[i] = rows.scores(i * S::TILE);
-          next_stage();
-        }
-      }
-      rows.l = rows_half_sum(rows.l);
-      const int rt = wave * 32 + (lane & 31);
-      auto slot = [&](int p) {
-        return a.many + (before + ((int64_t)p * tiles + back) * a.hk + h) * slot_floats(kRowsMany, D);
-      };
-      const __amdgpu_buffer_rsrc_t dst = coherent_rsrc(slot(part));
-      if (rt < R) {
-#pragma unroll
-        for (int i = 0; i < R_t::DT; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const int d = i * 32 + 2 * e + 4 * rows.half;
-            const f32x4 o{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
-            if (parts > 1) put_part(dst, rt * D + d, o);
-            else finish(s, h, tile * kRowsMany + rt, rows.m, rows.l, d, o);
-          }
-        if (parts > 1 && lane < 32) {
-          put_part(dst, kRowsMany * D + rt, rows.m);
-          put_part(dst, kRowsMany * (D + 1) + rt, rows.l);
-        }
-      }
-      if (parts > 1) {
-        const int64_t first = before + (int64_t)back * a.hk + h;  // the tile's first part among all
-        if (last_part(a.counters + kCus + first, parts, &L.last, tid))
-          join_many<D>(L.u.join_many, R, parts, rows.c, tid, slot,
-                       [&](int row, float m, float l, int d, f32x4 o) {
-                         finish(s, h, tile * kRowsMany + row, m, l, d, o);
-                       });
-      }
-      barrier();
-    }
-  };
-
   // Reading the cache for few rows leaves the matrix cores idle and the other way
   // round: every other workgroup of an XCD begins with the one, the rest with the other.
   [[maybe_unused]] const bool turn = blockIdx.x >> 3 & 1;
@@ -436,7 +246,8 @@ __global__ void __launch_bounds__(kThreads) chunk_attend_kernel(AttendCall a) {
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       if ((i == 0) != turn) {
-        if (cut.many) many_rows(0);
+        if (cut.many)
+          many_rows<T, D, P>(a, cut, L, tid, wave, CopiedStages<T, D, P>{phys_bytes, page_bytes, kcopy, vcopy}, finish);
       } else {
         if (cut.line) few_rows();
       }
@@ -480,23 +291,6 @@ size_t chunk_workspace(const Geometry& g, int n_rows) {
                         bounds(g, n_rows).parts * slot_floats(kRowsMany, g.D);
   return kCounterBytes + ((floats * sizeof(float) + 255) & ~size_t(255));
 }
-
-namespace {
-
-// Whether the call gets the kernel that also takes tiles of many rows, which costs a
-// call without them 3 us and 5 to 18 % (a token each of 33 to 512 sequences at 60 to 8000
-// tokens).  The device knows the lengths; the host may know the longest one: up to 32 rows
-// there are no such tiles, and above 128 they are worth having (a chunk beside empty ranges,
-// us without and with them: 280 rows of 256 sequences at 4000 96 and 57, 540 of 512 at 4000
-// 146 and 69, at 0 52 and 31; 64 of 64 at 4000 34 and 37).  In between, and where it is
-// unknown, every sequence is taken to have a row, which bounds the longest.
-bool may_have_many(const retro_chunk& ch, int batch, int G) {
-  const int64_t longest = (int64_t)std::min(ch.longest, ch.n_rows) * G;
-  if (longest > 4 * kRowsFew) return true;
-  return ((int64_t)ch.n_rows - batch + 1) * G > 4 * kRowsFew && (longest <= 0 || longest > kRowsFew);
-}
-
-}  // namespace
 
 hipError_t launch_chunk_attend(const Geometry& g, const retro_kv_cache& c, const retro_chunk& ch,
                                const void* q, int64_t q_stride, void* out, float* lse, void* ws,

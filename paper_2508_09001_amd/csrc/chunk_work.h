@@ -325,6 +325,19 @@ inline AttendCall attend_call(const Geometry& g, const retro_kv_cache& c, const 
                     g.sm_scale};
 }
 
+// Whether the call gets the kernel that also takes tiles of many rows, which costs a
+// call without them 3 us and 5 to 18 % (a token each of 33 to 512 sequences at 60 to 8000
+// tokens).  The device knows the lengths; the host may know the longest one: up to 32 rows
+// there are no such tiles, and above 128 they are worth having (a chunk beside empty ranges,
+// us without and with them: 280 rows of 256 sequences at 4000 96 and 57, 540 of 512 at 4000
+// 146 and 69, at 0 52 and 31; 64 of 64 at 4000 34 and 37).  In between, and where it is
+// unknown, every sequence is taken to have a row, which bounds the longest.
+inline bool may_have_many(const retro_chunk& ch, int batch, int G) {
+  const int64_t longest = (int64_t)std::min(ch.longest, ch.n_rows) * G;
+  if (longest > 4 * kRowsFew) return true;
+  return ((int64_t)ch.n_rows - batch + 1) * G > 4 * kRowsFew && (longest <= 0 || longest > kRowsFew);
+}
+
 // ---- LDS pieces ----------------------------------------------------------------------
 
 template <typename T, int D, int P>
@@ -714,6 +727,19 @@ struct Pages {
   }
 };
 
+// A sequence's pages, and row rho of its rows for KV head h (the last one for those behind it).
+template <int P>
+__device__ __forceinline__ Pages pages_of(const AttendCall& a, const Seq& s, int b) {
+  return Pages{a.pt + (int64_t)b * a.max_pages, max((s.end + P - 1) / P - 1, 0), a.num_phys};
+}
+template <typename T, int D>
+__device__ __forceinline__ const T* row_at(const AttendCall& a, const Seq& s, int h, int rho, bool& live, int& lim) {
+  live = rho < s.rows;
+  const int r = min(rho, s.rows - 1);
+  lim = min(s.run.pos + r / a.G, s.end - 1);
+  return (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride + (int64_t)(h * a.G + r % a.G) * D;
+}
+
 // ---- parts -------------------------------------------------------------------------------
 
 // Stores and loads of parts go past the XCDs' L2s, through a resource per part.
@@ -922,6 +948,219 @@ __device__ __forceinline__ void join_many(JoinManyLds& L, int R, int parts, floa
   for (int i = 0; i < ITEMS; ++i) {
     const int row = row0 + i * PER;
     if (row < R) done(row, L.m[row], L.sum[row], d, o[i]);
+  }
+}
+
+// ---- many rows ---------------------------------------------------------------------------
+
+// Stages of 64 keys for all wavefronts, copied from pages in T.  A stage of LDS holds 64
+// keys' values and the next 64 keys.
+template <typename T, int D, int P>
+struct CopiedStages {
+  using S = Shape<T, D, P>;
+  static constexpr int MINE = S::NB * S::LOADS / kWaves;  // copies of keys (and of values) per wavefront
+  static_assert(MINE >= 1 && S::PPP % MINE == 0, "a wavefront's copies lie in one page");
+  int64_t phys_bytes, page_bytes;
+  uint32_t kcopy, vcopy;  // a lane's place within a copy of keys, and of values
+  const char *kh, *vh;
+  Pages page_of;
+  uint32_t to;
+  int first, page, page_next;
+
+  __device__ __forceinline__ int page_at(int key) const {  // of the wavefront's copies of the stage from this key on
+    bool bad;
+    return page_of(key / P + first / S::PPP, bad);
+  }
+  // copy i of a tile: rows further on, whose numbers change the order by this
+  static __device__ __forceinline__ uint32_t kxor(int i) { return (uint32_t)S::fk(i * (64 / S::CPR) & 31) << 4; }
+  static __device__ __forceinline__ uint32_t vxor(int i) { return S::CPV == 8 ? (uint32_t)(i & 1) << 6 : 0u; }
+  __device__ __forceinline__ void copy_keys(int page) {
+    const char* src = kh + page * phys_bytes + first % S::PPP * 1024;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i)
+      copy_to_lds<false>(src + i * 1024, kcopy ^ kxor(first + i), to + (first + i) * 1024);
+  }
+  __device__ __forceinline__ void copy_values(int page) {
+    const char* src = vh + page * phys_bytes + first % S::PPP * 1024;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i)
+      copy_to_lds<false>(src + i * 1024, vcopy ^ vxor(first + i), to + S::NB * S::TILE + (first + i) * 1024);
+  }
+  // a tile of KV head h begins; LDS stages from `st` on
+  __device__ __forceinline__ void start(const AttendCall& a, const Pages& pages, int h, uint32_t st, int wave) {
+    page_of = pages;
+    kh = (const char*)a.kc + h * page_bytes;
+    vh = (const char*)a.vc + h * page_bytes;
+    to = st;
+    first = wave * MINE;
+  }
+  // the first stage's keys are there when this returns, its values and the next keys on their way
+  __device__ __forceinline__ void begin(int key, int key_end, int32_t by) {
+    page = page_at(key);
+    page_next = page_at(key + S::KEYS);
+    copy_keys(page);
+    to += by;
+    copy_values(page);
+    if (key + S::KEYS < key_end) copy_keys(page_next);
+    page = page_next;
+    page_next = page_at(key + 2 * S::KEYS);
+    wait_loads<MINE>();
+    barrier();
+  }
+  // in front of the work on the stage at `key`: its copies are there, the next one's begin
+  __device__ __forceinline__ void turn(int key, int key_end, int32_t by) {
+    wait_loads<0>();
+    barrier();
+    to += by;
+    if (key + S::KEYS < key_end) copy_values(page);
+    if (key + 2 * S::KEYS < key_end) copy_keys(page_next);
+    page = page_next;
+    page_next = page_at(key + 3 * S::KEYS);
+  }
+};
+
+// Tiles of 256 rows: 32 of them for each wavefront, over the same 64 keys.  finish: the
+// result of a row, four elements of d.
+template <typename T, int D, int P, typename Lds, typename Stages, typename Finish>
+__device__ __forceinline__ void many_rows(const AttendCall& a, const Cut& cut, Lds& L, int tid, int wave,
+                                          Stages stages, Finish&& finish) {
+  using S = Shape<T, D, P>;
+  using R_t = Rows<T, D, P>;
+  const uint32_t st = lds_address(&L.u);
+  constexpr int PS = S::KEYS / P;  // pages of a stage
+  const int most = (int)cut.part;
+  auto parts_of = [&](int steps) { return (steps + most - 1) / most; };
+  for (int64_t round = 0;; ++round) {
+    // longest first; every other round backwards, eight neighbours (one per XCD) together
+    int64_t k = blockIdx.x;
+    if (round & 1) k = (int64_t)(gridDim.x / 8 - 1 - k / 8) * 8 + k % 8;
+    int b;
+    int64_t u, before;
+    Seq s;
+    if (!find_seq(a, P, round * gridDim.x + k, L.find, tid,
+                  [&](const Seq& s) {
+                    return s.few ? 0 : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
+                  },
+                  [&](const Seq& s) {
+                    return s.few || s.steps() <= most
+                               ? 0
+                               : (int64_t)s.tiles(kRowsMany) * a.hk * parts_of(s.steps());
+                  },
+                  s, b, u, before))
+      break;
+    const int un = __builtin_amdgcn_readfirstlane((int)u);
+    // KV head fastest (a head's units meet in one L2), then row tiles, last first
+    const int tiles = s.tiles(kRowsMany);
+    const int h = un % a.hk, part = un / a.hk / tiles, back = un / a.hk % tiles;
+    const int tile = tiles - 1 - back;
+    const int R = min(s.rows - tile * kRowsMany, kRowsMany);
+    const int end = s.seen(tile * kRowsMany + R, a.G);   // tokens that the tile sees
+    const int steps = max((end + 63) / 64, 1), parts = parts_of(steps);
+    if (part >= parts) continue;
+    const int per = (steps + parts - 1) / parts;
+    const int key_begin = part * per * 64, key_end = min(end, (part + 1) * per * 64);
+    const Pages page_of = pages_of<P>(a, s, b);
+    const int lane = thread_index() & 63;
+    R_t rows;
+    rows.init(lane, a.scale);
+    const int rho0 = tile * kRowsMany + wave * 32;
+    const bool any = rho0 < s.rows;
+    bool live;
+    int lim;
+    const T* qrow = row_at<T, D>(a, s, h, rho0 + (lane & 31), live, lim);
+    rows.start(qrow, live, lim);
+    rows.read_from(st, st + S::NB * S::TILE);
+    // Every row sees the tokens up to the first row's; stages behind them, and all
+    // where a page is not mapped, are masked.  No row of the wavefront sees past lim1.
+    const int np = (key_end + P - 1) / P;
+    bool missing = false;
+    for (int i = key_begin / P + tid; i < np; i += kThreads) {
+      const int id = page_of.table[i];
+      missing |= id < 0 || id >= a.num_phys;
+    }
+    const int seen = __syncthreads_or(missing) ? 0 : min(s.run.pos + tile * kRowsMany / a.G, s.end - 1) + 1;
+    const int lim1 =
+        any ? min(s.run.pos + min(rho0 + 31, s.rows - 1) / a.G, s.end - 1) : -1;
+    // A stage of LDS holds 64 keys' values and the next 64 keys: while the weights of
+    // one are taken, the scores of the next are made.
+    int key = key_begin;
+    int32_t by = S::STAGE;  // to the other stage
+    stages.start(a, page_of, h, st, wave);
+    auto turn = [&]() { stages.turn(key, key_end, by); };
+    auto next_stage = [&]() {
+      rows.move_by(by);
+      by = -by;
+      key += S::KEYS;
+    };
+    if (key_begin < key_end) {
+      f32x16 sa[S::NB], sb[S::NB];
+      stages.begin(key, key_end, by);
+#pragma unroll
+      for (int i = 0; i < S::NB; ++i) sa[i] = rows.scores(i * S::TILE);
+      rows.move_by(by);
+      by = -by;
+      // stages that no mask touches, up to the last but one
+      const int clean = min(seen / S::KEYS * S::KEYS, key_end - S::KEYS);
+      auto step = [&](f32x16(&cur)[S::NB], f32x16(&next)[S::NB]) {
+        turn();
+        rows.weave(cur, next, rows.follow(cur));
+        next_stage();
+      };
+      while (key + S::KEYS < clean) {
+        step(sa, sb);
+        step(sb, sa);
+      }
+      if (key < clean) {
+        step(sa, sb);
+#pragma unroll
+        for (int i = 0; i < S::NB; ++i) sa[i] = sb[i];
+      }
+      while (key < key_end) {
+        turn();
+        if (key <= lim1) {
+          const uint32_t bad = page_of.template bad<PS>(key / P);
+          rows.mask(sa, key, bad);
+          rows.weights(sa, rows.follow(sa));
+#pragma unroll
+          for (int i = 0; i < S::NB; ++i)
+            rows.template values<false>(i * S::TILE, sa[i], s.end - key - 32 * i, bad >> (i * 32 / P));
+        }
+        if (key + S::KEYS <= lim1)
+#pragma unroll
+          for (int i = 0; i < S::NB; ++i) sa[i] = rows.scores(i * S::TILE);
+        next_stage();
+      }
+    }
+    rows.l = rows_half_sum(rows.l);
+    const int rt = wave * 32 + (lane & 31);
+    auto slot = [&](int p) {
+      return a.many + (before + ((int64_t)p * tiles + back) * a.hk + h) * slot_floats(kRowsMany, D);
+    };
+    const __amdgpu_buffer_rsrc_t dst = coherent_rsrc(slot(part));
+    if (rt < R) {
+#pragma unroll
+      for (int i = 0; i < R_t::DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const int d = i * 32 + 2 * e + 4 * rows.half;
+          const f32x4 o{rows.acc[i][e], rows.acc[i][e + 1], rows.acc[i][e + 2], rows.acc[i][e + 3]};
+          if (parts > 1) put_part(dst, rt * D + d, o);
+          else finish(s, h, tile * kRowsMany + rt, rows.m, rows.l, d, o);
+        }
+      if (parts > 1 && lane < 32) {
+        put_part(dst, kRowsMany * D + rt, rows.m);
+        put_part(dst, kRowsMany * (D + 1) + rt, rows.l);
+      }
+    }
+    if (parts > 1) {
+      const int64_t first = before + (int64_t)back * a.hk + h;  // the tile's first part among all
+      if (last_part(a.counters + kCus + first, parts, &L.last, tid))
+        join_many<D>(L.u.join_many, R, parts, rows.c, tid, slot,
+                     [&](int row, float m, float l, int d, f32x4 o) {
+                       finish(s, h, tile * kRowsMany + row, m, l, d, o);
+                     });
+    }
+    barrier();
   }
 }
 

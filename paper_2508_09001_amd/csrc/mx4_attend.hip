@@ -10,24 +10,157 @@
 namespace retro {
 namespace {
 
-template <int D>
+template <int D, int P, bool MANY>
 struct Mx4Lds {
+  using S = Shape<bf16_t, D, P>;
   static constexpr int OROW = D + 4;
   union {
+    char stage[2][MANY ? S::STAGE : 16];
     float o[kWaves][kRowsFew][OROW];
     JoinLds join;
+    JoinManyLds join_many;
   } u;
   float m[kWaves][kRowsFew], l[kWaves][kRowsFew];
   int last;
   FindLds find;
 };
 
-template <typename T, int D, int P>
+// Stages of 64 keys for tiles of many rows, as chunk_attend.hip's copies leave them in LDS: the
+// codes of a stage are read into registers while the one before it is worked on, an eighth by
+// each wavefront (eight tokens of one page, keys and values), and go to LDS as
+// bf16 when its turn comes.
+template <int D, int P>
+struct Mx4Stages {
+  using S = Shape<bf16_t, D, P>;
+  static constexpr int64_t kBlock = mx4_block_bytes(P, D);
+  static constexpr int KP = D / 64;  // 16-byte pieces of a key that a lane makes
+  int64_t phys_bytes;
+  const char *kh, *vh;
+  Pages page_of;
+  uint32_t to;
+  int wave, page_k, page_v;  // pages of the keys and values to be read next
+  uint32_t k[KP], ke, v[2][D / 32], ve[2];
+
+  __device__ __forceinline__ int page_at(int key) const {
+    bool bad;
+    return page_of((key + 8 * wave) / P, bad);
+  }
+  __device__ __forceinline__ void load_keys(int page) {
+    const int lane = threadIdx.x & 63, key = 8 * wave % P + lane / 8, c = lane % 8;
+    const char* b = kh + page * phys_bytes;
+    const char* at = b + (key * (D / 2) + c * (D / 16));
+    if constexpr (KP == 2) {
+      const uint2 x = *reinterpret_cast<const uint2*>(at);
+      k[0] = x.x;
+      k[1] = x.y;
+    } else {
+      k[0] = *reinterpret_cast<const uint32_t*>(at);
+    }
+    ke = *reinterpret_cast<const uint8_t*>(b + (P * D / 2 + key * (D / 32) + c * (D / 8) / 32));
+  }
+  // element pair 2 lane, 2 lane + 1 of eight tokens
+  __device__ __forceinline__ void load_values(int page) {
+    const int lane = threadIdx.x & 63, part = lane / (D / 32) & 15, group = 8 * wave % P / 4;
+    const char* b = vh + page * phys_bytes;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* at = b + ((group + t) * 16 + part) * (D / 8);
+      if constexpr (D == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[t][i] = x[i];
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(at);
+        v[t][0] = x.x;
+        v[t][1] = x.y;
+      }
+      ve[t] = *reinterpret_cast<const uint32_t*>(
+          b + (P * D / 2 + ((group + t) * (D / 32) + (lane / 16) % (D / 32)) * 4));
+    }
+  }
+  static __device__ __forceinline__ void put(uint32_t at, u32x4 x) {
+    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = x;
+  }
+  __device__ __forceinline__ void put_keys() const {
+    const int lane = threadIdx.x & 63, key = 8 * wave + lane / 8, row = key % 32;
+    const float scale = mx4_scale((int)ke);
+#pragma unroll
+    for (int i = 0; i < KP; ++i)
+      put(to + key / 32 * S::TILE + row * (D * 2) + ((lane % 8 * KP + i) ^ S::fk(row)) * 16,
+          mx4_piece<bf16_t>(k[i], scale));
+  }
+  __device__ __forceinline__ void put_values() const {
+    const int lane = threadIdx.x & 63, token = 8 * wave % 32, d = 2 * lane, byte = lane % (D / 32) * 8;
+    if (d >= D) return;
+    uint32_t x[8];  // both elements of a token
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float scale[4] = {__uint_as_float(ve[t] << 23), __uint_as_float(ve[t] << 15),
+                              __uint_as_float(ve[t] << 7), __uint_as_float(ve[t] >> 1)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t w = v[t][e * (D / 32) / 4] >> byte;
+        x[4 * t + e] = e * (D / 32) % 4 ? mx4_bf16<2>(w, scale[e]) : mx4_bf16<0>(w, scale[e]);
+      }
+    }
+    const uint32_t at = to + S::NB * S::TILE + 8 * wave / 32 * S::TILE + token / P * (D * P * 2);
+    u32x4 a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = low_halves(x[2 * i], x[2 * i + 1]);
+      b[i] = high_halves(x[2 * i], x[2 * i + 1]);
+    }
+    const int piece = (token % P / 8 ^ S::fv(d)) * 16;  // (the same for d + 1)
+    put(at + d * (P * 2) + piece, a);
+    put(at + (d + 1) * (P * 2) + piece, b);
+  }
+  __device__ __forceinline__ void start(const AttendCall& a, const Pages& pages, int h, uint32_t st, int w) {
+    page_of = pages;
+    phys_bytes = kBlock * a.hk;
+    kh = (const char*)a.kc + h * kBlock;
+    vh = (const char*)a.vc + h * kBlock;
+    to = st;
+    wave = w;
+  }
+  __device__ __forceinline__ void begin(int key, int key_end, int32_t by) {
+    const int page = page_at(key);
+    page_v = page_at(key + S::KEYS);
+    load_keys(page);
+    load_values(page);
+    put_keys();
+    to += by;
+    load_keys(page_v);
+    put_values();
+    put_keys();
+    page_k = page_at(key + 2 * S::KEYS);
+    read_next(key, key_end);
+    page_k = page_at(key + 3 * S::KEYS);
+    barrier();
+  }
+  // the values of the stage behind the one at `key` and the keys behind those
+  __device__ __forceinline__ void read_next(int key, int key_end) {
+    if (key + S::KEYS < key_end) load_values(page_v);
+    if (key + 2 * S::KEYS < key_end) load_keys(page_k);
+    page_v = page_k;
+  }
+  // in front of the work on the stage at `key`: it is there, the next one is written
+  __device__ __forceinline__ void turn(int key, int key_end, int32_t by) {
+    barrier();
+    to += by;
+    if (key + S::KEYS < key_end) put_values();
+    if (key + 2 * S::KEYS < key_end) put_keys();
+    read_next(key + S::KEYS, key_end);
+    page_k = page_at(key + 4 * S::KEYS);
+  }
+};
+
+// MANY: with tiles of many rows, as in chunk_attend.hip.
+template <typename T, int D, int P, bool MANY>
 __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
-  __shared__ __attribute__((aligned(1024))) Mx4Lds<D> L;
+  __shared__ __attribute__((aligned(1024))) Mx4Lds<D, P, MANY> L;
   const int tid = thread_index();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Cut cut = make_cut<false>(a, P, L.find, tid);
+  const Cut cut = make_cut<MANY>(a, P, L.find, tid);
   constexpr int64_t kBlock = mx4_block_bytes(P, D);
   const int64_t phys_bytes = kBlock * a.hk;
   const float c = a.scale * kLog2e;
@@ -123,88 +256,105 @@ __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
     }
   };
 
-  // this workgroup's share of the line of steps
-  const int64_t me = kCus - 1 - blockIdx.x, mine = cut.begin(me), upto = min(cut.begin(me + 1), cut.line);
-  for (int64_t pos = mine; pos < upto;) {
-    int b = 0;
-    int64_t local = 0, before;
-    Seq s;
-    find_seq(a, P, pos, L.find, tid, [&](const Seq& s) { return cut.line_of(s, a); },
-             [](const Seq&) { return (int64_t)0; }, s, b, local, before);
-    const int tiles = s.tiles(kRowsFew);
-    // its KV heads and their tiles, one after the other
-    const int64_t per_head = s.place(tiles, a.G);
-    int h = (int)(local / per_head), tile = 0;
-    local -= h * per_head;
-    for (int n = tiles; n > 1;) {  // the last tile that begins at or in front of local
-      const int half = n / 2;
-      if (s.place(tile + half, a.G) <= local) {
-        tile += half;
-        n -= half;
-      } else {
-        n = half;
-      }
-    }
-    int step0 = (int)(local - s.place(tile, a.G));
-    while (h < a.hk && pos < upto) {
-      const int rho0 = tile * kRowsFew, nr = min(s.rows - rho0, kRowsFew);
-      const int length = (int)(s.place(tile + 1, a.G) - s.place(tile, a.G));
-      const int n = (int)min((int64_t)(length - step0), upto - pos);
-      // (a place's last steps may lie behind the tile's end, in a sequence whose start_pos
-      // is out of range far behind: then nothing is read)
-      const int key_begin = min(step0, 1 << 24) * 64,
-                key_end = (int)min((int64_t)s.seen(rho0 + kRowsFew, a.G), ((int64_t)step0 + n) * 64);
-      if (nr <= 16) tile_of(std::integral_constant<int, 1>{}, s, b, h, rho0, nr, key_begin, key_end);
-      else tile_of(std::integral_constant<int, 2>{}, s, b, h, rho0, nr, key_begin, key_end);
-      barrier();
-      // a part: slot 2 k of workgroup k for what its share begins with, 2 k + 1 for what it ends with
-      const bool whole = n == length;
-      auto slot = [&](int64_t i) { return a.few + i * slot_floats(kRowsFew, D); };
-      const __amdgpu_buffer_rsrc_t part = coherent_rsrc(slot(2 * me + (pos != mine)));
-      for (int i = tid; i < nr * (D / 4); i += kThreads) {
-        const int row = i / (D / 4), d = i % (D / 4) * 4;
-        float m = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, L.m[w][row]);
-        const float mu = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        f32x4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * c);
-          const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
-          l = __builtin_fmaf(e, L.l[w][row], l);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
-        }
-        if (whole) {
-          finish(s, h, rho0 + row, m, l, d, o);
+  // ---- tiles of 32 rows: this workgroup's share of the line of steps
+  auto few_rows = [&]() {
+    const int64_t me = kCus - 1 - blockIdx.x, mine = cut.begin(me), upto = min(cut.begin(me + 1), cut.line);
+    for (int64_t pos = mine; pos < upto;) {
+      int b = 0;
+      int64_t local = 0, before;
+      Seq s;
+      find_seq(a, P, pos, L.find, tid, [&](const Seq& s) { return cut.line_of(s, a); },
+               [](const Seq&) { return (int64_t)0; }, s, b, local, before);
+      const int tiles = s.tiles(kRowsFew);
+      // its KV heads and their tiles, one after the other
+      const int64_t per_head = s.place(tiles, a.G);
+      int h = (int)(local / per_head), tile = 0;
+      local -= h * per_head;
+      for (int n = tiles; n > 1;) {  // the last tile that begins at or in front of local
+        const int half = n / 2;
+        if (s.place(tile + half, a.G) <= local) {
+          tile += half;
+          n -= half;
         } else {
-          put_part(part, row * D + d, o);
-          if (d == 0) {
-            put_part(part, kRowsFew * D + row, m);
-            put_part(part, kRowsFew * (D + 1) + row, l);
+          n = half;
+        }
+      }
+      int step0 = (int)(local - s.place(tile, a.G));
+      while (h < a.hk && pos < upto) {
+        const int rho0 = tile * kRowsFew, nr = min(s.rows - rho0, kRowsFew);
+        const int length = (int)(s.place(tile + 1, a.G) - s.place(tile, a.G));
+        const int n = (int)min((int64_t)(length - step0), upto - pos);
+        // (a place's last steps may lie behind the tile's end, in a sequence whose start_pos
+        // is out of range far behind: then nothing is read)
+        const int key_begin = min(step0, 1 << 24) * 64,
+                  key_end = (int)min((int64_t)s.seen(rho0 + kRowsFew, a.G), ((int64_t)step0 + n) * 64);
+        if (nr <= 16) tile_of(std::integral_constant<int, 1>{}, s, b, h, rho0, nr, key_begin, key_end);
+        else tile_of(std::integral_constant<int, 2>{}, s, b, h, rho0, nr, key_begin, key_end);
+        barrier();
+        // a part: slot 2 k of workgroup k for what its share begins with, 2 k + 1 for what it ends with
+        const bool whole = n == length;
+        auto slot = [&](int64_t i) { return a.few + i * slot_floats(kRowsFew, D); };
+        const __amdgpu_buffer_rsrc_t part = coherent_rsrc(slot(2 * me + (pos != mine)));
+        for (int i = tid; i < nr * (D / 4); i += kThreads) {
+          const int row = i / (D / 4), d = i % (D / 4) * 4;
+          float m = -INFINITY;
+  #pragma unroll
+          for (int w = 0; w < kWaves; ++w) m = fmaxf(m, L.m[w][row]);
+          const float mu = m == -INFINITY ? 0.f : m;
+          float l = 0.f;
+          f32x4 o{0.f, 0.f, 0.f, 0.f};
+  #pragma unroll
+          for (int w = 0; w < kWaves; ++w) {
+            const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * c);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
+            l = __builtin_fmaf(e, L.l[w][row], l);
+  #pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
+          }
+          if (whole) {
+            finish(s, h, rho0 + row, m, l, d, o);
+          } else {
+            put_part(part, row * D + d, o);
+            if (d == 0) {
+              put_part(part, kRowsFew * D + row, m);
+              put_part(part, kRowsFew * (D + 1) + row, l);
+            }
           }
         }
-      }
-      if (!whole) {
-        // the tile's steps are start .. start + length - 1 of the line
-        const int64_t start = pos - step0, k0 = cut.owner(start);
-        const int parts = (int)(cut.owner(start + length - 1) - k0) + 1;
-        if (last_part(a.counters + k0, parts, &L.last, tid))
-          join_few<D>(
-              L.u.join, nr, parts, c, tid,
-              [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != cut.begin(k0))); },
-              [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, rho0 + row, m, l, d, o); });
-      }
-      barrier();
-      pos += n;
-      step0 = 0;
-      if (++tile == tiles) {
-        tile = 0;
-        ++h;
+        if (!whole) {
+          // the tile's steps are start .. start + length - 1 of the line
+          const int64_t start = pos - step0, k0 = cut.owner(start);
+          const int parts = (int)(cut.owner(start + length - 1) - k0) + 1;
+          if (last_part(a.counters + k0, parts, &L.last, tid))
+            join_few<D>(
+                L.u.join, nr, parts, c, tid,
+                [&](int p) { return slot(2 * (k0 + p) + (p == 0 && start != cut.begin(k0))); },
+                [&](int row, float m, float l, int d, f32x4 o) { finish(s, h, rho0 + row, m, l, d, o); });
+        }
+        barrier();
+        pos += n;
+        step0 = 0;
+        if (++tile == tiles) {
+          tile = 0;
+          ++h;
+        }
       }
     }
+  };
+
+  // (the half of an XCD's workgroups that begins with the one way, the rest with the other)
+  [[maybe_unused]] const bool turn = blockIdx.x >> 3 & 1;
+  if constexpr (MANY) {
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+      if ((i == 0) != turn) {
+        if (cut.many) many_rows<bf16_t, D, P>(a, cut, L, tid, wave, Mx4Stages<D, P>{}, finish);
+      } else {
+        if (cut.line) few_rows();
+      }
+    }
+  } else {
+    if (cut.line) few_rows();
   }
 }
 
@@ -215,7 +365,15 @@ hipError_t launch_mx4_attend(const Geometry& g, const retro_kv_cache& c, const r
                              hipStream_t s) {
   const AttendCall a = attend_call(g, c, ch, q, q_stride, out, lse, ws);
   auto go = [&](auto t, auto d, auto ps) {
-    mx4_attend_kernel<decltype(t), decltype(d)::value, decltype(ps)::value><<<kCus, kThreads, 0, s>>>(a);
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value, P = decltype(ps)::value;
+    if constexpr (sizeof(T) == 2) {
+      if (may_have_many(ch, g.batch, g.G)) {
+        mx4_attend_kernel<T, D, P, true><<<kCus, kThreads, 0, s>>>(a);
+        return hipGetLastError();
+      }
+    }
+    mx4_attend_kernel<T, D, P, false><<<kCus, kThreads, 0, s>>>(a);
     return hipGetLastError();
   };
   auto with_page = [&](auto t, auto d) {

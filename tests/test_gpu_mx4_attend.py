@@ -134,6 +134,50 @@ def test_chunks(dtype, P, d, hk, G, seqs):
     Chunk(dtype, hk, G, d, P, seqs, seed=P + d + G).run().check()
 
 
+# enough work for tiles of 256 rows (bf16), whose stages of 64 keys and parts end inside
+# the sequences: at least 1024 steps of 64 keys over tiles and KV heads
+LARGE = [
+    ([(700, 0), (300, 2500), (64, 1000), (1, 700), (9, 130)], 8, 4),
+    ([(1500, 100), (600, 900)], 8, 1),
+    ([(200, 1500), (130, 3)], 4, 16),
+    ([(517, 1400), (300, 333)], 9, 3),
+]
+
+
+@pytest.mark.parametrize("P,d", [(16, 128), (32, 128), (16, 64), (32, 64)])
+@pytest.mark.parametrize("seqs,hk,G", LARGE, ids=[str(i) for i in range(len(LARGE))])
+def test_large_chunks(P, d, seqs, hk, G):
+    Chunk("bf16", hk, G, d, P, seqs, seed=P + d + G).run().check()
+
+
+def test_large_chunks_cut_unmapped_or_short():
+    Chunk("f32", 2, 4, 64, 16, [(700, 0), (300, 1500)], seed=2).run().check()
+    Chunk("bf16", 2, 4, 128, 16, [(150, 9000), (1, 5000)], seed=12).run().check()
+    un = [(0, 0), (0, 50), (0, 107), (1, 0), (1, 1), (2, 3), (2, 62)]
+    Chunk("bf16", 8, 4, 128, 16, [(700, 1000), (300, 0), (40, 960)], seed=13, unmapped=un).run().check()
+    for P, d in ((32, 64), (16, 128)):
+        c = Chunk("bf16", 8, 4, d, P, [(700, 1000), (300, 800), (300, 0)], seed=14)
+        lens = [1350, 500, 0]
+        c.len_t.copy_(torch.tensor(lens, dtype=torch.int32))
+        c.run().check(lens)
+
+
+def test_large_chunks_same_results_again():
+    """The same call gives the same bits, also told the longest run, on a workspace that other dims used."""
+    c = Chunk("bf16", 8, 4, 128, 16, [(400, 2000), (1, 3000), (30, 100)], seed=19)
+    other = Chunk("f32", 3, 1, 64, 32, [(100, 900)], seed=18)
+    c.run().check()
+    want, z = c.out.clone(), c.lse.clone()
+    other.ws, other.ws_bytes = c.ws, c.ws_bytes
+    for _ in range(3):
+        other.run().check()
+        c.out.fill_(5.0)
+        c.run()
+        assert torch.equal(c.out, want) and torch.equal(c.lse, z)
+    c.chunk.longest = 400
+    c.run().check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("P,d", [(16, 128), (32, 64)])
 def test_chunks_unmapped(dtype, P, d):
