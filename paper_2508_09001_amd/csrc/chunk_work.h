@@ -568,9 +568,10 @@ struct Rows {
   // product with the tiles of values from here on, woven together: a matrix
   // instruction takes 32 cycles of its unit and 4 to issue, so the vector
   // instructions of the softmax run beside it, a share of them behind each; LDS is
-  // read four pieces ahead.  (sched_barrier: the compiler keeps this order.)
-  template <int NB>
-  __device__ __forceinline__ void weave(f32x16 (&s)[NB], f32x16 (&next)[NB], float mc) {
+  // read four pieces ahead.  (sched_barrier: the compiler keeps this order.)  beside(i, n):
+  // more to be done next to matrix instruction i of n.
+  template <int NB, typename Beside>
+  __device__ __forceinline__ void weave(f32x16 (&s)[NB], f32x16 (&next)[NB], float mc, Beside&& beside) {
     static_assert(sizeof(T) == 2, "tiles of many rows are bf16");
     constexpr int SE = 16 / (32 / (2 * S::E));   // scores of a lane that a step of values takes
     constexpr int NS = NB * S::QC, STEPS = NB * 16 / SE, TOTAL = NS + STEPS * DT;
@@ -612,6 +613,7 @@ struct Rows {
 #pragma unroll
       for (int e = min(i * EL / SPAN, EL); e < min((i + 1) * EL / SPAN, EL); ++e)
         s[e / 16][e % 16] = weight(s[e / 16][e % 16], mc);
+      beside(i, TOTAL);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -953,8 +955,7 @@ __device__ __forceinline__ void join_many(JoinManyLds& L, int R, int parts, floa
 
 // ---- many rows ---------------------------------------------------------------------------
 
-// Stages of 64 keys for all wavefronts, copied from pages in T.  A stage of LDS holds 64
-// keys' values and the next 64 keys.
+// Stages of 64 keys for all wavefronts, copied from pages in T.
 template <typename T, int D, int P>
 struct CopiedStages {
   using S = Shape<T, D, P>;
@@ -1017,6 +1018,9 @@ struct CopiedStages {
     page = page_next;
     page_next = page_at(key + 3 * S::KEYS);
   }
+  // what is left of a turn: beside the matrix instructions, or at once
+  __device__ __forceinline__ void beside(int, int) {}
+  __device__ __forceinline__ void finish() {}
 };
 
 // Tiles of 256 rows: 32 of them for each wavefront, over the same 64 keys.  finish: the
@@ -1103,7 +1107,7 @@ __device__ __forceinline__ void many_rows(const AttendCall& a, const Cut& cut, L
       const int clean = min(seen / S::KEYS * S::KEYS, key_end - S::KEYS);
       auto step = [&](f32x16(&cur)[S::NB], f32x16(&next)[S::NB]) {
         turn();
-        rows.weave(cur, next, rows.follow(cur));
+        rows.weave(cur, next, rows.follow(cur), [&](int i, int n) { stages.beside(i, n); });
         next_stage();
       };
       while (key + S::KEYS < clean) {
@@ -1117,6 +1121,7 @@ __device__ __forceinline__ void many_rows(const AttendCall& a, const Cut& cut, L
       }
       while (key < key_end) {
         turn();
+        stages.finish();
         if (key <= lim1) {
           const uint32_t bad = page_of.template bad<PS>(key / P);
           rows.mask(sa, key, bad);

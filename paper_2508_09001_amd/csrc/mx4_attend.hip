@@ -10,12 +10,22 @@
 namespace retro {
 namespace {
 
+// What a wavefront reads of a stage of 64 keys: codes and exponents of eight tokens' keys,
+// and of eight tokens' values.
+template <int D>
+struct Mx4Share {
+  char codes[2][4 * D], exps[2][D / 4];
+};
+
 template <int D, int P, bool MANY>
 struct Mx4Lds {
   using S = Shape<bf16_t, D, P>;
   static constexpr int OROW = D + 4;
   union {
-    char stage[2][MANY ? S::STAGE : 16];
+    struct {
+      char stage[2][MANY ? S::STAGE : 16];
+      Mx4Share<D> shares[MANY ? 2 * kWaves : 1];
+    } many;
     float o[kWaves][kRowsFew][OROW];
     JoinLds join;
     JoinManyLds join_many;
@@ -25,94 +35,113 @@ struct Mx4Lds {
   FindLds find;
 };
 
-// Stages of 64 keys for tiles of many rows, as chunk_attend.hip's copies leave them in LDS: the
-// codes of a stage are read into registers while the one before it is worked on, an eighth by
-// each wavefront (eight tokens of one page, keys and values), and go to LDS as
-// bf16 when its turn comes.
+// Stages of 64 keys for tiles of many rows, as chunk_attend.hip's copies leave them in LDS.
+// Each wavefront copies an eighth of the next stage's codes to LDS (eight tokens of one
+// page, keys and values), converts those of this one to bf16, values with eight tokens of
+// an element together, and writes them to the stage.  The conversion is woven into the
+// matrix instructions of the stage in front.
 template <int D, int P>
 struct Mx4Stages {
   using S = Shape<bf16_t, D, P>;
   static constexpr int64_t kBlock = mx4_block_bytes(P, D);
   static constexpr int KP = D / 64;  // 16-byte pieces of a key that a lane makes
+  const Mx4Share<D>* shares;         // the workgroup's, of two stages
   int64_t phys_bytes;
   const char *kh, *vh;
   Pages page_of;
   uint32_t to;
-  int wave, page_k, page_v;  // pages of the keys and values to be read next
-  uint32_t k[KP], ke, v[2][D / 32], ve[2];
+  int wave, now, page_k, page_v;  // share that is converted next; pages to be copied next
+  uint32_t k[KP], ke, v[2][D / 32], ve[2], x[8];
 
   __device__ __forceinline__ int page_at(int key) const {
     bool bad;
     return page_of((key + 8 * wave) / P, bad);
   }
-  __device__ __forceinline__ void load_keys(int page) {
-    const int lane = threadIdx.x & 63, key = 8 * wave % P + lane / 8, c = lane % 8;
-    const char* b = kh + page * phys_bytes;
-    const char* at = b + (key * (D / 2) + c * (D / 16));
-    if constexpr (KP == 2) {
-      const uint2 x = *reinterpret_cast<const uint2*>(at);
-      k[0] = x.x;
-      k[1] = x.y;
-    } else {
-      k[0] = *reinterpret_cast<const uint32_t*>(at);
+  __device__ __forceinline__ const Mx4Share<D>& share(int which) const { return shares[which * kWaves + wave]; }
+  // copies keys of one page and values of another into a share, without waiting
+  __device__ __forceinline__ void copy(int key_page, int value_page, const Mx4Share<D>& s) const {
+    const int lane = threadIdx.x & 63, slot = 8 * wave % P;
+    const char *kb = kh + key_page * phys_bytes, *vb = vh + value_page * phys_bytes;
+    // (m0 and its wait states as in copy_to_lds)
+    if (lane < D / 2) {
+      const char* from = (lane < D / 4 ? kb : vb) + (slot * (D / 2) + (lane & (D / 4 - 1)) * 16);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off"
+                   :
+                   : "s"(lds_address(s.codes)), "v"(from)
+                   : "memory");
     }
-    ke = *reinterpret_cast<const uint8_t*>(b + (P * D / 2 + key * (D / 32) + c * (D / 8) / 32));
+    if (lane < D / 8) {
+      const char* from = (lane < D / 16 ? kb : vb) + (P * D / 2 + slot * (D / 32) + (lane & (D / 16 - 1)) * 4);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off"
+                   :
+                   : "s"(lds_address(s.exps)), "v"(from)
+                   : "memory");
+    }
   }
-  // element pair 2 lane, 2 lane + 1 of eight tokens
-  __device__ __forceinline__ void load_values(int page) {
-    const int lane = threadIdx.x & 63, part = lane / (D / 32) & 15, group = 8 * wave % P / 4;
-    const char* b = vh + page * phys_bytes;
+  // the next copy: values of the stage at `key` and the keys behind them
+  __device__ __forceinline__ void copy_next(int key, int key_end) {
+    if (key < key_end) copy(page_k, page_v, share(now ^ 1));
+    page_v = page_k;
+    page_k = page_at(key + 2 * S::KEYS);
+  }
+  // the lane's part of the share
+  __device__ __forceinline__ void read() {
+    const Mx4Share<D>& s = share(now);
+    const int lane = threadIdx.x & 63, part = lane / (D / 32) & 15;
+#pragma unroll
+    for (int i = 0; i < KP; ++i) k[i] = *reinterpret_cast<const uint32_t*>(s.codes[0] + lane * (D / 16) + 4 * i);
+    ke = (uint8_t)s.exps[0][lane / 8 * (D / 32) + lane % 8 * (D / 8) / 32];
+    // elements 2 lane, 2 lane + 1 of eight tokens
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const char* at = b + ((group + t) * 16 + part) * (D / 8);
-      if constexpr (D == 128) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[t][i] = x[i];
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(at);
-        v[t][0] = x.x;
-        v[t][1] = x.y;
-      }
-      ve[t] = *reinterpret_cast<const uint32_t*>(
-          b + (P * D / 2 + ((group + t) * (D / 32) + (lane / 16) % (D / 32)) * 4));
+      for (int i = 0; i < D / 32; ++i)
+        v[t][i] = *reinterpret_cast<const uint32_t*>(s.codes[1] + t * (2 * D) + part * (D / 8) + 4 * i);
+      ve[t] = *reinterpret_cast<const uint32_t*>(s.exps[1] + t * (D / 8) + (lane / 16) % (D / 32) * 4);
     }
   }
-  static __device__ __forceinline__ void put(uint32_t at, u32x4 x) {
-    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = x;
+  static __device__ __forceinline__ void put(uint32_t at, u32x4 y) {
+    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = y;
   }
-  __device__ __forceinline__ void put_keys() const {
+  __device__ __forceinline__ void put_keys(int i) const {
     const int lane = threadIdx.x & 63, key = 8 * wave + lane / 8, row = key % 32;
-    const float scale = mx4_scale((int)ke);
-#pragma unroll
-    for (int i = 0; i < KP; ++i)
-      put(to + key / 32 * S::TILE + row * (D * 2) + ((lane % 8 * KP + i) ^ S::fk(row)) * 16,
-          mx4_piece<bf16_t>(k[i], scale));
+    put(to + key / 32 * S::TILE + row * (D * 2) + ((lane % 8 * KP + i) ^ S::fk(row)) * 16,
+        mx4_piece<bf16_t>(k[i], mx4_scale((int)ke)));
   }
-  __device__ __forceinline__ void put_values() const {
-    const int lane = threadIdx.x & 63, token = 8 * wave % 32, d = 2 * lane, byte = lane % (D / 32) * 8;
+  __device__ __forceinline__ void convert_values(int t, int e) {
+    const int byte = (threadIdx.x & 63) % (D / 32) * 8;
+    // (a scale's bits below its exponent field, and its sign, do not count)
+    const float scale = __uint_as_float(e < 3 ? ve[t] << (23 - 8 * e) : ve[t] >> 1);
+    const uint32_t w = v[t][e * (D / 32) / 4] >> byte;
+    x[4 * t + e] = e * (D / 32) % 4 ? mx4_bf16<2>(w, scale) : mx4_bf16<0>(w, scale);
+  }
+  __device__ __forceinline__ void put_values(int high) const {
+    const int lane = threadIdx.x & 63, token = 8 * wave % 32, d = 2 * lane;
     if (d >= D) return;
-    uint32_t x[8];  // both elements of a token
+    u32x4 y;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const float scale[4] = {__uint_as_float(ve[t] << 23), __uint_as_float(ve[t] << 15),
-                              __uint_as_float(ve[t] << 7), __uint_as_float(ve[t] >> 1)};
+    for (int i = 0; i < 4; ++i)
+      y[i] = high ? high_halves(x[2 * i], x[2 * i + 1]) : low_halves(x[2 * i], x[2 * i + 1]);
+    put(to + S::NB * S::TILE + 8 * wave / 32 * S::TILE + token / P * (D * P * 2) + (d + high) * (P * 2) +
+            (token % P / 8 ^ S::fv(d)) * 16,  // (the same for d + 1)
+        y);
+  }
+  // the conversion in kUnits units
+  static constexpr int kUnits = 11 + KP;
+  __device__ __forceinline__ void unit(int u) {
+    if (u == 0) read();
+    else if (u <= KP) put_keys(u - 1);
+    else if (u <= KP + 8) convert_values((u - KP - 1) / 4, (u - KP - 1) % 4);
+    else put_values(u - KP - 9);
+  }
+  __device__ __forceinline__ void beside(int i, int n) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t w = v[t][e * (D / 32) / 4] >> byte;
-        x[4 * t + e] = e * (D / 32) % 4 ? mx4_bf16<2>(w, scale[e]) : mx4_bf16<0>(w, scale[e]);
-      }
-    }
-    const uint32_t at = to + S::NB * S::TILE + 8 * wave / 32 * S::TILE + token / P * (D * P * 2);
-    u32x4 a, b;
+    for (int u = 0; u < kUnits; ++u)
+      if (u * n / kUnits == i) unit(u);
+  }
+  __device__ __forceinline__ void finish() {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      a[i] = low_halves(x[2 * i], x[2 * i + 1]);
-      b[i] = high_halves(x[2 * i], x[2 * i + 1]);
-    }
-    const int piece = (token % P / 8 ^ S::fv(d)) * 16;  // (the same for d + 1)
-    put(at + d * (P * 2) + piece, a);
-    put(at + (d + 1) * (P * 2) + piece, b);
+    for (int u = 0; u < kUnits; ++u) unit(u);
   }
   __device__ __forceinline__ void start(const AttendCall& a, const Pages& pages, int h, uint32_t st, int w) {
     page_of = pages;
@@ -122,35 +151,34 @@ struct Mx4Stages {
     to = st;
     wave = w;
   }
+  // the first stage of LDS takes the first keys, the second one their values and the next keys
   __device__ __forceinline__ void begin(int key, int key_end, int32_t by) {
-    const int page = page_at(key);
-    page_v = page_at(key + S::KEYS);
-    load_keys(page);
-    load_values(page);
-    put_keys();
+    page_v = page_at(key);
+    page_k = page_at(key + S::KEYS);
+    copy(page_v, page_v, share(0));
+    copy(page_k, page_v, share(1));
+    wait_loads<0>();
+    now = 0;
+    read();
+#pragma unroll
+    for (int i = 0; i < KP; ++i) put_keys(i);
     to += by;
-    load_keys(page_v);
-    put_values();
-    put_keys();
-    page_k = page_at(key + 2 * S::KEYS);
-    read_next(key, key_end);
-    page_k = page_at(key + 3 * S::KEYS);
-    barrier();
-  }
-  // the values of the stage behind the one at `key` and the keys behind those
-  __device__ __forceinline__ void read_next(int key, int key_end) {
-    if (key + S::KEYS < key_end) load_values(page_v);
-    if (key + 2 * S::KEYS < key_end) load_keys(page_k);
+    now = 1;
+    finish();
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
     page_v = page_k;
+    page_k = page_at(key + 2 * S::KEYS);
+    copy_next(key + S::KEYS, key_end);
+    barrier();
   }
-  // in front of the work on the stage at `key`: it is there, the next one is written
+  // in front of the work on the stage at `key`, which is there: the next one's codes are
+  // there too, and those behind them are copied (what is converted past the end is not used)
   __device__ __forceinline__ void turn(int key, int key_end, int32_t by) {
+    wait_loads<0>();
     barrier();
     to += by;
-    if (key + S::KEYS < key_end) put_values();
-    if (key + 2 * S::KEYS < key_end) put_keys();
-    read_next(key + S::KEYS, key_end);
-    page_k = page_at(key + 4 * S::KEYS);
+    now ^= 1;
+    copy_next(key + 2 * S::KEYS, key_end);
   }
 };
 
@@ -348,7 +376,7 @@ __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       if ((i == 0) != turn) {
-        if (cut.many) many_rows<bf16_t, D, P>(a, cut, L, tid, wave, Mx4Stages<D, P>{}, finish);
+        if (cut.many) many_rows<bf16_t, D, P>(a, cut, L, tid, wave, Mx4Stages<D, P>{L.u.many.shares}, finish);
       } else {
         if (cut.line) few_rows();
       }
