@@ -52,6 +52,10 @@ struct Mx4Stages {
   uint32_t to;
   int wave, now, page_k, page_v;  // share that is converted next; pages to be copied next
   uint32_t k[KP], ke, v[2][D / 32], ve[2], x[8];
+  // where the lane reads a share and writes a stage, two places to a register (the loop has
+  // few left: places worked out in it cost as many instructions as the conversion, kept apart they
+  // are spilled): codes and exponent of keys, of values; its piece of a key, of a value
+  uint32_t of_keys, of_values, puts;
 
   __device__ __forceinline__ int page_at(int key) const {
     bool bad;
@@ -60,7 +64,7 @@ struct Mx4Stages {
   __device__ __forceinline__ const Mx4Share<D>& share(int which) const { return shares[which * kWaves + wave]; }
   // copies keys of one page and values of another into a share, without waiting
   __device__ __forceinline__ void copy(int key_page, int value_page, const Mx4Share<D>& s) const {
-    const int lane = threadIdx.x & 63, slot = 8 * wave % P;
+    const int lane = thread_index() & 63, slot = 8 * wave % P;
     const char *kb = kh + key_page * phys_bytes, *vb = vh + value_page * phys_bytes;
     // (m0 and its wait states as in copy_to_lds)
     if (lane < D / 2) {
@@ -84,47 +88,53 @@ struct Mx4Stages {
     page_v = page_k;
     page_k = page_at(key + 2 * S::KEYS);
   }
+  __device__ __forceinline__ void places() {
+    const int lane = thread_index() & 63, part = lane / (D / 32) & 15;
+    of_keys = lane * (D / 16) | (lane / 8 * (D / 32) + lane % 8 * (D / 8) / 32) << 16;
+    of_values = part * (D / 8) | (lane / 16) % (D / 32) * 4 << 16;
+    const int key = 8 * wave + lane / 8, row = key % 32, token = 8 * wave % 32, d = 2 * lane % D;
+    const int at_key = key / 32 * S::TILE + row * (D * 2) + (lane % 8 * KP ^ S::fk(row)) * 16;
+    const int at_value = 8 * wave / 32 * S::TILE + token / P * (D * P * 2) + d * (P * 2) + (token % P / 8 ^ S::fv(d)) * 16;
+    static_assert(S::NB * S::TILE <= 1 << 16, "places within a stage's keys, or values, have 16 bits");
+    puts = at_key | at_value << 16;
+    asm volatile("" : "+v"(of_keys), "+v"(of_values), "+v"(puts));  // kept as they are
+  }
   // the lane's part of the share
   __device__ __forceinline__ void read() {
-    const Mx4Share<D>& s = share(now);
-    const int lane = threadIdx.x & 63, part = lane / (D / 32) & 15;
+    const uint32_t s = lds_address(&share(now));
+    auto word = [](uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)at; };
+    const uint32_t at_k = s + (of_keys & 0xffff), at_v = s + 4 * D + (of_values & 0xffff);
 #pragma unroll
-    for (int i = 0; i < KP; ++i) k[i] = *reinterpret_cast<const uint32_t*>(s.codes[0] + lane * (D / 16) + 4 * i);
-    ke = (uint8_t)s.exps[0][lane / 8 * (D / 32) + lane % 8 * (D / 8) / 32];
+    for (int i = 0; i < KP; ++i) k[i] = word(at_k + 4 * i);
+    ke = *(const __attribute__((address_space(3))) uint8_t*)(uintptr_t)(s + 8 * D + (of_keys >> 16));
     // elements 2 lane, 2 lane + 1 of eight tokens
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        v[t][i] = *reinterpret_cast<const uint32_t*>(s.codes[1] + t * (2 * D) + part * (D / 8) + 4 * i);
-      ve[t] = *reinterpret_cast<const uint32_t*>(s.exps[1] + t * (D / 8) + (lane / 16) % (D / 32) * 4);
+      for (int i = 0; i < D / 32; ++i) v[t][i] = word(at_v + t * (2 * D) + 4 * i);
+      ve[t] = word(s + 8 * D + D / 4 + (of_values >> 16) + t * (D / 8));
     }
   }
   static __device__ __forceinline__ void put(uint32_t at, u32x4 y) {
     *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = y;
   }
   __device__ __forceinline__ void put_keys(int i) const {
-    const int lane = threadIdx.x & 63, key = 8 * wave + lane / 8, row = key % 32;
-    put(to + key / 32 * S::TILE + row * (D * 2) + ((lane % 8 * KP + i) ^ S::fk(row)) * 16,
-        mx4_piece<bf16_t>(k[i], mx4_scale((int)ke)));
+    // (a lane's pieces are neighbours, the first of even number: their places differ in one bit)
+    put(to + ((puts & 0xffff) ^ 16 * i), mx4_piece<bf16_t>(k[i], mx4_scale((int)ke)));
   }
   __device__ __forceinline__ void convert_values(int t, int e) {
-    const int byte = (threadIdx.x & 63) % (D / 32) * 8;
     // (a scale's bits below its exponent field, and its sign, do not count)
     const float scale = __uint_as_float(e < 3 ? ve[t] << (23 - 8 * e) : ve[t] >> 1);
-    const uint32_t w = v[t][e * (D / 32) / 4] >> byte;
+    const uint32_t w = v[t][e * (D / 32) / 4] >> (of_keys * (128 / D) & (D / 32 - 1) * 8);  // byte lane % (D / 32)
     x[4 * t + e] = e * (D / 32) % 4 ? mx4_bf16<2>(w, scale) : mx4_bf16<0>(w, scale);
   }
   __device__ __forceinline__ void put_values(int high) const {
-    const int lane = threadIdx.x & 63, token = 8 * wave % 32, d = 2 * lane;
-    if (d >= D) return;
     u32x4 y;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       y[i] = high ? high_halves(x[2 * i], x[2 * i + 1]) : low_halves(x[2 * i], x[2 * i + 1]);
-    put(to + S::NB * S::TILE + 8 * wave / 32 * S::TILE + token / P * (D * P * 2) + (d + high) * (P * 2) +
-            (token % P / 8 ^ S::fv(d)) * 16,  // (the same for d + 1)
-        y);
+    // (element d + 1 has the order of pieces of element d; for d 64 two lanes write the same)
+    put(to + S::NB * S::TILE + (puts >> 16) + high * (P * 2), y);
   }
   // the conversion in kUnits units
   static constexpr int kUnits = 11 + KP;
@@ -150,6 +160,7 @@ struct Mx4Stages {
     vh = (const char*)a.vc + h * kBlock;
     to = st;
     wave = w;
+    places();
   }
   // the first stage of LDS takes the first keys, the second one their values and the next keys
   __device__ __forceinline__ void begin(int key, int key_end, int32_t by) {
