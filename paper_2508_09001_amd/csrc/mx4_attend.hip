@@ -214,9 +214,10 @@ __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
 
   // The rows from rho0 on (nr of them) with the keys of [key_begin, key_end), this
   // wavefront's share of them; results into LDS.
-  auto tile_of = [&](auto row_tiles, const Seq& s, int b, int h, int rho0, int nr, int key_begin, int key_end) {
+  auto tile_of = [&](auto row_tiles, const Seq& s, int b, int h, int rho0, int nr, int begin, int end) {
     constexpr int NR = decltype(row_tiles)::value;
     const int lane = thread_index() & 63;
+    const int key_begin = __builtin_amdgcn_readfirstlane(begin), key_end = __builtin_amdgcn_readfirstlane(end);
     const Pages page_of{a.pt + (int64_t)b * a.max_pages, max((s.end + P - 1) / P - 1, 0), a.num_phys};
     const char* kh = (const char*)a.kc + h * kBlock;
     const char* vh = (const char*)a.vc + h * kBlock;
@@ -230,54 +231,86 @@ __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
       rows.start(n, (const T*)a.q + (int64_t)(s.run.row + r / a.G) * a.q_stride + (int64_t)(h * a.G + r % a.G) * D,
                  rho < s.rows, lane);
     }
-    const int all_see = min(s.run.pos + rho0 / a.G, s.end - 1);  // last token that every row sees
+    // last token that every row sees
+    const int all_see = __builtin_amdgcn_readfirstlane(min(s.run.pos + rho0 / a.G, s.end - 1));
     const Mx4Places<D, P> at(lane);
-    // loads a tile; which of its halves lie in pages that are not mapped
-    auto load = [&](Mx4Tile<D>& x, int key) {
-      uint32_t bits = 0;
+    // places of a tile's halves in the pool; which of them lie in pages that are not mapped
+    struct Halves {
+      int64_t page[2];
+      uint32_t bad;
+    };
+    auto halves = [&](int key) {
+      Halves f;
+      f.bad = 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         bool bad;
-        const int64_t page = page_of((key + 16 * t) / P, bad) * phys_bytes;
-        bits |= (uint32_t)bad << t;
-        at.load(x, t, kh + page, vh + page, (key + 16 * t) % P);
+        f.page[t] = page_of((key + 16 * t) / P, bad) * phys_bytes;
+        f.bad |= (uint32_t)bad << t;
       }
-      return bits;
+      return f;
     };
-    auto work = [&](Mx4Tile<D>& x, int key, uint32_t bad) {
+    const int last = (key_end - 1) / 32 * 32;  // (tiles begin at whole ones)
+    constexpr bool ONCE = NR == 1;  // (most often the only tile of these keys)
+    constexpr int kNext = 32 * kWaves;
+    // The tile at `key`, and into its registers the one two tiles on as soon as they
+    // are free: keys after the first product, values after the second.  (Always a tile, if need
+    // be the last one again: what is on its way can be waited for in part only where
+    // its number does not depend on a branch.)
+    Halves ahead;  // of the tile two on
+    auto work = [&](Mx4Tile<D>& x, uint32_t& bad, int key) {
       const bool clean = !bad && key + 31 <= all_see;
-      if (!clean) {
-        const int first = key + 4 * (lane >> 4);
+      const int first = key + 4 * (lane >> 4);
+      const Halves next = ahead;
+      ahead = halves(min(key + 3 * kNext, last));
+      if (!clean)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           x.ve[t] = live_exponents(x.ve[t], bad >> t & 1 ? 0 : s.end - (first + 16 * t));
-      }
-      rows.step(x, [&](int n, f32x4(&sc)[2]) {
-        if (clean) return;
-        const int first = key + 4 * (lane >> 4);
+      rows.step(
+          x,
+          [&](int n, f32x4(&sc)[2]) {
+            if (clean) return;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (first + 16 * t + e > lim[n] || (bad >> t & 1)) sc[t][e] = -INFINITY;
-      });
+              for (int e = 0; e < 4; ++e)
+                if (first + 16 * t + e > lim[n] || (bad >> t & 1)) sc[t][e] = -INFINITY;
+          },
+          [&]() {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) at.template load_keys<ONCE>(x, t, kh + next.page[t], 16 * t % P);
+            __builtin_amdgcn_sched_barrier(0);
+          },
+          [&]() {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) at.template load_values<ONCE>(x, t, vh + next.page[t], 16 * t % P);
+          });
+      bad = next.bad;
     };
-    constexpr int kNext = 32 * kWaves;
     int key = key_begin + wave * 32;
     if (key < key_end) {
       Mx4Tile<D> x, y;
-      uint32_t bx = load(x, key), by = 0;
+      uint32_t bx, by;
+      auto load = [&](Mx4Tile<D>& z, int key) {
+        const Halves f = halves(key);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          at.template load_keys<ONCE>(z, t, kh + f.page[t], 16 * t % P);
+          at.template load_values<ONCE>(z, t, vh + f.page[t], 16 * t % P);
+        }
+        return f.bad;
+      };
+      bx = load(x, key);
+      by = load(y, min(key + kNext, last));
+      ahead = halves(min(key + 2 * kNext, last));
       for (;;) {
-        const bool more = key + kNext < key_end;
-        if (more) by = load(y, key + kNext);
-        work(x, key, bx);
-        if (!more) break;
-        key += kNext;
-        const bool again = key + kNext < key_end;
-        if (again) bx = load(x, key + kNext);
-        work(y, key, by);
-        if (!again) break;
-        key += kNext;
+        work(x, bx, key);
+        if ((key += kNext) >= key_end) break;
+        work(y, by, key);
+        if ((key += kNext) >= key_end) break;
       }
     }
     // results, for the join of the wavefronts

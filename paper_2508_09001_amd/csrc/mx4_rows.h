@@ -34,7 +34,7 @@ struct Mx4Tile {
 // Where a lane's pieces of 16 tokens lie behind the first one's place in the page.
 template <int D, int P>
 struct Mx4Places {
-  int k, v, ke, ve;
+  uint32_t k, v, ke, ve;  // (unsigned: added to a scalar address by the load itself)
   __device__ __forceinline__ explicit Mx4Places(int lane) {
     const int r = lane & 15, quarter = lane >> 4;
     k = r * (D / 2) + quarter * (D / 8);
@@ -42,28 +42,27 @@ struct Mx4Places {
     ke = P * D / 2 + r * (D / 32) + quarter * (D / 32) / 4;
     ve = P * D / 2 + (quarter * (D / 32) + r * (D / 16) / 32) * 4;
   }
-  // half t of a tile: 16 tokens from `slot` on of a page whose keys and values are at kb, vb
-  __device__ __forceinline__ void load(Mx4Tile<D>& x, int t, const char* kb, const char* vb, int slot) const {
-    const int codes = slot * (D / 2), exps = slot * (D / 32);
-    if constexpr (D == 128) {
-      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-      const u32x4 a = *reinterpret_cast<const u32x4*>(kb + (k + codes));
-      const u32x4 b = *reinterpret_cast<const u32x4*>(vb + (v + codes));
+  // keys, or values, of half t of a tile: 16 tokens from `slot` on of the page at `block`.
+  // ONCE: not kept in the caches.
+  template <bool ONCE>
+  __device__ __forceinline__ void load_keys(Mx4Tile<D>& x, int t, const char* block, int slot) const {
+    piece<ONCE>(x.k[t], block + slot * (D / 2) + k);
+    x.ke[t] = *reinterpret_cast<const uint8_t*>(block + slot * (D / 32) + ke);
+  }
+  template <bool ONCE>
+  __device__ __forceinline__ void load_values(Mx4Tile<D>& x, int t, const char* block, int slot) const {
+    piece<ONCE>(x.v[t], block + slot * (D / 2) + v);
+    x.ve[t] = *reinterpret_cast<const uint32_t*>(block + slot * (D / 32) + ve);
+  }
+  template <bool ONCE>
+  static __device__ __forceinline__ void piece(uint32_t (&to)[D / 32], const char* from) {
+    typedef uint32_t words __attribute__((ext_vector_type(D / 32)));
+    const words* p = reinterpret_cast<const words*>(from);
+    words w;
+    if constexpr (ONCE) w = __builtin_nontemporal_load(p);
+    else w = *p;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x.k[t][i] = a[i];
-        x.v[t][i] = b[i];
-      }
-    } else {
-      const uint2 a = *reinterpret_cast<const uint2*>(kb + (k + codes));
-      const uint2 b = *reinterpret_cast<const uint2*>(vb + (v + codes));
-      x.k[t][0] = a.x;
-      x.k[t][1] = a.y;
-      x.v[t][0] = b.x;
-      x.v[t][1] = b.y;
-    }
-    x.ke[t] = *reinterpret_cast<const uint8_t*>(kb + (ke + exps));
-    x.ve[t] = *reinterpret_cast<const uint32_t*>(vb + (ve + exps));
+    for (int i = 0; i < D / 32; ++i) to[i] = w[i];
   }
 };
 
@@ -135,9 +134,11 @@ struct Mx4Rows {
   }
 
   // The tile's keys and values with the rows.  hide(n, s): -inf for scores that do not
-  // count, s[t][e] that of the lane's row and token 16 t + 4 (lane / 16) + e.
-  template <typename Hide>
-  __device__ __forceinline__ void step(const Mx4Tile<D>& x, Hide&& hide) {
+  // count, s[t][e] that of the lane's row and token 16 t + 4 (lane / 16) + e.  keys_done, values_done:
+  // the tile's keys, or values, are no longer needed.
+  template <typename Hide, typename KeysDone, typename ValuesDone>
+  __device__ __forceinline__ void step(const Mx4Tile<D>& x, Hide&& hide, KeysDone&& keys_done,
+                                       ValuesDone&& values_done) {
     f32x4 s[NR][2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -157,6 +158,7 @@ struct Mx4Rows {
             s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[n][term][i], s[n][t], 0, 0, 0);
       }
     }
+    keys_done();
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       hide(n, s[n]);
@@ -240,6 +242,7 @@ struct Mx4Rows {
                                                                       acc[n][2 * j + 1], 0, 0, 0);
         }
     }
+    values_done();
   }
 
   // A row's outputs that the lane holds: f(d, o) for pieces of four elements from d on.

@@ -90,13 +90,16 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
   const Mx4Places<D, P> at(lane);
   const char* kh = (const char*)a.kc + h * kBlock;
   const char* vh = (const char*)a.vc + h * kBlock;
-  auto load = [&](Mx4Tile<D>& x, int ch) {
+  auto block = [&](int ch, int t) {
+    return (int64_t)__builtin_amdgcn_readfirstlane(L.list.phys[ch * PT + (PT == 2 ? t : 0)]) * (kBlock * g.hk);
+  };
+  auto load_keys = [&](Mx4Tile<D>& x, int ch) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int64_t page = (int64_t)__builtin_amdgcn_readfirstlane(L.list.phys[ch * PT + (PT == 2 ? t : 0)]) *
-                           (kBlock * g.hk);
-      at.load(x, t, kh + page, vh + page, PT == 2 ? 0 : 16 * t);
-    }
+    for (int t = 0; t < 2; ++t) at.template load_keys<false>(x, t, kh + block(ch, t), PT == 2 ? 0 : 16 * t);
+  };
+  auto load_values = [&](Mx4Tile<D>& x, int ch) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) at.template load_values<false>(x, t, vh + block(ch, t), PT == 2 ? 0 : 16 * t);
   };
   auto work = [&](Mx4Tile<D>& x, int ch) {
     int live[2], mask[2];  // of the lane's four tokens of each half
@@ -110,27 +113,37 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
     if (cut)
 #pragma unroll
       for (int t = 0; t < 2; ++t) x.ve[t] = live_exponents(x.ve[t], live[t]);
-    rows.step(x, [&](int n, f32x4(&s)[2]) {
-      if (!cut && wave_ballot(max(mask[0], mask[1]) >= thr[n]) == 0) return;
+    rows.step(
+        x,
+        [&](int n, f32x4(&s)[2]) {
+          if (!cut && wave_ballot(max(mask[0], mask[1]) >= thr[n]) == 0) return;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+          for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e >= live[t] || mask[t] >= thr[n]) s[t][e] = -INFINITY;
-    });
+            for (int e = 0; e < 4; ++e)
+              if (e >= live[t] || mask[t] >= thr[n]) s[t][e] = -INFINITY;
+        },
+        [] {}, [] {});
   };
   if (wt < nch) {
     Mx4Tile<D> x, y;
     int ch = wt;
-    load(x, ch);
+    load_keys(x, ch);
+    load_values(x, ch);
     for (;;) {
       const bool more = ch + NT < nch;
-      if (more) load(y, ch + NT);
+      if (more) {
+        load_keys(y, ch + NT);
+        load_values(y, ch + NT);
+      }
       work(x, ch);
       if (!more) break;
       ch += NT;
       const bool again = ch + NT < nch;
-      if (again) load(x, ch + NT);
+      if (again) {
+        load_keys(x, ch + NT);
+        load_values(x, ch + NT);
+      }
       work(y, ch);
       if (!again) break;
       ch += NT;
