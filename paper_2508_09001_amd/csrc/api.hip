@@ -323,8 +323,12 @@ retro_status retro_decode_attend(const retro_dims* dims, int32_t step, const voi
   float* l_ws = ws_at(workspace, g.ws_lpart);
   const bool mx4 = retro::is_mx4(g);
   if (mx4 && !aligned16({q_window, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
+  if (mx4 && !aligned16({o_part})) return RETRO_EINVAL;
   const Geometry ga = mx4 ? retro::mx4_window_geometry(g) : retro::attend_geometry(g);
-  hipError_t e = mx4 ? retro::launch_mx4_window(ga, step, q_window, *cache, *sel, o_ws, l_ws, s)
+  if (mx4 && ga.n_splits == 1)
+    return from_hip(retro::launch_mx4_window(ga, step, q_window, *cache, *sel, nullptr, nullptr, o_part,
+                                             lse_part, s));
+  hipError_t e = mx4 ? retro::launch_mx4_window(ga, step, q_window, *cache, *sel, o_ws, l_ws, nullptr, nullptr, s)
                      : retro::launch_attend(ga, step, q_window, *cache, *sel, nullptr, o_ws, l_ws,
                                             (char*)workspace + g.ws_dummy, s);
   if (e == hipSuccess)

@@ -25,10 +25,12 @@ inline bool is_mx4(const Geometry& g) { return (g.flags & RETRO_FLAG_KV_MX4) != 
 
 // Attention of the window over the selected pages (mx4_window.hip): launch_attend's
 // arguments and partials, with the split of mx4_window_geometry(g), which the combine of
-// the partials takes too.
+// the partials takes too; or, with o_out and l_out (a single split), launch_combine_merge's
+// results of mode 0.
 Geometry mx4_window_geometry(const Geometry& g);
 hipError_t launch_mx4_window(const Geometry& g, int step, const void* q_window, const retro_kv_cache& c,
-                             const retro_selection& sel, float* o_ws, float* l_ws, hipStream_t s);
+                             const retro_selection& sel, float* o_ws, float* l_ws, float* o_out, float* l_out,
+                             hipStream_t s);
 
 constexpr int mx4_block_bytes(int P, int D) { return P * D / 2 + P * D / 32; }
 

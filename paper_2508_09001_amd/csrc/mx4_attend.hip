@@ -71,14 +71,14 @@ struct Mx4Stages {
       const char* from = (lane < D / 4 ? kb : vb) + (slot * (D / 2) + (lane & (D / 4 - 1)) * 16);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off"
                    :
-                   : "s"(lds_address(s.codes)), "v"(from)
+                   : "s"(__builtin_amdgcn_readfirstlane(lds_address(s.codes))), "v"(from)
                    : "memory");
     }
     if (lane < D / 8) {
       const char* from = (lane < D / 16 ? kb : vb) + (P * D / 2 + slot * (D / 32) + (lane & (D / 16 - 1)) * 4);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dword %1, off"
                    :
-                   : "s"(lds_address(s.exps)), "v"(from)
+                   : "s"(__builtin_amdgcn_readfirstlane(lds_address(s.exps))), "v"(from)
                    : "memory");
     }
   }
@@ -314,7 +314,6 @@ __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
       }
     }
     // results, for the join of the wavefronts
-    barrier();
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const int r = 16 * n + (lane & 15);
@@ -370,17 +369,17 @@ __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
         for (int i = tid; i < nr * (D / 4); i += kThreads) {
           const int row = i / (D / 4), d = i % (D / 4) * 4;
           float m = -INFINITY;
-  #pragma unroll
+#pragma unroll
           for (int w = 0; w < kWaves; ++w) m = fmaxf(m, L.m[w][row]);
           const float mu = m == -INFINITY ? 0.f : m;
           float l = 0.f;
           f32x4 o{0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
           for (int w = 0; w < kWaves; ++w) {
             const float e = __builtin_amdgcn_exp2f((L.m[w][row] - mu) * c);
             const f32x4 x = *reinterpret_cast<const f32x4*>(&L.u.o[w][row][d]);
             l = __builtin_fmaf(e, L.l[w][row], l);
-  #pragma unroll
+#pragma unroll
             for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e, x[j], o[j]);
           }
           if (whole) {

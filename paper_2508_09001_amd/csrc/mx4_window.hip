@@ -1,12 +1,11 @@
 // Attention of the retrospective window's queries over the selected pages of a cache in
-// 4 bits: one (sequence, KV head, split, row group) per workgroup, its eight wavefronts
-// SIDE side by side over the rows (RT tiles of 16 each) and NT = 8 / SIDE over the
-// split's chunks of 32 tokens (wt, wt + NT, ...), which they read straight from the pages
+// 4 bits: one (sequence, KV head, split, row group of RT tiles of 16) per workgroup, whose
+// eight wavefronts take the split's chunks of 32 tokens in turn, straight from the pages
 // into registers (mx4_rows.h), the next chunk's codes under way while one is worked on.
 // A past query takes the pages with M_p < tau (Alg. 2, "Retrospective Mask" paragraph).
 // The wavefronts' states are merged through LDS; the partial outputs and log-normalisers of
 // a split go to the workspace as those of the other attention kernels, for the same
-// combine launch.
+// combine launch, or where there is one split to the results themselves.
 #include <algorithm>
 
 #include "mx4_rows.h"
@@ -15,14 +14,15 @@ namespace retro {
 namespace {
 
 constexpr int kWaves = 8;
-constexpr int kListPages = 1024;  // pages of a split (list in LDS)
+constexpr int kListPages = 512;  // pages of a split (list in LDS)
 
 struct WindowCall {
   Geometry g;
   int step;
   const void *q, *kc, *vc;
   const int32_t *pt, *seq_lens, *sel, *msk, *nsel;
-  float *o_ws, *l_ws;
+  float *o_ws, *l_ws;   // partials, or
+  float *o_out, *l_out;  // the results, of a single split
 };
 
 template <int D, int RT>
@@ -35,14 +35,13 @@ struct WindowLds {
   float m[kWaves][RT * 16], l[kWaves][RT * 16];
 };
 
-template <typename T, int D, int P, int RT, int SIDE>
-__global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
-  constexpr int NT = kWaves / SIDE, PT = 32 / P;  // pages of a chunk
+template <typename T, int D, int P, int RT>
+__global__ void __launch_bounds__(64 * kWaves, RT == 1 && sizeof(T) == 2 ? 4 : 2) mx4_window_kernel(WindowCall a) {
+  constexpr int PT = 32 / P;  // pages of a chunk
   __shared__ __attribute__((aligned(16))) WindowLds<D, RT> L;
   const Geometry& g = a.g;
   const int tid = thread_index(), lane = tid & 63, ln16 = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = wave % SIDE, wt = wave / SIDE;
   // row group fastest: a split's row groups run at the same time on one XCD
   int u = xcd_remap(blockIdx.x, gridDim.x);
   const int rg = u % g.n_rgroups;
@@ -53,18 +52,15 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
 
   // the split's pages
   const int first = split * g.pages_per_split;
-  const int np = max(0, min(min(g.pages_per_split, a.nsel[bh] - first), g.k_max - first));
-  const int nch = (np + PT - 1) / PT;
-  const int seq_len = a.seq_lens[b];
-  for (int i = tid; i < nch * PT; i += 64 * kWaves) {
-    int lp = -1, m = 0, phys = -1;
-    if (i < np) {
-      const int64_t o = (int64_t)bh * g.k_max + first + i;
-      lp = a.sel[o];
-      m = a.msk[o];
-      if (lp >= 0 && lp < g.max_pages) phys = a.pt[(int64_t)b * g.max_pages + lp];
-    }
-    const bool ok = phys >= 0 && phys < g.num_phys;
+  const int rows_of_list = max(0, min(g.pages_per_split, g.k_max - first));
+  const int np = min(rows_of_list, max(sload(a.nsel + bh) - first, 0));
+  const int nch = (np + PT - 1) / PT, seq_len = sload(a.seq_lens + b);
+  for (int i = tid; i < (rows_of_list + PT - 1) / PT * PT; i += 64 * kWaves) {
+    // (entries behind the selected ones are read too, so as not to wait for their number)
+    const int64_t o = (int64_t)bh * g.k_max + first + min(i, rows_of_list - 1);
+    const int lp = a.sel[o], m = a.msk[o];
+    const int phys = lp >= 0 && lp < g.max_pages ? a.pt[(int64_t)b * g.max_pages + lp] : -1;
+    const bool ok = i < np && phys >= 0 && phys < g.num_phys;
     // a page without stored tokens reads page 0 of the pool; none of it is used
     L.list.phys[i] = ok ? phys : 0;
     L.list.len[i] = ok ? max(0, min(P, seq_len - lp * P)) : 0;
@@ -78,8 +74,8 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
   int thr[RT];
 #pragma unroll
   for (int n = 0; n < RT; ++n) {
-    const int lt = wr * RT + n, rho = (rg * g.tiles_per_group + lt) * 16 + ln16;
-    const bool live = lt < g.tiles_per_group && rho < g.R;
+    const int rho = (rg * RT + n) * 16 + ln16;
+    const bool live = rho < g.R;
     const int r = live ? rho / g.G : 0, gq = live ? rho - r * g.G : 0, tau = a.step - W + r;
     thr[n] = (live && tau >= 0) ? (r == W ? 0x7fffffff : tau) : (int)0x80000000;
     rows.start(n, (const T*)a.q + (((int64_t)b * (W + 1) + r) * g.hq + (int64_t)h * g.G + gq) * D, live, lane);
@@ -101,7 +97,11 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) at.template load_values<false>(x, t, vh + block(ch, t), PT == 2 ? 0 : 16 * t);
   };
+  // Chunks are under way in two sets of registers in turn, or, with one tile of rows (and so
+  // two workgroups on a compute unit), into the one as its keys, and then its values, are done with.
+  constexpr int DEPTH = RT == 1 ? 1 : 2;
   auto work = [&](Mx4Tile<D>& x, int ch) {
+    [[maybe_unused]] const int next = min(ch + kWaves, nch - 1);
     int live[2], mask[2];  // of the lane's four tokens of each half
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -123,30 +123,40 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
             for (int e = 0; e < 4; ++e)
               if (e >= live[t] || mask[t] >= thr[n]) s[t][e] = -INFINITY;
         },
-        [] {}, [] {});
+        [&]() {
+          if constexpr (DEPTH == 1) load_keys(x, next);
+        },
+        [&]() {
+          if constexpr (DEPTH == 1) load_values(x, next);
+        });
   };
-  if (wt < nch) {
-    Mx4Tile<D> x, y;
-    int ch = wt;
+  if (wave < nch) {
+    Mx4Tile<D> x;
+    int ch = wave;
     load_keys(x, ch);
     load_values(x, ch);
-    for (;;) {
-      const bool more = ch + NT < nch;
-      if (more) {
-        load_keys(y, ch + NT);
-        load_values(y, ch + NT);
+    if constexpr (DEPTH == 1) {
+      for (; ch < nch; ch += kWaves) work(x, ch);
+    } else {
+      Mx4Tile<D> y;
+      for (;;) {
+        const bool more = ch + kWaves < nch;
+        if (more) {
+          load_keys(y, ch + kWaves);
+          load_values(y, ch + kWaves);
+        }
+        work(x, ch);
+        if (!more) break;
+        ch += kWaves;
+        const bool again = ch + kWaves < nch;
+        if (again) {
+          load_keys(x, ch + kWaves);
+          load_values(x, ch + kWaves);
+        }
+        work(y, ch);
+        if (!again) break;
+        ch += kWaves;
       }
-      work(x, ch);
-      if (!more) break;
-      ch += NT;
-      const bool again = ch + NT < nch;
-      if (again) {
-        load_keys(x, ch + NT);
-        load_values(x, ch + NT);
-      }
-      work(y, ch);
-      if (!again) break;
-      ch += NT;
     }
   }
 
@@ -161,117 +171,104 @@ __global__ void __launch_bounds__(64 * kWaves) mx4_window_kernel(WindowCall a) {
   }
   __syncthreads();
   const int64_t part0 = ((int64_t)bh * g.n_splits + split) * g.R;
+  // where row rho's outputs go, in rows of d
+  auto place = [&](int rho) {
+    const int r = rho / g.G;
+    return a.o_out ? ((int64_t)b * (W + 1) + r) * g.hq + h * g.G + rho - r * g.G : part0 + rho;
+  };
+  float *const o_to = a.o_out ? a.o_out : a.o_ws, *const l_to = a.o_out ? a.l_out : a.l_ws;
 #pragma unroll
   for (int n = 0; n < RT; ++n) {
-    const int lt = wr * RT + n, row = (rg * g.tiles_per_group + lt) * 16 + ln16, rr = n * 16 + ln16;
+    const int rho0 = (rg * RT + n) * 16, rr = n * 16 + ln16;
     float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NT; ++w) M = fmaxf(M, L.m[w * SIDE + wr][rr]);
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, L.m[w][rr]);
     const float Mu = M == -INFINITY ? 0.f : M;
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < NT; ++w)
-      sum += L.l[w * SIDE + wr][rr] * __builtin_amdgcn_exp2f((L.m[w * SIDE + wr][rr] - Mu) * rows.c);
-    const float f = sum > 0.f ? __builtin_amdgcn_exp2f((rows.m[n] - Mu) * rows.c) / sum : 0.f;
-    // -inf for an empty sum; +inf (fminf skips NaN) for a NaN one, from NaN or infinite
-    // scores: the combine then makes the row NaN
-    if (wt == 0 && quarter == 0 && lt < g.tiles_per_group && row < g.R)
-      a.l_ws[part0 + row] = fminf(__builtin_fmaf(M, g.sm_scale, __log2f(sum) * kLn2), INFINITY);
-    if (n > 0) __syncthreads();  // the previous tiles have been read
+    for (int w = 0; w < kWaves; ++w)
+      sum += L.l[w][rr] * __builtin_amdgcn_exp2f((L.m[w][rr] - Mu) * rows.c);
+    // (a NaN sum, from NaN or infinite scores, makes the row NaN: here, or, with a
+    // log-normaliser of +inf, in the combine)
+    const float f = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f((rows.m[n] - Mu) * rows.c) / sum;
+    if (wave == 0 && quarter == 0 && rho0 + ln16 < g.R) {
+      const float z = __builtin_fmaf(M, g.sm_scale, __log2f(sum) * kLn2);
+      l_to[place(rho0 + ln16)] = a.o_out ? z : fminf(z, INFINITY);  // (fminf skips NaN)
+    }
+    if (n > 0) __syncthreads();  // the previous tile has been read
     rows.each(n, lane, [&](int d, f32x4 o) { *reinterpret_cast<f32x4*>(&L.o[wave][ln16][d]) = o * f; });
     __syncthreads();
     constexpr int VPR = D / 4;  // 16-byte pieces per row
-    // tile n of each of the SIDE row ranges: the NT wavefronts' rows added up
+    for (int e = tid; e < 16 * VPR; e += 64 * kWaves) {
+      const int rw = e / VPR, c4 = (e - rw * VPR) * 4;
+      f32x4 o = *reinterpret_cast<const f32x4*>(&L.o[0][rw][c4]);
 #pragma unroll
-    for (int r0 = 0; r0 < SIDE; ++r0) {
-      const int t0 = r0 * RT + n;
-      if (t0 >= g.tiles_per_group) break;  // uniform
-      const int row0 = (rg * g.tiles_per_group + t0) * 16;
-      for (int e = tid; e < 16 * VPR; e += 64 * kWaves) {
-        const int rw = e / VPR, c4 = (e - rw * VPR) * 4;
-        f32x4 o = *reinterpret_cast<const f32x4*>(&L.o[r0][rw][c4]);
-#pragma unroll
-        for (int w = 1; w < NT; ++w) o += *reinterpret_cast<const f32x4*>(&L.o[w * SIDE + r0][rw][c4]);
-        if (row0 + rw < g.R)
-          __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(a.o_ws + (part0 + row0 + rw) * D + c4));
-      }
+      for (int w = 1; w < kWaves; ++w) o += *reinterpret_cast<const f32x4*>(&L.o[w][rw][c4]);
+      if (rho0 + rw < g.R)
+        __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(o_to + place(rho0 + rw) * D + c4));
     }
   }
 }
 
-// tiles of 16 rows of a workgroup at most, and how its wavefronts share `tiles` of them:
-// RT each, SIDE side by side.  (fp32 rows have three times the operands: a tile each.)
-constexpr int most_tiles(int dtype) { return dtype == RETRO_BF16 ? 6 : 4; }
-int side_by_side(int dtype, int tiles) {
-  return dtype == RETRO_BF16 ? (tiles <= 3 ? 1 : 2) : (tiles == 1 ? 1 : tiles == 2 ? 2 : 4);
-}
-
-template <typename T, int D, int P, int RT, int SIDE>
+template <typename T, int D, int P, int RT>
 hipError_t go(const WindowCall& a, hipStream_t s) {
   const Geometry& g = a.g;
   const int64_t n = (int64_t)g.n_splits * g.n_rgroups * g.hk * g.batch;
-  mx4_window_kernel<T, D, P, RT, SIDE><<<(unsigned)n, 64 * kWaves, 0, s>>>(a);
+  mx4_window_kernel<T, D, P, RT><<<(unsigned)n, 64 * kWaves, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, int D, int P>
 hipError_t go_tiles(const WindowCall& a, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    switch (a.g.tiles_per_group) {
-      case 1: return go<T, D, P, 1, 1>(a, s);
-      case 2: return go<T, D, P, 2, 1>(a, s);
-      case 3: return go<T, D, P, 3, 1>(a, s);
-      case 4: return go<T, D, P, 2, 2>(a, s);
-      case 5:
-      case 6: return go<T, D, P, 3, 2>(a, s);
-      default: return hipErrorInvalidValue;
-    }
-  } else {
-    switch (a.g.tiles_per_group) {
-      case 1: return go<T, D, P, 1, 1>(a, s);
-      case 2: return go<T, D, P, 1, 2>(a, s);
-      case 3:
-      case 4: return go<T, D, P, 1, 4>(a, s);
-      default: return hipErrorInvalidValue;
-    }
+    if (a.g.tiles_per_group == 2) return go<T, D, P, 2>(a, s);
+    if (a.g.tiles_per_group == 3) return go<T, D, P, 3>(a, s);
   }
+  return a.g.tiles_per_group == 1 ? go<T, D, P, 1>(a, s) : hipErrorInvalidValue;
 }
 
 }  // namespace
 
+// One workgroup takes RT tiles of rows (fp32 rows, with three times the operands, one) and a
+// number of chunks that its wavefronts go through in `it` turns.  A turn takes 1.15, 2.0 and 2.9
+// us for RT 1, 2 and 3 (d 128), a workgroup's beginning and end 5.5, a further round of workgroups on
+// a compute unit 4 of these (1.5 for RT 1, whose workgroups are two at a time), the combine
+// 3.5 and more for more splits.  The choice for some shapes, in us, and others: 8 heads of
+// 68 rows, 128 pages, RT 1 in 4 splits 9.9 (RT 1 in 2 12.1, in 8 11.3; RT 2 in 8 11.2; RT 3, 6 tiles side by side, in 16 13.5);
+// 128 heads of 36 rows, 64 pages, RT 2 in one 14.5 (in two 19.4; RT 1 in one, with the combine that
+// it does not need, 19.9).
 Geometry mx4_window_geometry(const Geometry& g) {
+  static constexpr float kTurn[3] = {1.15f, 2.0f, 2.9f}, kRound[3] = {1.5f, 4.f, 4.f};
   Geometry x = g;
-  const int most = most_tiles(g.dtype);
-  x.n_rgroups = (g.row_tiles + most - 1) / most;
-  x.tiles_per_group = (g.row_tiles + x.n_rgroups - 1) / x.n_rgroups;
   x.stream = 1;
-  // the split count with the smallest time, counted in chunk iterations of a wavefront: rounds
-  // of workgroups times the iterations of one, plus three for its start and merge
-  const int nt = kWaves / side_by_side(g.dtype, x.tiles_per_group);
-  const int64_t heads = (int64_t)g.batch * g.hk * x.n_rgroups;
-  const int cap = compute_units(), cps_max = kListPages / g.chunk_pages;
-  int best = 0;
-  int64_t best_cost = 0;
-  for (int it = (std::min(g.chunks_max, cps_max) + nt - 1) / nt; it >= 1; --it) {
-    const int cps = std::min(it * nt, cps_max), ns = (g.chunks_max + cps - 1) / cps;
-    if (ns > g.n_splits) break;
-    const int64_t cost = (heads * ns + cap - 1) / cap * (it + 3);
-    if (best == 0 || cost < best_cost) {
-      best = ns;
-      best_cost = cost;
+  const int most = g.dtype == RETRO_BF16 ? 3 : 1, cap = compute_units(), cps_max = kListPages / g.chunk_pages;
+  float best = 0.f;
+  for (int rt = 1; rt <= std::min(most, g.row_tiles); ++rt) {
+    const int groups = (g.row_tiles + rt - 1) / rt;
+    for (int it = 1; it <= (std::min(g.chunks_max, cps_max) + kWaves - 1) / kWaves; ++it) {
+      const int cps = std::min(it * kWaves, cps_max), ns = (g.chunks_max + cps - 1) / cps;
+      if (ns > g.n_splits) continue;
+      const int64_t rounds = ((int64_t)g.batch * g.hk * groups * ns + cap - 1) / cap;
+      const float time = (float)(rounds * it) * kTurn[rt - 1] + (float)(rounds - 1) * kRound[rt - 1] +
+                         (ns > 1 ? 3.5f + 0.1f * (float)ns : 0.f);
+      if (best != 0.f && time >= best) continue;
+      best = time;
+      x.tiles_per_group = rt;
+      x.n_rgroups = groups;
+      x.chunks_per_split = (g.chunks_max + ns - 1) / ns;
     }
   }
-  if (best == 0) best = g.n_splits;
-  x.chunks_per_split = (g.chunks_max + best - 1) / best;
   x.n_splits = (g.chunks_max + x.chunks_per_split - 1) / x.chunks_per_split;
   x.pages_per_split = x.chunks_per_split * g.chunk_pages;
   return x;
 }
 
 hipError_t launch_mx4_window(const Geometry& g, int step, const void* q_window, const retro_kv_cache& c,
-                             const retro_selection& sel, float* o_ws, float* l_ws, hipStream_t s) {
-  const WindowCall a{g,          step,         q_window,         c.k_cache, c.v_cache, c.page_table, c.seq_lens,
-                     sel.selected, sel.mask, sel.num_selected, o_ws,      l_ws};
+                             const retro_selection& sel, float* o_ws, float* l_ws, float* o_out, float* l_out,
+                             hipStream_t s) {
+  const WindowCall a{g,           step,         q_window, c.k_cache,        c.v_cache, c.page_table,
+                     c.seq_lens,  sel.selected, sel.mask, sel.num_selected, o_ws,      l_ws,
+                     o_out,       l_out};
   auto with_page = [&](auto t, auto d) {
     return g.P == 16 ? go_tiles<decltype(t), decltype(d)::value, 16>(a, s)
                      : go_tiles<decltype(t), decltype(d)::value, 32>(a, s);
