@@ -108,7 +108,8 @@ typedef struct retro_dims {
                               == 0 select as usual.  0 or 1: every step selects.    */
 } retro_dims;
 
-/* The paged KV cache of one layer (Sec. 2.1; pages as in a vLLM-style pool).
+/* The paged KV cache of one layer (Sec. 2.1; pages as in a vLLM-style pool), in dtype; with
+ * RETRO_FLAG_KV_MX4 the pages of keys and values are in 4 bits instead.
  *   k_cache     [num_phys_pages][h_k][P][d]   dtype  key page, token-major
  *   v_cache     [num_phys_pages][h_k][d][P]   dtype  value page, stored transposed
  *                                                    (d-major) so that the token
@@ -576,9 +577,13 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
  *           turn, of a part the tokens in turn; exponents [P / 4][d / 32][4]
  * digest and the queries stay in dtype; a digest holds the minimum and maximum of what the
  * page's keys stand for, so that pages are scored as they will be attended.
- * retro_append_kv_rotary, retro_read_kv, retro_chunk_attend and retro_decode_attend take such dims, and so
- * do the calls that touch neither keys nor values (retro_select_pages, retro_copy_scores,
- * retro_merge_output_cache, retro_rotate_qk and the sizes); the others return RETRO_EUNSUPPORTED. */
+ * Every call takes such dims but retro_project_qkv_update and retro_step_attend_partials
+ * (RETRO_EUNSUPPORTED), with the semantics that it has for a cache whose keys and values are what
+ * the codes stand for; queries, keys and values that it is given, the outputs of attention,
+ * k_cache and v_cache have to be 16-byte aligned (RETRO_EINVAL).  retro_step is four or five
+ * launches then (the append, the scores, the selection, the attention, combine + merge), and
+ * retro_chunk_attend takes bf16 rows' weights for sequences of few rows as two bf16 halves and
+ * for the others as one, retro_decode_attend and retro_step as three, fp32 rows always as three. */
 
 /* Rows of the cache as keys and values: row j of sequence b, as `chunk` lays them out, is
  * the token at position start_pos[b] + j; k_out, v_out [n_rows][h_k][d] dtype (either may

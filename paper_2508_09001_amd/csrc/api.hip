@@ -164,6 +164,39 @@ retro_status check_ws(const Geometry& g, void* ws, size_t ws_bytes) {
 
 float* ws_at(void* ws, size_t off) { return reinterpret_cast<float*>((char*)ws + off); }
 
+// a call's steps in the cache's format
+hipError_t append_token(const Geometry& g, int step, const retro_kv_cache& cache, const void* k_new,
+                        const void* v_new, hipStream_t s) {
+  return retro::is_mx4(g) ? retro::launch_mx4_append_tokens(g, step, cache, 1, k_new, v_new, s)
+                          : retro::launch_append(g, step, cache, k_new, v_new, s);
+}
+Geometry attend_plan(const Geometry& g) {
+  return retro::is_mx4(g) ? retro::mx4_window_geometry(g) : retro::attend_geometry(g);
+}
+bool attend_ok(const Geometry& g, const retro_kv_cache* cache, const void* q_window) {
+  return !retro::is_mx4(g) || aligned16({q_window, cache->k_cache, cache->v_cache});
+}
+hipError_t attend_partials(const Geometry& g, const Geometry& ga, int step, const void* q_window,
+                           const retro_kv_cache& cache, const retro_selection& sel, const int32_t* sel_phys,
+                           void* ws, hipStream_t s) {
+  float *o_ws = ws_at(ws, g.ws_opart), *l_ws = ws_at(ws, g.ws_lpart);
+  return retro::is_mx4(g)
+             ? retro::launch_mx4_window(ga, step, q_window, cache, sel, o_ws, l_ws, nullptr, nullptr, s)
+             : retro::launch_attend(ga, step, q_window, cache, sel, sel_phys, o_ws, l_ws, (char*)ws + g.ws_dummy, s);
+}
+// PageSelect + UpdateAndBuildMask, or on a top-k reuse step Alg. 2 on the rows sel holds
+hipError_t select(const Geometry& g, int step, const void* q_cur, int64_t q_batch_stride,
+                  const retro_kv_cache& cache, const retro_selection& sel, void* ws, hipStream_t s) {
+  if (retro::reuse_step(g, step)) return retro::launch_reuse_mask(g, step, cache, sel, s);
+  float* scores = ws_at(ws, g.ws_scores);
+  if (retro::score_selects(g))
+    return retro::launch_score(g, q_cur, q_batch_stride, cache, nullptr, nullptr, scores, s, step, &sel,
+                               reinterpret_cast<int32_t*>((char*)ws + g.ws_sel));
+  hipError_t e = retro::launch_score(g, q_cur, q_batch_stride, cache, nullptr, nullptr, scores, s);
+  if (e == hipSuccess) e = retro::launch_topk_mask(g, step, scores, cache, sel, nullptr, s);
+  return e;
+}
+
 // retro_step's launch plan: scores, selection and attention in one launch
 // where every workgroup of it fits on the GPU at once and the caller did not
 // ask for a separate score launch
@@ -224,12 +257,12 @@ retro_status retro_prefill_kv(const retro_dims* dims, const retro_kv_cache* cach
   Geometry g;
   retro_status st = retro::make_geometry(dims, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || !k_src || !v_src) return RETRO_EINVAL;
   if (seq < 0 || seq >= g.batch || start_pos < 0 || n_tokens < 0) return RETRO_EINVAL;
   if ((int64_t)start_pos + n_tokens > (int64_t)g.max_pages * g.P) return RETRO_EINVAL;
-  return from_hip(retro::launch_prefill(g, *cache, seq, start_pos, n_tokens, k_src, v_src,
-                                        (hipStream_t)stream));
+  if (retro::is_mx4(g) && !aligned16({k_src, v_src, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
+  return from_hip((retro::is_mx4(g) ? retro::launch_mx4_prefill : retro::launch_prefill)(
+      g, *cache, seq, start_pos, n_tokens, k_src, v_src, (hipStream_t)stream));
 }
 
 retro_status retro_append_kv(const retro_dims* dims, int32_t step, const retro_kv_cache* cache,
@@ -237,9 +270,9 @@ retro_status retro_append_kv(const retro_dims* dims, int32_t step, const retro_k
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || !k_new || !v_new) return RETRO_EINVAL;
-  return from_hip(retro::launch_append(g, step, *cache, k_new, v_new, (hipStream_t)stream));
+  if (retro::is_mx4(g) && !aligned16({k_new, v_new, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
+  return from_hip(append_token(g, step, *cache, k_new, v_new, (hipStream_t)stream));
 }
 
 retro_status retro_append_kv_tokens(const retro_dims* dims, int32_t step,
@@ -248,12 +281,12 @@ retro_status retro_append_kv_tokens(const retro_dims* dims, int32_t step,
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || n_tokens < 0) return RETRO_EINVAL;
   if (n_tokens == 0) return RETRO_OK;
   if (!k_new || !v_new) return RETRO_EINVAL;
-  return from_hip(retro::launch_append_tokens(g, step, *cache, n_tokens, k_new, v_new,
-                                              (hipStream_t)stream));
+  if (retro::is_mx4(g) && !aligned16({k_new, v_new, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
+  return from_hip((retro::is_mx4(g) ? retro::launch_mx4_append_tokens : retro::launch_append_tokens)(
+      g, step, *cache, n_tokens, k_new, v_new, (hipStream_t)stream));
 }
 
 retro_status retro_update_kv(const retro_dims* dims, const retro_kv_cache* cache,
@@ -262,12 +295,13 @@ retro_status retro_update_kv(const retro_dims* dims, const retro_kv_cache* cache
   Geometry g;
   retro_status st = make_geometry(dims, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!cache_ok(cache) || n_tokens < 0) return RETRO_EINVAL;
   if (n_tokens == 0) return RETRO_OK;
   if (!k_upd || !v_upd) return RETRO_EINVAL;
   if (n_tokens > g.max_pages * g.P) return RETRO_EINVAL;
-  return from_hip(retro::launch_update_kv(g, *cache, n_tokens, k_upd, v_upd, (hipStream_t)stream));
+  if (retro::is_mx4(g) && !aligned16({k_upd, v_upd, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
+  return from_hip((retro::is_mx4(g) ? retro::launch_mx4_update_kv : retro::launch_update_kv)(
+      g, *cache, n_tokens, k_upd, v_upd, (hipStream_t)stream));
 }
 
 retro_status retro_project_qkv_update(const retro_dims* dims, const retro_kv_cache* cache,
@@ -296,17 +330,7 @@ retro_status retro_select_pages(const retro_dims* dims, int32_t step, const void
   if (st != RETRO_OK) return st;
   if (!q_cur || !cache_ok(cache) || !sel_ok(sel)) return RETRO_EINVAL;
   if ((st = check_ws(g, workspace, ws_bytes)) != RETRO_OK) return st;
-  hipStream_t s = (hipStream_t)stream;
-  if (retro::reuse_step(g, step))  // top-k reuse: Alg. 2 on the rows sel holds
-    return from_hip(retro::launch_reuse_mask(g, step, *cache, *sel, s));
-  float* scores = ws_at(workspace, g.ws_scores);
-  const int64_t qbs = (int64_t)g.hq * g.D;
-  if (retro::score_selects(g))
-    return from_hip(retro::launch_score(g, q_cur, qbs, *cache, nullptr, nullptr, scores, s, step, sel,
-                                        reinterpret_cast<int32_t*>((char*)workspace + g.ws_sel)));
-  hipError_t e = retro::launch_score(g, q_cur, qbs, *cache, nullptr, nullptr, scores, s);
-  if (e == hipSuccess) e = retro::launch_topk_mask(g, step, scores, *cache, *sel, nullptr, s);
-  return from_hip(e);
+  return from_hip(select(g, step, q_cur, (int64_t)g.hq * g.D, *cache, *sel, workspace, (hipStream_t)stream));
 }
 
 retro_status retro_decode_attend(const retro_dims* dims, int32_t step, const void* q_window,
@@ -318,22 +342,17 @@ retro_status retro_decode_attend(const retro_dims* dims, int32_t step, const voi
   if (st != RETRO_OK) return st;
   if (!q_window || !cache_ok(cache) || !sel_ok(sel) || !o_part || !lse_part) return RETRO_EINVAL;
   if ((st = check_ws(g, workspace, ws_bytes)) != RETRO_OK) return st;
+  if (!attend_ok(g, cache, q_window) || (retro::is_mx4(g) && !aligned16({o_part}))) return RETRO_EINVAL;
   hipStream_t s = (hipStream_t)stream;
-  float* o_ws = ws_at(workspace, g.ws_opart);
-  float* l_ws = ws_at(workspace, g.ws_lpart);
-  const bool mx4 = retro::is_mx4(g);
-  if (mx4 && !aligned16({q_window, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
-  if (mx4 && !aligned16({o_part})) return RETRO_EINVAL;
-  const Geometry ga = mx4 ? retro::mx4_window_geometry(g) : retro::attend_geometry(g);
-  if (mx4 && ga.n_splits == 1)
-    return from_hip(retro::launch_mx4_window(ga, step, q_window, *cache, *sel, nullptr, nullptr, o_part,
-                                             lse_part, s));
-  hipError_t e = mx4 ? retro::launch_mx4_window(ga, step, q_window, *cache, *sel, o_ws, l_ws, nullptr, nullptr, s)
-                     : retro::launch_attend(ga, step, q_window, *cache, *sel, nullptr, o_ws, l_ws,
-                                            (char*)workspace + g.ws_dummy, s);
+  const Geometry ga = attend_plan(g);
+  if (retro::is_mx4(g) && ga.n_splits == 1)
+    return from_hip(
+        retro::launch_mx4_window(ga, step, q_window, *cache, *sel, nullptr, nullptr, o_part, lse_part, s));
+  hipError_t e = attend_partials(g, ga, step, q_window, *cache, *sel, nullptr, workspace, s);
   if (e == hipSuccess)
-    e = retro::launch_combine_merge(ga, step, 0, o_ws, l_ws, sel->num_selected, nullptr, nullptr,
-                                    o_part, lse_part, nullptr, nullptr, nullptr, nullptr, s);
+    e = retro::launch_combine_merge(ga, step, 0, ws_at(workspace, g.ws_opart), ws_at(workspace, g.ws_lpart),
+                                    sel->num_selected, nullptr, nullptr, o_part, lse_part, nullptr, nullptr,
+                                    nullptr, nullptr, s);
   return from_hip(e);
 }
 
@@ -344,12 +363,11 @@ retro_status retro_decode_attend_partials(const retro_dims* dims, int32_t step,
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!q_window || !cache_ok(cache) || !sel_ok(sel)) return RETRO_EINVAL;
   if ((st = check_ws(g, workspace, ws_bytes)) != RETRO_OK) return st;
-  return from_hip(retro::launch_attend(retro::attend_geometry(g), step, q_window, *cache, *sel,
-                                       nullptr, ws_at(workspace, g.ws_opart), ws_at(workspace, g.ws_lpart),
-                                       (char*)workspace + g.ws_dummy, (hipStream_t)stream));
+  if (!attend_ok(g, cache, q_window)) return RETRO_EINVAL;
+  return from_hip(attend_partials(g, attend_plan(g), step, q_window, *cache, *sel, nullptr, workspace,
+                                  (hipStream_t)stream));
 }
 
 retro_status retro_step_attend_partials(const retro_dims* dims, int32_t step,
@@ -391,8 +409,7 @@ retro_status retro_attend_plan(const retro_dims* dims, int32_t selects, int32_t*
   if (!row_tiles || !splits) return RETRO_EINVAL;
   retro_status st = prepare(dims, 0, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
-  const Geometry ga = retro::attend_geometry(g, selects != 0);
+  const Geometry ga = retro::is_mx4(g) ? attend_plan(g) : retro::attend_geometry(g, selects != 0);
   *row_tiles = ga.stream ? ga.tiles_per_group : 0;
   *splits = ga.n_splits;
   return RETRO_OK;
@@ -403,7 +420,10 @@ retro_status retro_step_launches(const retro_dims* dims, int32_t* launches) {
   if (!launches) return RETRO_EINVAL;
   retro_status st = retro::make_geometry(dims, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
+  if (retro::is_mx4(g)) {  // the append, scores with or without the selection, attention, combine + merge
+    *launches = retro::score_selects(g) ? 4 : 5;
+    return RETRO_OK;
+  }
   Geometry gp = g;
   gp.token_pending = 1;
   *launches = one_launch(gp) ? 1 : select_in_attention(gp) ? 3 : 4;
@@ -447,7 +467,6 @@ retro_status retro_step(const retro_dims* dims, int32_t step, const void* q_wind
   Geometry g;
   retro_status st = prepare(dims, step, &g);
   if (st != RETRO_OK) return st;
-  if (retro::is_mx4(g)) return RETRO_EUNSUPPORTED;
   if (!q_window || !k_new || !v_new || !cache_ok(cache) || !sel_ok(sel) || !o_out || !lse_out)
     return RETRO_EINVAL;
   if (g.W > 0 && (!ocache || !ocache->o_cache || !ocache->lse_cache)) return RETRO_EINVAL;
@@ -462,14 +481,15 @@ retro_status retro_step(const retro_dims* dims, int32_t step, const void* q_wind
   int32_t* tok = reinterpret_cast<int32_t*>((char*)workspace + g.ws_tok);
   int32_t* err = reinterpret_cast<int32_t*>((char*)workspace + g.ws_err);
   const void* dummy = (char*)workspace + g.ws_dummy;
-  if (retro::reuse_step(g, step)) {
+  if (retro::is_mx4(g) && (!attend_ok(g, cache, q_window) || !aligned16({k_new, v_new}))) return RETRO_EINVAL;
+  if (retro::reuse_step(g, step) || retro::is_mx4(g)) {
     // top-k reuse: the token's append (with Alg. 2's current-page rule and the
-    // seq_lens advance), Alg. 2 on the kept selection, attention, combine + merge
-    const Geometry ga = retro::attend_geometry(g);
-    hipError_t e = retro::launch_append(g, step, *cache, k_new, v_new, s);
-    if (e == hipSuccess) e = retro::launch_reuse_mask(g, step, *cache, *sel, s);
-    if (e == hipSuccess)
-      e = retro::launch_attend(ga, step, q_window, *cache, *sel, nullptr, o_ws, l_ws, dummy, s);
+    // seq_lens advance), Alg. 2 on the kept selection, attention, combine + merge;
+    // a cache in 4 bits, whose pages no other launch writes: the same with a selection
+    const Geometry ga = attend_plan(g);
+    hipError_t e = append_token(g, step, *cache, k_new, v_new, s);
+    if (e == hipSuccess) e = select(g, step, q_cur, qbs, *cache, *sel, workspace, s);
+    if (e == hipSuccess) e = attend_partials(g, ga, step, q_window, *cache, *sel, nullptr, workspace, s);
     if (e == hipSuccess)
       e = retro::launch_combine_merge(ga, step, 2, o_ws, l_ws, sel->num_selected, nullptr,
                                       nullptr, nullptr, nullptr, ocache, o_out, lse_out, cache, s);

@@ -14,7 +14,8 @@
 // fp32 rows are taken apart into three bf16 terms (8 bits each: all of the 24), queries
 // and weights alike; the values of codes are exact in bf16, so that products are exact
 // and sums in fp32, in three matrix instructions instead of the sixteen times slower
-// ones of fp32.  Weights of bf16 rows are two terms: what the first one's rounding leaves is in the second.
+// ones of fp32.  Weights of bf16 rows are two terms or three (PT), each what the rounding
+// of those before it leaves.
 #pragma once
 
 #include "mx4.h"
@@ -84,12 +85,11 @@ __device__ __forceinline__ float below_bf16(float x) {
   return fabsf(x) < INFINITY ? x - top : 0.f;
 }
 
-template <typename T, int D, int NR>
+template <typename T, int D, int NR, int PT = sizeof(T) == 2 ? 2 : 3>
 struct Mx4Rows {
   static constexpr int KK = D / 32;                      // products of a contraction over d
   static constexpr int DT = D / 16;                      // products of the outputs
   static constexpr int QT = sizeof(T) == 2 ? 1 : 3;      // terms of a query
-  static constexpr int PT = sizeof(T) == 2 ? 2 : 3;      // and of a weight
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   bf16x8 q[NR][QT][KK];
   f32x4 acc[NR][DT];

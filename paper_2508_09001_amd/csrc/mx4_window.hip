@@ -69,7 +69,10 @@ __global__ void __launch_bounds__(64 * kWaves, RT == 1 && sizeof(T) == 2 ? 4 : 2
 
   // the rows, and the mask value from which one may not use a page (none for a row
   // that does not exist, all for the current query)
-  Mx4Rows<T, D, RT> rows;
+  // (weights as three bf16 terms: the outputs are fp32 and merged again and again; with two, as
+  // for chunks, they are 1.5e-6 off 64 bits instead of 1.5e-7, 128 heads of 36 rows 14.5 us
+  // instead of 15.7)
+  Mx4Rows<T, D, RT, 3> rows;
   rows.c = g.sm_scale * kLog2e;
   int thr[RT];
 #pragma unroll
@@ -234,8 +237,8 @@ hipError_t go_tiles(const WindowCall& a, hipStream_t s) {
 // us for RT 1, 2 and 3 (d 128), a workgroup's beginning and end 5.5, a further round of workgroups on
 // a compute unit 4 of these (1.5 for RT 1, whose workgroups are two at a time), the combine
 // 3.5 and more for more splits.  The choice for some shapes, in us, and others: 8 heads of
-// 68 rows, 128 pages, RT 1 in 4 splits 9.9 (RT 1 in 2 12.1, in 8 11.3; RT 2 in 8 11.2; RT 3, 6 tiles side by side, in 16 13.5);
-// 128 heads of 36 rows, 64 pages, RT 2 in one 14.5 (in two 19.4; RT 1 in one, with the combine that
+// 68 rows, 128 pages, RT 1 in 4 splits 10.0 (RT 1 in 2 12.1, in 8 11.3; RT 2 in 8 11.2; RT 3, 6 tiles side by side, in 16 13.5);
+// 128 heads of 36 rows, 64 pages, RT 2 in one 15.7 (in two 19.4; RT 1 in one, with the combine that
 // it does not need, 19.9).
 Geometry mx4_window_geometry(const Geometry& g) {
   static constexpr float kTurn[3] = {1.15f, 2.0f, 2.9f}, kRound[3] = {1.5f, 4.f, 4.f};

@@ -221,38 +221,6 @@ __global__ void __launch_bounds__(256) rotate_qk_kernel(
 
 constexpr int kAppendThreads = 128;
 
-// A lane's piece of a head's vector in codes; the lanes of a block together.
-template <typename T>
-struct Codes {
-  static constexpr int E = 16 / sizeof(T);
-  uint32_t codes;  // E of them
-  int e;
-  __device__ explicit Codes(u32x4 piece) {
-    float x[E];
-    unpack<T>(piece, x);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = max(top, (uint32_t)dpp_i<kDppXor1>((int)top));
-    top = max(top, (uint32_t)dpp_i<kDppXor2>((int)top));
-    if constexpr (E == 4) top = max(top, (uint32_t)dpp_i<kDppHalfMirror>((int)top));
-    e = mx4_exponent(top);
-    // (a block that is NaN as a whole has codes like any other)
-    const float s = mx4_scale(e == kMx4NaN ? 127 : e);
-    codes = mx4_encode<0>(0, x[0], x[1], s);
-    codes = mx4_encode<1>(codes, x[2], x[3], s);
-    if constexpr (E == 8) {
-      codes = mx4_encode<2>(codes, x[4], x[5], s);
-      codes = mx4_encode<3>(codes, x[6], x[7], s);
-    }
-  }
-  __device__ void store(char* at) const {
-    if constexpr (E == 8) *reinterpret_cast<uint32_t*>(at) = codes;
-    else *reinterpret_cast<uint16_t*>(at) = (uint16_t)codes;
-  }
-  __device__ u32x4 values() const { return mx4_piece<T>(codes, mx4_scale(e)); }
-};
-
 // One workgroup per (page of a sequence's run, KV head) stores the page's new
 // keys (token-major) and values (d-major, transposed through LDS, whole 16-byte
 // pieces where the run covers them) and widens the digest; as many others turn
@@ -355,20 +323,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
     u32x4 kt = turn(kr[i], r.k_norm != nullptr, wt, a, lane);
     if constexpr (MX4) {
       const Codes<T> kq(kt), vq(vr[i]);
-      const int n = E / 2, block = turn.c * E / 32, part = turn.c * E / (D / 16), in = turn.c * E % (D / 16);
-      kq.store(kblk + t * (D / 2) + turn.c * n);
-      char* group = vblk + t / 4 * (2 * D);
-      if constexpr (E <= D / 16) {
-        vq.store(group + (part * 4 + t % 4) * (D / 32) + in / 2);
-      } else {  // (two parts of four elements)
-        static_assert(E == 2 * (D / 16), "a piece is a part, or half of one, or two");
-        reinterpret_cast<uint16_t*>(group)[part * 4 + t % 4] = (uint16_t)vq.codes;
-        reinterpret_cast<uint16_t*>(group)[part * 4 + 4 + t % 4] = (uint16_t)(vq.codes >> 16);
-      }
-      if (turn.c * E % 32 == 0) {
-        kblk[PS * D / 2 + t * (D / 32) + block] = (char)kq.e;
-        vblk[PS * D / 2 + (t / 4 * (D / 32) + block) * 4 + t % 4] = (char)vq.e;
-      }
+      kq.template store_key<PS, D>(kblk, t, turn.c);
+      vq.template store_value<PS, D>(vblk, t, turn.c);
       kt = kq.values();
     } else {
       reinterpret_cast<u32x4*>((T*)kblk + t * D)[turn.c] = kt;

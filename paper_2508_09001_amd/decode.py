@@ -45,7 +45,7 @@ class RetroDecoder:
     [d_model][h_k*d]`` and ``wo [h_q*d][d_model]`` (host arrays or device tensors);
     ``d_model = h_q * d``.  ``layer_kw`` are the RetroLayer arguments shared by all
     layers (batch, num_kv_heads, group, head_dim, page_size, budget, window,
-    max_pages, dtype, budget_permille, ...).  ``library_projections=False`` keeps
+    max_pages, dtype, budget_permille, kv, ...).  ``library_projections=False`` keeps
     the products on torch.matmul (for comparison); with the library projections,
     ``fuse_update`` folds UpdateKV into the query / key / value launch
     (``retro_project_qkv_update``) instead of a ``retro_update_kv`` of its own.
@@ -123,7 +123,7 @@ class RetroDecoder:
             self.v = torch.zeros_like(self.k)
             self.k_new = torch.zeros(self.batch, self.hk, self.d, dtype=td, device=dev)
             self.v_new = torch.zeros_like(self.k_new)
-        self.fuse_update = self.fused and fuse_update and not self.rotated
+        self.fuse_update = self.fused and fuse_update and not self.rotated and lay.kv == "dtype"
         # fp32: library projections on the unpacked weights (retro_project_f32)
         self.f32_library = library_projections and self.dtype == torch.float32
         if self.f32_library:

@@ -82,17 +82,23 @@ def _on(device: torch.device):
 
 class RetroLayer:
     """State of one layer: paged KV cache, digests, retrospective mask, selection,
-    output cache, outputs and workspace, all on one device."""
+    output cache, outputs and workspace, all on one device.  ``kv``: how the cache is
+    held, in the layer's ``dtype`` or as "mx4" in 4 bits (``RETRO_FLAG_KV_MX4``)."""
 
     def __init__(self, batch: int, num_kv_heads: int, group: int, head_dim: int, page_size: int,
                  budget: int, window: int, max_pages: int, dtype: str = "bf16",
                  num_phys_pages: Optional[int] = None, page_table: Optional[torch.Tensor] = None,
                  sm_scale: float = 0.0, budget_permille: int = 0, flags: int = 0,
                  reuse_interval: int = 0,
-                 device: str = "cuda"):
+                 device: str = "cuda", kv: str = "dtype"):
         self.device = torch.device(device)
         if num_phys_pages is None:
             num_phys_pages = batch * max_pages
+        if kv not in ("dtype", "mx4"):
+            raise ValueError('kv must be "dtype" or "mx4"')
+        self.kv = kv
+        if kv == "mx4":
+            flags |= B.RETRO_FLAG_KV_MX4
         self.dims = B.Dims(batch, num_kv_heads, group, head_dim, page_size, budget, window,
                            max_pages, num_phys_pages, _RETRO_DTYPE[dtype], sm_scale,
                            budget_permille, flags, reuse_interval)
@@ -103,8 +109,13 @@ class RetroLayer:
         self.dtype = _TORCH_DTYPE[dtype]
         dev, td = self.device, self.dtype
         hk, d, P = num_kv_heads, head_dim, page_size
-        self.k_cache = torch.zeros(num_phys_pages, hk, P, d, dtype=td, device=dev)
-        self.v_cache = torch.zeros(num_phys_pages, hk, d, P, dtype=td, device=dev)
+        if kv == "mx4":  # codes, then exponents, of a page of a KV head
+            page = P * d // 2 + P * d // 32
+            self.k_cache = torch.zeros(num_phys_pages, hk, page, dtype=torch.uint8, device=dev)
+            self.v_cache = torch.zeros_like(self.k_cache)
+        else:
+            self.k_cache = torch.zeros(num_phys_pages, hk, P, d, dtype=td, device=dev)
+            self.v_cache = torch.zeros(num_phys_pages, hk, d, P, dtype=td, device=dev)
         # per logical page of each sequence, as the header lays it out (not per
         # physical page: the pool may hold more or fewer pages than batch * max_pages)
         self.digest = torch.zeros(batch, hk, max_pages, 2, d, dtype=td, device=dev)
@@ -157,7 +168,8 @@ class RetroLayer:
     def _dev(self, x) -> torch.Tensor:
         if not isinstance(x, torch.Tensor):
             x = torch.from_numpy(x)
-        return x.to(device=self.device, dtype=self.dtype).contiguous()
+        x = x.to(device=self.device, dtype=self.dtype).contiguous()
+        return x.clone() if self.kv == "mx4" and x.data_ptr() % 16 else x
 
     # -- calls ----------------------------------------------------------------------
     def prefill(self, seq: int, k, v, stream=None) -> None:
@@ -390,6 +402,20 @@ class RetroLayer:
             self._lens[b] += chunk.rows[b]
         self._keep_chunk = (q, k, v, chunk, rotary)
         return out
+
+    def read(self, chunk: RetroChunk, keys: bool = True, values: bool = True, stream=None
+             ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+        """The chunk's rows as the cache holds them: keys and values [rows][h_k][d] (None for
+        one that is not asked for), zeros for rows that are not stored."""
+        self._check_chunk(chunk)
+        if not keys and not values:
+            return None, None
+        with self._on_stream(stream, chunk.row_start):
+            k, v = (torch.zeros(chunk.n_rows, self.hk, self.d, dtype=self.dtype, device=self.device)
+                    if x else None for x in (keys, values))
+            B.retro_read_kv(self.dims, self.cache, chunk.struct, k, v, stream)
+        self._keep_read = chunk
+        return k, v
 
     def attend_chunk(self, chunk: RetroChunk, q, lse: bool = False, stream=None
                      ) -> Union[torch.Tensor, Tuple[torch.Tensor, torch.Tensor]]:

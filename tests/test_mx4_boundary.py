@@ -55,21 +55,48 @@ def test_flag(B):
     assert B.retro_chunk_workspace_size(_dims(B), 9) == B.retro_chunk_workspace_size(_dims(B, flags=0), 9)
 
 
-def test_calls_on_pages_in_dtype_are_refused(B):
+def test_steps(B):
+    """The calls that write pages in dtype by their own launches are refused, the others check
+    what they are given."""
     lib, d, cache = B.load_library(), _dims(B, window=2), B.KVCache(*[A] * 6)
+    odd = B.KVCache(A, A + 8, A, A, A, A)
     sel, oc = B.Selection(A, A, A), B.OutputCache(A, A)
-    D, c, s = C.byref(d), C.byref(cache), C.byref(sel)
+    D, c, s, o = C.byref(d), C.byref(cache), C.byref(sel), C.byref(oc)
     big = 1 << 40
-    calls = dict(
-        prefill=lib.retro_prefill_kv(D, c, 0, 0, 1, A, A, None),
-        append=lib.retro_append_kv(D, 0, c, A, A, None),
-        tokens=lib.retro_append_kv_tokens(D, 0, c, 1, A, A, None),
-        update=lib.retro_update_kv(D, c, 1, A, A, None),
-        project=lib.retro_project_qkv_update(D, c, A, 1024, A, 1, A, A, A, None),
-        partials=lib.retro_decode_attend_partials(D, 0, A, c, s, A, big, None),
-        step_partials=lib.retro_step_attend_partials(D, 0, A, c, s, A, big, None),
-        step=lib.retro_step(D, 0, A, A, A, c, s, C.byref(oc), A, A, A, big, None))
-    assert set(calls.values()) == {UNSUPPORTED}, calls
+    assert lib.retro_project_qkv_update(D, c, A, 1024, A, 1, A, A, A, None) == UNSUPPORTED
+    assert lib.retro_step_attend_partials(D, 0, A, c, s, A, big, None) == UNSUPPORTED
+    for ca, x in ((c, A + 8), (c, None), (C.byref(odd), A)):
+        assert lib.retro_prefill_kv(D, ca, 0, 0, 1, x, A, None) == INVALID
+        assert lib.retro_prefill_kv(D, ca, 0, 0, 1, A, x, None) == INVALID
+        assert lib.retro_append_kv(D, 0, ca, x, A, None) == INVALID
+        assert lib.retro_append_kv_tokens(D, 0, ca, 1, A, x, None) == INVALID
+        assert lib.retro_update_kv(D, ca, 1, x, A, None) == INVALID
+        assert lib.retro_decode_attend_partials(D, 0, x, ca, s, A, big, None) == INVALID
+        assert lib.retro_step(D, 0, A, x, A, ca, s, o, A, A, A, big, None) == INVALID
+        assert lib.retro_step(D, 0, x, A, A, ca, s, o, A, A, A, big, None) == INVALID
+    assert lib.retro_append_kv_tokens(D, 0, c, 0, None, None, None) == OK
+    assert lib.retro_append_kv_tokens(D, 0, c, -1, A, A, None) == INVALID
+    assert lib.retro_update_kv(D, c, 64 * 16 + 1, A, A, None) == INVALID
+    assert lib.retro_prefill_kv(D, c, 2, 0, 1, A, A, None) == INVALID
+    assert lib.retro_step(D, 0, A, A, A, c, s, o, A, A, A, 1000, None) == WORKSPACE
+
+
+def test_layer(B):
+    import torch
+    from paper_2508_09001_amd.layer import RetroChunk, RetroLayer
+    kw = dict(batch=2, num_kv_heads=3, group=2, head_dim=64, page_size=16, budget=16, window=0, max_pages=2,
+              device="cpu")
+    lay = RetroLayer(kv="mx4", **kw)
+    assert lay.dims.flags == B.RETRO_FLAG_KV_MX4 and lay.k_cache.shape == (4, 3, 16 * 64 // 2 + 32)
+    assert lay.k_cache.dtype == torch.uint8 and lay.digest.dtype == torch.bfloat16
+    assert RetroLayer(**kw).dims.flags == 0 and RetroLayer(flags=1, kv="mx4", **kw).dims.flags == 17
+    with pytest.raises(ValueError):
+        RetroLayer(kv="fp4", **kw)
+    with pytest.raises(ValueError):
+        lay.read(RetroChunk((1,), (0,), "cpu"))
+    assert lay.read(RetroChunk((1, 0), (0, 0), "cpu"), keys=False, values=False) == (None, None)
+    x = torch.zeros(130)[1:129].to(torch.bfloat16)
+    assert lay._dev(torch.zeros(129, dtype=torch.bfloat16)[1:]).data_ptr() % 16 == 0 and x.is_contiguous()
 
 
 def test_attention(B):
