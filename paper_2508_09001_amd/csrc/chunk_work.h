@@ -163,8 +163,16 @@ __device__ __forceinline__ Seq first_seq(const FindLds& L, int b, int G) {
 // tokens 34 and 47, 128 at 4000 49 and 57; but 256 at 2000 53 and 50, 512 at 4000 136
 // and 69, 128 rows of a new prompt 33 and 21.  fp32 tiles always are of 32 rows: its
 // matrix instructions are 16 times slower, and the reading does not show.
-template <bool MANY>
+//
+// MX4: over a cache in 4 bits a step of 32 rows costs a workgroup 0.42 us, a tile besides 20
+// where a workgroup has several, a part 0.4; one of 256 rows 2.0, and where tiles are cut
+// 8 and 1.6 a part (8 KV heads of 4 query heads, us with 32 and 256 rows: 64 rows at 8000 35
+// and 68, at 32000 74 and 116; 128 at 8000 48 and 73, at 32000 125 and 117; 256 at 2000 40 and
+// 50, at 8000 77 and 75; 512 at 2000 61 and 55; 1000 at 8000 260 and 160; a chunk of 100 beside 15 tokens at 2K to 8K 60 and
+// 79).  Uncut tiles of 256 rows need no such question: 128 rows of a new prompt 27 and 21.
+template <bool MANY, bool MX4 = false>
 __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, int tid) {
+  constexpr int64_t kManyCost = MX4 ? 5 : retro::kManyCost;
   enum { kLine, kLineTiles, kSmall, kSmallTiles, kMany, kTiles, kSums };
   static_assert(kSums <= kScans, "sums made together");
   Scan<kSums> x;
@@ -196,12 +204,32 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
   const int64_t n = gridDim.x, many = x.total[kMany], tiles = x.total[kTiles];
   Cut c;
   c.all_line = !MANY || (many < 5 * n && 8 * tiles < n && many > 16 * tiles);
+  if constexpr (MANY && MX4) {
+    // (in microseconds; no quotients of 64-bit integers, which took 3 of them)
+    auto over = [](float a, float b) { return a * __builtin_amdgcn_rcpf(b); };
+    const float cus = (float)n, of_many = (float)tiles, of_few = (float)x.total[kSmallTiles];
+    const float steps = over((float)many, fmaxf(of_many, 1.f));
+    const float whole = of_many < cus ? over(steps, floorf(over(cus, fmaxf(of_many, 1.f)))) : 0.f;
+    const float part = fmaxf(fmaxf(over((float)many, cus), whole), (float)kMinMany);
+    const float as_many = 2.0f * part + 10.f + 1.6f * over(steps, part);
+    const float as_few = 0.42f * over((float)x.total[kSmall], cus) +
+                         (of_few > cus ? 20.f * (over(of_few, cus) - 1.f) : 0.4f * over(cus, fmaxf(of_few, 1.f)));
+    c.all_line = steps > part && as_few < as_many;
+  }
   c.line = x.total[kLine] + (c.all_line ? x.total[kSmall] : 0);
   c.many = c.all_line ? 0 : many;
   // (tiles shorter than four steps are a share each: one after the other they would take
   // as many round trips: 33 sequences of 33 tokens 22 us, 13 so)
   const int64_t of_line = x.total[kLineTiles] + (c.all_line ? x.total[kSmallTiles] : 0);
-  const int64_t least = of_line ? min((c.line + of_line - 1) / of_line, (int64_t)kMinFew) : 1;
+  int64_t least = MX4 ? 1 : of_line ? min((c.line + of_line - 1) / of_line, (int64_t)kMinFew) : 1;
+  if constexpr (MX4) {
+    // A tile of up to eight steps is not cut, a longer one into some 32 parts at most, whose
+    // joining costs as much as the reading of as many codes does (a token at 500 tokens 13.4 -> 10.4 us, at
+    // 32000 of 2 KV heads of 16 query heads in 128, 64, 32 and 16 parts 45, 31, 26 and 28).
+    const int64_t steps = c.line > 8 * of_line ? (int64_t)((float)c.line * __builtin_amdgcn_rcpf((float)of_line)) : 1;
+    least = c.line > 8 * of_line ? max((int64_t)kMinFew, (steps + 31) / 32)
+                                 : of_line ? (c.line + of_line - 1) / of_line : 1;
+  }
   c.share = max((c.line + n - 1) / n, least);
   c.first = c.long_share = 0;
   // A part's most steps: all workgroups' share of the work, but no less than that gives

@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads) mx4_attend_kernel(AttendCall a) {
   __shared__ __attribute__((aligned(1024))) Mx4Lds<D, P, MANY> L;
   const int tid = thread_index();
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Cut cut = make_cut<MANY>(a, P, L.find, tid);
+  const Cut cut = make_cut<MANY, true>(a, P, L.find, tid);
   constexpr int64_t kBlock = mx4_block_bytes(P, D);
   const int64_t phys_bytes = kBlock * a.hk;
   const float c = a.scale * kLog2e;

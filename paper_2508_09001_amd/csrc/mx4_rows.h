@@ -113,7 +113,7 @@ struct Mx4Rows {
         for (int j = 0; j < 2; ++j) {
           const f32x4 y = live ? reinterpret_cast<const f32x4*>(mine)[2 * i + j] : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[4 * j + e] = y[e];
+          for (int e = 0; e < 4; ++e) x[4 * j + e] = y[e] != y[e] ? __builtin_nanf("") : y[e];  // NaN in its upper bits
         }
 #pragma unroll
         for (int term = 0; term < 3; ++term) {
