@@ -13,8 +13,10 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kReadThreads = 128;
+constexpr int64_t kL2Bytes = 32 << 20;
 
-template <typename T, int PS, int D, bool MX4>
+// PAST: the values are more than the L2s hold and are written past them.
+template <typename T, int PS, int D, bool MX4, bool PAST>
 __global__ void __launch_bounds__(kReadThreads) read_kv_kernel(Geometry g, retro_chunk ch,
                                                                const char* __restrict__ kc,
                                                                const char* __restrict__ vc,
@@ -42,6 +44,10 @@ __global__ void __launch_bounds__(kReadThreads) read_kv_kernel(Geometry g, retro
   const int64_t block = (int64_t)max(phys, 0) * g.hk + h;
   const char *kblk = kc + block * kBytes, *vblk = vc + block * kBytes;
   const int c = tid % LPV;
+  auto put = [](T* to, u32x4 x) {
+    if constexpr (PAST) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to));
+    else *reinterpret_cast<u32x4*>(to) = x;
+  };
   if constexpr (MX4) {
     uint32_t code[2][NP];
     int e[2][NP];
@@ -75,8 +81,8 @@ __global__ void __launch_bounds__(kReadThreads) read_kv_kernel(Geometry g, retro
       const int t = tid / LPV + j * (kReadThreads / LPV);
       if (t < s0 || t >= s1) continue;
       const int64_t at = ((row0 + t) * g.hk + h) * D + c * E;
-      if (k_out) *reinterpret_cast<u32x4*>(k_out + at) = mx4_piece<T>(code[0][j], mx4_scale(e[0][j]));
-      if (v_out) *reinterpret_cast<u32x4*>(v_out + at) = mx4_piece<T>(code[1][j], mx4_scale(e[1][j]));
+      if (k_out) put(k_out + at, mx4_piece<T>(code[0][j], mx4_scale(e[0][j])));
+      if (v_out) put(v_out + at, mx4_piece<T>(code[1][j], mx4_scale(e[1][j])));
     }
   } else {
     if (v_out) {  // E consecutive tokens of one element of d per piece
@@ -98,8 +104,8 @@ __global__ void __launch_bounds__(kReadThreads) read_kv_kernel(Geometry g, retro
       u32x4 k{0, 0, 0, 0}, v{0, 0, 0, 0};
       if (t < held && k_out) k = reinterpret_cast<const u32x4*>(kblk)[t * LPV + c];
       if (t < held && v_out) v = *reinterpret_cast<const u32x4*>(vs + t * ROW + c * E);
-      if (k_out) *reinterpret_cast<u32x4*>(k_out + at) = k;
-      if (v_out) *reinterpret_cast<u32x4*>(v_out + at) = v;
+      if (k_out) put(k_out + at, k);
+      if (v_out) put(v_out + at, v);
     }
   }
 }
@@ -111,12 +117,16 @@ bool read_kv_supported(const Geometry& g, int n_rows) { return page_blocks(g, n_
 hipError_t launch_read_kv(const Geometry& g, const retro_kv_cache& c, const retro_chunk& ch, void* k_out,
                           void* v_out, hipStream_t s) {
   const unsigned grid = (unsigned)page_blocks(g, ch.n_rows, g.hk);
-  auto go = [&](auto t, auto ps, auto d, auto in_4_bits) {
+  const bool past = (int64_t)ch.n_rows * g.hk * g.D * g.elt * ((k_out != nullptr) + (v_out != nullptr)) > kL2Bytes;
+  auto launch = [&](auto t, auto ps, auto d, auto in_4_bits, auto past_l2) {
     using T = decltype(t);
-    read_kv_kernel<T, decltype(ps)::value, decltype(d)::value, decltype(in_4_bits)::value>
+    read_kv_kernel<T, decltype(ps)::value, decltype(d)::value, decltype(in_4_bits)::value, decltype(past_l2)::value>
         <<<grid, kReadThreads, 0, s>>>(g, ch, (const char*)c.k_cache, (const char*)c.v_cache, c.page_table,
                                        c.seq_lens, (T*)k_out, (T*)v_out);
     return hipGetLastError();
+  };
+  auto go = [&](auto t, auto ps, auto d, auto in_4_bits) {
+    return past ? launch(t, ps, d, in_4_bits, std::true_type{}) : launch(t, ps, d, in_4_bits, std::false_type{});
   };
   auto with_format = [&](auto t, auto ps, auto d) {
     return is_mx4(g) ? go(t, ps, d, std::true_type{}) : go(t, ps, d, std::false_type{});

@@ -299,6 +299,18 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
     if (tid == 0 && first_bad > 0)
       seq_lens[b] = (int)min((int64_t)run.pos + run.n, (int64_t)(lp0 + first_bad) * PS);
   }
+  constexpr int NP = PS * LPV / kAppendThreads;  // passes over a page's rows
+  u32x4 kr[NP], vr[NP];
+  auto load = [&] {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int t = tid / LPV + i * (kAppendThreads / LPV);
+      if (t < s0 || t >= s1) continue;
+      kr[i] = reinterpret_cast<const u32x4*>(k + (row0 + t) * k_stride + h * D)[turn.c];
+      vr[i] = reinterpret_cast<const u32x4*>(v + (row0 + t) * v_stride + h * D)[turn.c];
+    }
+  };
+  if constexpr (MX4) load();  // without waiting for the page's number
   if (lp >= g.max_pages) return;
   const int phys = pt[(int64_t)b * g.max_pages + lp];
   if (phys < 0 || phys >= g.num_phys) return;
@@ -306,21 +318,16 @@ __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
   const int64_t block = (int64_t)phys * g.hk + h;
   constexpr int kBytes = MX4 ? mx4_block_bytes(PS, D) : PS * D * (int)sizeof(T);
   char *const kblk = kc + block * kBytes, *const vblk = vc + block * kBytes;
-  constexpr int NP = PS * LPV / kAppendThreads;  // passes over a page's rows
-  u32x4 kr[NP], vr[NP];
+  if constexpr (!MX4) load();
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     const int t = tid / LPV + i * (kAppendThreads / LPV);
     if (t < s0 || t >= s1) continue;
-    kr[i] = reinterpret_cast<const u32x4*>(k + (row0 + t) * k_stride + h * D)[turn.c];
-    vr[i] = reinterpret_cast<const u32x4*>(v + (row0 + t) * v_stride + h * D)[turn.c];
-  }
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int t = tid / LPV + i * (kAppendThreads / LPV);
-    if (t < s0 || t >= s1) continue;
-    turn.angles(lp * PS + t, a);
-    u32x4 kt = turn(kr[i], r.k_norm != nullptr, wt, a, lane);
+    u32x4 kt = kr[i];
+    if (!MX4 || r.rot_dim || r.k_norm) {
+      turn.angles(lp * PS + t, a);
+      kt = turn(kt, r.k_norm != nullptr, wt, a, lane);
+    }
     if constexpr (MX4) {
       const Codes<T> kq(kt), vq(vr[i]);
       kq.template store_key<PS, D>(kblk, t, turn.c);
