@@ -2,8 +2,21 @@
 // chunk_attend.hip does over pages in dtype, with the same layout of the work
 // (chunk_work.h): the steps of all tiles of 32 rows form one line, cut into shares for
 // the workgroups, and the parts of a cut tile are joined by the workgroup that counts
-// itself last.  A workgroup's wavefronts take 32 tokens in turn, codes straight from the page into
-// registers (mx4_rows.h), and join their (maximum, sum, output) at the end of a tile.
+// itself last; tiles of 256 rows where there is work for them (bf16).
+//   - 32 rows: a workgroup's wavefronts take 32 tokens in turn, codes straight from the page into
+//     registers (mx4_rows.h), and join their (maximum, sum, output) at the end of a tile.  Up to 16
+//     rows are one tile of a product, of which more wavefronts' instructions are left.
+//   - 256 rows: chunk_attend.hip's stages of 64 keys in LDS, in bf16, which the wavefronts
+//     make of the codes while they work on the stage in front (Mx4Stages).
+//
+// Measured (bf16, 8 KV heads of 4 query heads of 128): 16 tokens at 8K to 32K, 306 MB of
+// codes, 62 us (187 over pages in bf16): 50 of them at 6.1 TB/s, the rest is the first keys' way and
+// the joins; a token at 32768 18.0 us (32.5), of which 4.6 are the reading, 1.6 the start of all workgroups, 3.8
+// lengths, layout and page numbers, 1.9 the slowest wavefront's lead, 1.2 the joining of eight
+// wavefronts and 4 that of 32 parts.  8192 rows from 0 519 to 546 us on cards where pages in bf16 take 500 to 510: the matrix
+// units are busy 48 % of the cycles, the vector units, which do the softmax and the conversion, 57 %.
+// Two workgroups of a compute unit side by side, with half of the registers and 512 shares, took 82
+// us for the 16 tokens and 34 for the one, whose 64 parts are joined by one workgroup.
 #include "chunk_work.h"
 #include "mx4_rows.h"
 
@@ -94,7 +107,8 @@ struct Mx4Stages {
     of_values = part * (D / 8) | (lane / 16) % (D / 32) * 4 << 16;
     const int key = 8 * wave + lane / 8, row = key % 32, token = 8 * wave % 32, d = 2 * lane % D;
     const int at_key = key / 32 * S::TILE + row * (D * 2) + (lane % 8 * KP ^ S::fk(row)) * 16;
-    const int at_value = 8 * wave / 32 * S::TILE + token / P * (D * P * 2) + d * (P * 2) + (token % P / 8 ^ S::fv(d)) * 16;
+    const int at_value = 8 * wave / 32 * S::TILE + token / P * (D * P * 2) + (d + (lane >> 3 & 1)) * (P * 2) +
+                         (token % P / 8 ^ S::fv(d)) * 16;
     static_assert(S::NB * S::TILE <= 1 << 16, "places within a stage's keys, or values, have 16 bits");
     puts = at_key | at_value << 16;
     asm volatile("" : "+v"(of_keys), "+v"(of_values), "+v"(puts));  // kept as they are
@@ -128,13 +142,16 @@ struct Mx4Stages {
     const uint32_t w = v[t][e * (D / 32) / 4] >> (of_keys * (128 / D) & (D / 32 - 1) * 8);  // byte lane % (D / 32)
     x[4 * t + e] = e * (D / 32) % 4 ? mx4_bf16<2>(w, scale) : mx4_bf16<0>(w, scale);
   }
-  __device__ __forceinline__ void put_values(int high) const {
+  // One of a lane's two elements, then the other: every other eight lanes begin with the second
+  // one, so that sixteen write to as many groups of banks.  (Element d + 1 has the order of
+  // pieces of element d; for d 64 two lanes write the same.)
+  __device__ __forceinline__ void put_values(int other) const {
+    constexpr int kRow = P * 2;  // bytes of an element's tokens in a page
+    const uint32_t halves = (0x05040100u + (puts >> 16 & kRow) / kRow * 0x02020202u) ^ other * 0x02020202u;
     u32x4 y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      y[i] = high ? high_halves(x[2 * i], x[2 * i + 1]) : low_halves(x[2 * i], x[2 * i + 1]);
-    // (element d + 1 has the order of pieces of element d; for d 64 two lanes write the same)
-    put(to + S::NB * S::TILE + (puts >> 16) + high * (P * 2), y);
+    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], halves);
+    put(to + S::NB * S::TILE + (puts >> 16 ^ other * kRow), y);
   }
   // the conversion in kUnits units
   static constexpr int kUnits = 11 + KP;
@@ -144,10 +161,14 @@ struct Mx4Stages {
     else if (u <= KP + 8) convert_values((u - KP - 1) / 4, (u - KP - 1) % 4);
     else put_values(u - KP - 9);
   }
+  // (from the first product's last instructions on: 8192 rows from 0 547 us spread over all of
+  // them, 543, 541, 541, 544 and 549 from number 4, 8, 12, 16 and 20 of 32 on; without the
+  // conversion 10 % less, of which values, with their shifts and halves, are two thirds)
   __device__ __forceinline__ void beside(int i, int n) {
+    const int first = n * 3 / 8;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u)
-      if (u * n / kUnits == i) unit(u);
+      if (u * (n - first) / kUnits + first == i) unit(u);
   }
   __device__ __forceinline__ void finish() {
 #pragma unroll
