@@ -517,8 +517,8 @@ retro_status retro_rotate_qk(const retro_dims* dims, const retro_rotary* rotary,
  * initial -1).  The first row whose page is not mapped is dropped with every
  * later row of its sequence (slots past the new seq_lens, and digests and last_loaded of
  * pages past it, are then unspecified).  Queries are written for dropped rows
- * too (NaN past rotary->positions); q_out may be q where q_stride is h_q * d.  With rot_dim > 0, rotary->positions must be
- * at least max_pages * P (RETRO_EINVAL).  n_rows == 0 does nothing. */
+ * too (NaN past rotary->positions); q_out may be q where q_stride is h_q * d.  With rot_dim > 0,
+ * rotary->positions must be at least max_pages * P (RETRO_EINVAL).  n_rows == 0 does nothing. */
 retro_status retro_append_kv_rotary(const retro_dims* dims, int32_t step,
                                     const retro_kv_cache* cache, const retro_chunk* chunk,
                                     const retro_rotary* rotary, const void* q, int64_t q_stride,
@@ -559,16 +559,17 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
 /* ---- The cache in 4 bits ---------------------------------------------------------
  * With RETRO_FLAG_KV_MX4 in dims->flags a cache's keys and values are held in 4.25 bits
  * an element (the elements and scales of the OCP Microscaling Formats specification's
- * MXFP4), for 3.8 times the tokens in the same memory and as much less to read.  A head's vector is cut into blocks of 32 elements.
- * A block has one exponent byte e and 32 codes: a sign bit and the magnitudes 0, 0.5, 1,
- * 1.5, 2, 3, 4, 6 in the order of the other three bits; an element stands for its code's
- * value times 2^(e - 127), which is exact in bf16.  Storing an element x of dtype (a key
+ * MXFP4), for 3.8 times the tokens of bf16 in the same memory and as much less to read.  A head's
+ * vector is cut into blocks of 32 elements.  A block has one exponent byte e and 32 codes: a sign bit and the
+ * magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 in the order of the other three bits; an element stands for
+ * its code's value times 2^(e - 127), which is exact in bf16.  Storing an element x of dtype (a key
  * as the other format would hold it, normalised, rotated and rounded):
  *   with m the largest magnitude of the block and 2^f <= m < 2^(f + 1),
  *   e = 127 + f - 2 for m < 1.75 * 2^f, one more from there on, cut to 2 .. 252;
  *   the code is the one nearest to x / 2^(e - 127), of two equally near ones that with an
  *   even last bit, and 6 for what lies beyond.
- * A block with a NaN or an infinity gets e = 255: all of it stands for NaN.
+ * A block with a NaN or an infinity gets e = 255: all of it stands for NaN.  (A cache that
+ * another program has filled holds no other exponents either; slots past seq_lens may.)
  * k_cache and v_cache are then bytes, [num_phys_pages][h_k][P d / 2 + P d / 32], a page of
  * a KV head being its codes (element 2 i in the low half of a byte, 2 i + 1 in the high
  * one), then its exponents:

@@ -168,8 +168,9 @@ __device__ __forceinline__ Seq first_seq(const FindLds& L, int b, int G) {
 // where a workgroup has several, a part 0.4; one of 256 rows 2.0, and where tiles are cut
 // 8 and 1.6 a part (8 KV heads of 4 query heads, us with 32 and 256 rows: 64 rows at 8000 35
 // and 68, at 32000 74 and 116; 128 at 8000 48 and 73, at 32000 125 and 117; 256 at 2000 40 and
-// 50, at 8000 77 and 75; 512 at 2000 61 and 55; 1000 at 8000 260 and 160; a chunk of 100 beside 15 tokens at 2K to 8K 60 and
-// 79).  Uncut tiles of 256 rows need no such question: 128 rows of a new prompt 27 and 21.
+// 50, at 8000 77 and 75; 512 at 2000 61 and 55; 1000 at 8000 260 and 160; a chunk of 100 beside 15
+// tokens at 2K to 8K 60 and 79).  Uncut tiles of 256 rows need no such question: 128 rows of a new
+// prompt 27 and 21.
 template <bool MANY, bool MX4 = false>
 __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, int tid) {
   constexpr int64_t kManyCost = MX4 ? 5 : retro::kManyCost;
@@ -224,8 +225,9 @@ __device__ __forceinline__ Cut make_cut(const AttendCall& a, int P, FindLds& L, 
   int64_t least = MX4 ? 1 : of_line ? min((c.line + of_line - 1) / of_line, (int64_t)kMinFew) : 1;
   if constexpr (MX4) {
     // A tile of up to eight steps is not cut, a longer one into some 32 parts at most, whose
-    // joining costs as much as the reading of as many codes does (a token at 500 tokens 13.4 -> 10.4 us, at
-    // 32000 of 2 KV heads of 16 query heads in 128, 64, 32 and 16 parts 45, 31, 26 and 28).
+    // joining costs as much as the reading of as many codes does (a token at 500 tokens 13.4 ->
+    // 10.4 us, at 32000 of 2 KV heads of 16 query heads in 128, 64, 32 and 16 parts 45, 31, 26 and
+    // 28).
     const int64_t steps = c.line > 8 * of_line ? (int64_t)((float)c.line * __builtin_amdgcn_rcpf((float)of_line)) : 1;
     least = c.line > 8 * of_line ? max((int64_t)kMinFew, (steps + 31) / 32)
                                  : of_line ? (c.line + of_line - 1) / of_line : 1;

@@ -2,14 +2,14 @@
 // (a row: a query of one head of the group), shared by the attention kernels.
 //
 // S^T = K Q^T and O^T += V^T P^T on 16 x 16 x 32 products, 16 tokens of each tile's
-// scores to a product, with operands made in registers: a lane reads its codes (a quarter of a key; four
-// tokens' elements of a sixteenth of the vector) straight from the page, and the converted values are the
-// operand.  The order within a contraction is free as long as both operands have
-// it: lane l's share of key l % 16 is the block l / 16 of the vector as it lies, and its queries the
-// same elements; row i of product number p of the outputs is element (d / 16) i + p, so
-// that one piece of a value page feeds all of them.  A lane ends up with the scores
-// of tokens 4 (l / 16) .. + 3 of both halves of its row l % 16, which are the weights that it needs
-// for the second product, so that nothing moves between lanes.
+// scores to a product, with operands made in registers: a lane reads its codes (a quarter of a key;
+// four tokens' elements of a sixteenth of the vector) straight from the page, and the converted
+// values are the operand.  The order within a contraction is free as long as both operands have it:
+// lane l's share of key l % 16 is the block l / 16 of the vector as it lies, and its queries the
+// same elements; row i of product number p of the outputs is element (d / 16) i + p, so that one
+// piece of a value page feeds all of them.  A lane ends up with the scores of tokens 4 (l / 16) ..
+// + 3 of both halves of its row l % 16, which are the weights that it needs for the second product,
+// so that nothing moves between lanes.
 //
 // fp32 rows are taken apart into three bf16 terms (8 bits each: all of the 24), queries
 // and weights alike; the values of codes are exact in bf16, so that products are exact

@@ -237,9 +237,9 @@ hipError_t go_tiles(const WindowCall& a, hipStream_t s) {
 // us for RT 1, 2 and 3 (d 128), a workgroup's beginning and end 5.5, a further round of workgroups on
 // a compute unit 4 of these (1.5 for RT 1, whose workgroups are two at a time), the combine
 // 3.5 and more for more splits.  The choice for some shapes, in us, and others: 8 heads of
-// 68 rows, 128 pages, RT 1 in 4 splits 10.0 (RT 1 in 2 12.1, in 8 11.3; RT 2 in 8 11.2; RT 3, 6 tiles side by side, in 16 13.5);
-// 128 heads of 36 rows, 64 pages, RT 2 in one 15.7 (in two 19.4; RT 1 in one, with the combine that
-// it does not need, 19.9).
+// 68 rows, 128 pages, RT 1 in 4 splits 10.0 (RT 1 in 2 12.1, in 8 11.3; RT 2 in 8 11.2; RT 3, 6
+// tiles side by side, in 16 13.5); 128 heads of 36 rows, 64 pages, RT 2 in one 15.7 (in two 19.4;
+// RT 1 in one, with the combine that it does not need, 19.9).
 Geometry mx4_window_geometry(const Geometry& g) {
   static constexpr float kTurn[3] = {1.15f, 2.0f, 2.9f}, kRound[3] = {1.5f, 4.f, 4.f};
   Geometry x = g;
