@@ -225,26 +225,28 @@ template <typename T, int D, int P>
 hipError_t go_tiles(const WindowCall& a, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     if (a.g.tiles_per_group == 2) return go<T, D, P, 2>(a, s);
-    if (a.g.tiles_per_group == 3) return go<T, D, P, 3>(a, s);
   }
   return a.g.tiles_per_group == 1 ? go<T, D, P, 1>(a, s) : hipErrorInvalidValue;
 }
 
 }  // namespace
 
-// One workgroup takes RT tiles of rows (fp32 rows, with three times the operands, one) and a
-// number of chunks that its wavefronts go through in `it` turns.  A turn takes 1.15, 2.0 and 2.9
-// us for RT 1, 2 and 3 (d 128), a workgroup's beginning and end 5.5, a further round of workgroups on
-// a compute unit 4 of these (1.5 for RT 1, whose workgroups are two at a time), the combine
-// 3.5 and more for more splits.  The choice for some shapes, in us, and others: 8 heads of
-// 68 rows, 128 pages, RT 1 in 4 splits 10.0 (RT 1 in 2 12.1, in 8 11.3; RT 2 in 8 11.2; RT 3, 6
-// tiles side by side, in 16 13.5); 128 heads of 36 rows, 64 pages, RT 2 in one 15.7 (in two 19.4;
-// RT 1 in one, with the combine that it does not need, 19.9).
+// One workgroup takes one or two tiles of rows (fp32 rows, with three times the operands, one)
+// and a number of chunks that its wavefronts go through in `it` turns.  A turn takes 1.05 us
+// with one tile and 1.95 with two (d 128), the beginning and end of two tiles 0.3 more than those
+// of one, a further round of workgroups on a compute unit 1.2 and 4.7 (those of one tile are two
+// at a time); splits cost a combine of 2.8 us and its partials, 0.54 us a million elements.
+// These are fitted to 3700 pairs of a shape and its possible splits, where the choice is on average
+// 0.9 % behind the best of its shape.  Three tiles a workgroup (3.1 us a turn, 3.0 more at its
+// ends) were never the best.  Some choices: 16 heads of 68 rows, 128 pages, one tile in 3
+// splits 11.8 us (in 2 13.2, in 4 14.3, in one 15.2); 128 heads of 36 rows, 64 pages, two tiles in
+// one 16.2 (one tile 16.8); 512 heads of 36 rows, 32 pages, one tile 29.0 (two 41.7, three 34.5).
 Geometry mx4_window_geometry(const Geometry& g) {
-  static constexpr float kTurn[3] = {1.15f, 2.0f, 2.9f}, kRound[3] = {1.5f, 4.f, 4.f};
+  static constexpr float kTurn[2] = {1.05f, 1.95f}, kRound[2] = {1.2f, 4.7f}, kFirst[2] = {0.f, 0.3f};
   Geometry x = g;
   x.stream = 1;
-  const int most = g.dtype == RETRO_BF16 ? 3 : 1, cap = compute_units(), cps_max = kListPages / g.chunk_pages;
+  const int most = g.dtype == RETRO_BF16 ? 2 : 1, cap = compute_units(), cps_max = kListPages / g.chunk_pages;
+  const float partial = 0.54e-6f * (float)((int64_t)g.batch * g.hq * (g.W + 1) * g.D);
   float best = 0.f;
   for (int rt = 1; rt <= std::min(most, g.row_tiles); ++rt) {
     const int groups = (g.row_tiles + rt - 1) / rt;
@@ -253,7 +255,7 @@ Geometry mx4_window_geometry(const Geometry& g) {
       if (ns > g.n_splits) continue;
       const int64_t rounds = ((int64_t)g.batch * g.hk * groups * ns + cap - 1) / cap;
       const float time = (float)(rounds * it) * kTurn[rt - 1] + (float)(rounds - 1) * kRound[rt - 1] +
-                         (ns > 1 ? 3.5f + 0.1f * (float)ns : 0.f);
+                         kFirst[rt - 1] + (ns > 1 ? 2.8f + partial * (float)ns : 0.f);
       if (best != 0.f && time >= best) continue;
       best = time;
       x.tiles_per_group = rt;

@@ -333,3 +333,19 @@ def test_window_unmapped_and_large_scores():
 def test_window_batches():
     lens = [200 + 61 * i for i in range(24)]
     Window("bf16", 4, 4, 128, 16, lens, 8, 512, seed=3).run().check()
+
+
+@pytest.mark.parametrize("P,d", [(16, 128), (32, 128), (16, 64), (32, 64)])
+@pytest.mark.parametrize("dtype,hk,G,W,batch,pages,tiles,splits",
+                         [("bf16", 8, 4, 8, 16, 64, 2, 1), ("bf16", 8, 4, 16, 2, 128, 1, 3), ("bf16", 16, 4, 11, 16, 8, 1, 1),
+                          ("bf16", 3, 4, 7, 43, 96, 2, 1), ("bf16", 8, 2, 16, 12, 128, 2, 1),
+                          ("f32", 8, 4, 8, 16, 64, 1, None)])
+def test_window_tiles(P, d, dtype, hk, G, W, batch, pages, tiles, splits):
+    """One or two tiles of rows a workgroup, with and without splits; the last tiles not full."""
+    budget = pages * 16
+    w = Window(dtype, hk, G, d, P, [budget - 7 * b for b in range(batch)], W, budget, seed=tiles or 0)
+    got = w.B.retro_attend_plan(w.d_, False)
+    print("[plan]", got, flush=True)
+    assert tiles is None or got[0] == tiles
+    assert splits is None or got[1] == splits
+    w.run().check()
