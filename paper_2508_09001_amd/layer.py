@@ -80,6 +80,10 @@ def _on(device: torch.device):
     return torch.cuda.device(device) if device.index is not None else contextlib.nullcontext()
 
 
+def _as_stream(stream) -> torch.cuda.Stream:
+    return torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+
+
 class RetroLayer:
     """State of one layer: paged KV cache, digests, retrospective mask, selection,
     output cache, outputs and workspace, all on one device.  ``kv``: how the cache is
@@ -165,29 +169,36 @@ class RetroLayer:
         """Whether the device may have dropped rows that ``_lens`` counts."""
         return self._full_table is None or self._full_table != self._table_version()
 
-    def _dev(self, x) -> torch.Tensor:
+    def _dev(self, x, stream=None) -> torch.Tensor:
+        """x as the library reads it: as it is, or a copy, which is work of the call's stream."""
         if not isinstance(x, torch.Tensor):
             x = torch.from_numpy(x)
-        x = x.to(device=self.device, dtype=self.dtype).contiguous()
-        return x.clone() if self.kv == "mx4" and x.data_ptr() % 16 else x
+        odd = self.kv == "mx4" and x.data_ptr() % 16
+        if x.device == self.seq_lens.device and x.dtype == self.dtype and x.is_contiguous() and not odd:
+            if stream is not None and x.is_cuda:  # may be freed by the caller before `stream` has read it
+                x.record_stream(_as_stream(stream))
+            return x
+        with self._on_stream(stream, x):
+            y = x.to(device=self.device, dtype=self.dtype).contiguous()
+            return y.clone() if self.kv == "mx4" and y.data_ptr() % 16 else y
 
     # -- calls ----------------------------------------------------------------------
     def prefill(self, seq: int, k, v, stream=None) -> None:
-        k, v = self._dev(k), self._dev(v)
+        k, v = self._dev(k, stream), self._dev(v, stream)
         n = k.shape[0]
         B.retro_prefill_kv(self.dims, self.cache, seq, self._lens[seq], n, k, v, stream)
         self._lens[seq] += n
         self._keep = (k, v)  # keep sources alive until the copy has run
 
     def append(self, step: int, k_new, v_new, stream=None) -> None:
-        k_new, v_new = self._dev(k_new), self._dev(v_new)
+        k_new, v_new = self._dev(k_new, stream), self._dev(v_new, stream)
         B.retro_append_kv(self.dims, step, self.cache, k_new, v_new, stream)
         for b in range(self.batch):
             self._lens[b] += 1
 
     def append_tokens(self, step: int, k_new, v_new, stream=None) -> None:
         """Several tokens per sequence in one call: k_new / v_new [n][batch][h_k][d]."""
-        k_new, v_new = self._dev(k_new), self._dev(v_new)
+        k_new, v_new = self._dev(k_new, stream), self._dev(v_new, stream)
         n = int(k_new.shape[0])
         B.retro_append_kv_tokens(self.dims, step, self.cache, n, k_new, v_new, stream)
         for b in range(self.batch):
@@ -196,13 +207,13 @@ class RetroLayer:
         self._keep = (k_new, v_new)
 
     def select(self, step: int, q_cur, stream=None) -> None:
-        q_cur = self._dev(q_cur)
+        q_cur = self._dev(q_cur, stream)
         B.retro_select_pages(self.dims, step, q_cur, self.cache, self.sel, self.workspace,
                              self.ws_bytes, stream)
         self._keep = q_cur
 
     def attend(self, step: int, q_window, stream=None) -> None:
-        q_window = self._dev(q_window)
+        q_window = self._dev(q_window, stream)
         B.retro_decode_attend(self.dims, step, q_window, self.cache, self.sel, self.o_part,
                               self.lse_part, self.workspace, self.ws_bytes, stream)
         self._keep = q_window
@@ -215,7 +226,7 @@ class RetroLayer:
     def update_kv(self, k_upd, v_upd, stream=None) -> None:
         """UpdateKV: new keys / values [batch][n][h_k][d] for the n most recent stored
         tokens of every sequence (their pages' digests are recomputed)."""
-        k_upd, v_upd = self._dev(k_upd), self._dev(v_upd)
+        k_upd, v_upd = self._dev(k_upd, stream), self._dev(v_upd, stream)
         B.retro_update_kv(self.dims, self.cache, int(k_upd.shape[1]), k_upd, v_upd, stream)
         self._keep_upd = (k_upd, v_upd)
 
@@ -241,7 +252,7 @@ class RetroLayer:
     def step(self, step: int, q_window, k_new, v_new, stream=None, noalloc: bool = False) -> None:
         """One retro_step (noalloc: retro_step_noalloc, the library's static scratch in
         place of this layer's workspace)."""
-        q_window, k_new, v_new = self._dev(q_window), self._dev(k_new), self._dev(v_new)
+        q_window, k_new, v_new = self._dev(q_window, stream), self._dev(k_new, stream), self._dev(v_new, stream)
         if noalloc:
             B.retro_step_noalloc(self.dims, step, q_window, k_new, v_new, self.cache, self.sel,
                                  self.ocache, self.o_out, self.lse_out, stream)
@@ -259,11 +270,14 @@ class RetroLayer:
     @contextlib.contextmanager
     def _on_stream(self, stream, *inputs):
         """Work of a call on the cache's device and on `stream` (None: the current one)."""
+        if not self.seq_lens.is_cuda:
+            yield
+            return
         with torch.cuda.device(self.seq_lens.device):
             if stream is None:
                 yield
                 return
-            s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+            s = _as_stream(stream)
             with torch.cuda.stream(s):
                 yield
             for x in inputs:  # may be freed by the caller before `stream` has read them
