@@ -345,8 +345,8 @@ retro_status retro_step(const retro_dims* dims, int32_t step, const void* q_wind
 
 /* The number of kernel launches retro_step makes for these dims on the current
  * device in a step that selects (1: scores, selection, attention and merge in
- * one launch; 3 or 4: see retro_step; a top-k reuse step always makes 4), in
- * *launches.  Host only: nothing is enqueued. */
+ * one launch; 3 or 4: see retro_step; 4 or 5 over a cache in 4 bits; a top-k reuse
+ * step always makes 4), in *launches.  Host only: nothing is enqueued. */
 retro_status retro_step_launches(const retro_dims* dims, int32_t* launches);
 
 /* How the attention of these dims is launched on the current device: *row_tiles
@@ -582,8 +582,9 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
  * (RETRO_EUNSUPPORTED), with the semantics that it has for a cache whose keys and values are what
  * the codes stand for; queries, keys and values that it is given, the outputs of attention,
  * k_cache and v_cache have to be 16-byte aligned (RETRO_EINVAL).  retro_step is four or five
- * launches then (the append, the scores, the selection, the attention, combine + merge), and
- * retro_chunk_attend takes bf16 rows' weights for sequences of few rows as two bf16 halves and
+ * launches then (the append, the scores, the selection, which is a launch of its own for
+ * large tables, the attention, combine + merge; nothing that an earlier call has left in the
+ * workspace is read), and retro_chunk_attend takes bf16 rows' weights for sequences of few rows as two bf16 halves and
  * for the others as one, retro_decode_attend and retro_step as three, fp32 rows always as three. */
 
 /* Rows of the cache as keys and values: row j of sequence b, as `chunk` lays them out, is

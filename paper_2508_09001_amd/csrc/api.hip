@@ -166,8 +166,8 @@ float* ws_at(void* ws, size_t off) { return reinterpret_cast<float*>((char*)ws +
 
 // a call's steps in the cache's format
 hipError_t append_token(const Geometry& g, int step, const retro_kv_cache& cache, const void* k_new,
-                        const void* v_new, hipStream_t s) {
-  return retro::is_mx4(g) ? retro::launch_mx4_append_tokens(g, step, cache, 1, k_new, v_new, s)
+                        const void* v_new, hipStream_t s, int32_t* counters = nullptr) {
+  return retro::is_mx4(g) ? retro::launch_mx4_append_tokens(g, step, cache, 1, k_new, v_new, s, counters)
                           : retro::launch_append(g, step, cache, k_new, v_new, s);
 }
 Geometry attend_plan(const Geometry& g) {
@@ -285,8 +285,9 @@ retro_status retro_append_kv_tokens(const retro_dims* dims, int32_t step,
   if (n_tokens == 0) return RETRO_OK;
   if (!k_new || !v_new) return RETRO_EINVAL;
   if (retro::is_mx4(g) && !aligned16({k_new, v_new, cache->k_cache, cache->v_cache})) return RETRO_EINVAL;
-  return from_hip((retro::is_mx4(g) ? retro::launch_mx4_append_tokens : retro::launch_append_tokens)(
-      g, step, *cache, n_tokens, k_new, v_new, (hipStream_t)stream));
+  hipStream_t s = (hipStream_t)stream;
+  return from_hip(retro::is_mx4(g) ? retro::launch_mx4_append_tokens(g, step, *cache, n_tokens, k_new, v_new, s)
+                                   : retro::launch_append_tokens(g, step, *cache, n_tokens, k_new, v_new, s));
 }
 
 retro_status retro_update_kv(const retro_dims* dims, const retro_kv_cache* cache,
@@ -485,9 +486,11 @@ retro_status retro_step(const retro_dims* dims, int32_t step, const void* q_wind
   if (retro::reuse_step(g, step) || retro::is_mx4(g)) {
     // top-k reuse: the token's append (with Alg. 2's current-page rule and the
     // seq_lens advance), Alg. 2 on the kept selection, attention, combine + merge;
-    // a cache in 4 bits, whose pages no other launch writes: the same with a selection
+    // a cache in 4 bits, whose pages no other launch writes: the same with a selection,
+    // whose counters the append sets to zero
     const Geometry ga = attend_plan(g);
-    hipError_t e = append_token(g, step, *cache, k_new, v_new, s);
+    hipError_t e = append_token(g, step, *cache, k_new, v_new, s,
+                                reinterpret_cast<int32_t*>((char*)workspace + g.ws_sel));
     if (e == hipSuccess) e = select(g, step, q_cur, qbs, *cache, *sel, workspace, s);
     if (e == hipSuccess) e = attend_partials(g, ga, step, q_window, *cache, *sel, nullptr, workspace, s);
     if (e == hipSuccess)

@@ -24,9 +24,11 @@ namespace retro {
 inline bool is_mx4(const Geometry& g) { return (g.flags & RETRO_FLAG_KV_MX4) != 0; }
 
 // launch_append_tokens, launch_prefill and launch_update_kv (mx4_store.hip); sources and
-// cache 16-byte aligned
+// cache 16-byte aligned.  `counters`: those of the score launch that selects behind the
+// append in the same step, set to zero by it.
 hipError_t launch_mx4_append_tokens(const Geometry& g, int step, const retro_kv_cache& c, int n_tok,
-                                    const void* k_new, const void* v_new, hipStream_t s);
+                                    const void* k_new, const void* v_new, hipStream_t s,
+                                    int32_t* counters = nullptr);
 hipError_t launch_mx4_prefill(const Geometry& g, const retro_kv_cache& c, int seq, int start, int n,
                               const void* k_src, const void* v_src, hipStream_t s);
 hipError_t launch_mx4_update_kv(const Geometry& g, const retro_kv_cache& c, int n, const void* k_upd,

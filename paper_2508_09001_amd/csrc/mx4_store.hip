@@ -32,13 +32,19 @@ template <typename T, int PS, int D>
 __global__ void __launch_bounds__(kAppendThreads) mx4_append_kernel(
     Geometry g, int step, int n_tok, char* kc, char* __restrict__ vc, T* __restrict__ dg,
     const int32_t* __restrict__ pt, int32_t* __restrict__ seq_lens, int32_t* __restrict__ A,
-    const T* __restrict__ k_new, const T* __restrict__ v_new) {
+    const T* __restrict__ k_new, const T* __restrict__ v_new, int32_t* __restrict__ counters) {
   constexpr int E = 16 / sizeof(T), LPV = D / E, VECTORS = kAppendThreads / LPV;
   constexpr int kBytes = mx4_block_bytes(PS, D), kPages = kMx4AppendTokens / PS + 1;
   __shared__ int s_phys[kPages];
   __shared__ int s_nok;
   const int b = blockIdx.x, tid = threadIdx.x, c = tid % LPV;
   const int pos0 = seq_lens[b];
+  // (the score launch leaves them at zero, but a replayed step may find what another geometry's
+  // call has left at their place)
+  if (counters)
+    for (int h = tid; h < g.hk; h += kAppendThreads)
+      __hip_atomic_store(counters + ((int64_t)b * g.hk + h) * kSelCounterInts, 0, __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
   const int lp0 = pos0 >= 0 ? pos0 / PS : 0;
   const int npages = pos0 >= 0 ? (int)(((int64_t)pos0 + n_tok - 1) / PS) - lp0 + 1 : 0;
   if (tid == 0) s_nok = pos0 >= 0 ? n_tok : 0;
@@ -168,7 +174,7 @@ hipError_t launch_rows(const Geometry& g, const retro_kv_cache& c, dim3 grid, in
 }  // namespace
 
 hipError_t launch_mx4_append_tokens(const Geometry& g, int step, const retro_kv_cache& c, int n_tok,
-                                    const void* k_new, const void* v_new, hipStream_t s) {
+                                    const void* k_new, const void* v_new, hipStream_t s, int32_t* counters) {
   const size_t tok_elems = (size_t)g.batch * g.hk * g.D;
   return with_shape(g, [&](auto t, auto ps, auto d) {
     using T = decltype(t);
@@ -176,7 +182,7 @@ hipError_t launch_mx4_append_tokens(const Geometry& g, int step, const retro_kv_
       mx4_append_kernel<T, decltype(ps)::value, decltype(d)::value><<<g.batch, kAppendThreads, 0, s>>>(
           g, step, std::min(kMx4AppendTokens, n_tok - j0), (char*)c.k_cache, (char*)c.v_cache, (T*)c.digest,
           c.page_table, c.seq_lens, c.last_loaded, (const T*)k_new + j0 * tok_elems,
-          (const T*)v_new + j0 * tok_elems);
+          (const T*)v_new + j0 * tok_elems, counters);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
