@@ -87,7 +87,8 @@ def _as_stream(stream) -> torch.cuda.Stream:
 class RetroLayer:
     """State of one layer: paged KV cache, digests, retrospective mask, selection,
     output cache, outputs and workspace, all on one device.  ``kv``: how the cache is
-    held, in the layer's ``dtype`` or as "mx4" in 4 bits (``RETRO_FLAG_KV_MX4``)."""
+    held, in the layer's ``dtype`` or as "mx4" in 4 bits, which ``RETRO_FLAG_KV_MX4`` in
+    ``flags`` asks for too."""
 
     def __init__(self, batch: int, num_kv_heads: int, group: int, head_dim: int, page_size: int,
                  budget: int, window: int, max_pages: int, dtype: str = "bf16",
@@ -100,9 +101,10 @@ class RetroLayer:
             num_phys_pages = batch * max_pages
         if kv not in ("dtype", "mx4"):
             raise ValueError('kv must be "dtype" or "mx4"')
-        self.kv = kv
-        if kv == "mx4":
+        if kv == "mx4" or flags & B.RETRO_FLAG_KV_MX4:
+            kv = "mx4"
             flags |= B.RETRO_FLAG_KV_MX4
+        self.kv = kv
         self.dims = B.Dims(batch, num_kv_heads, group, head_dim, page_size, budget, window,
                            max_pages, num_phys_pages, _RETRO_DTYPE[dtype], sm_scale,
                            budget_permille, flags, reuse_interval)
