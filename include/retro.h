@@ -355,7 +355,8 @@ retro_status retro_step_launches(const retro_dims* dims, int32_t* launches);
  * small calls for which it is the faster one); *splits = the parts of the
  * selection per KV head.  selects == 0: retro_decode_attend and the attention
  * launch of steps without a selection in front of it; else the attention of a
- * step of three launches.  Host only: nothing is enqueued. */
+ * step of three launches.  Over a cache in 4 bits *row_tiles is 1 or 2 and `selects`
+ * makes no difference.  Host only: nothing is enqueued. */
 retro_status retro_attend_plan(const retro_dims* dims, int32_t selects, int32_t* row_tiles,
                                int32_t* splits);
 
@@ -559,7 +560,8 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
 /* ---- The cache in 4 bits ---------------------------------------------------------
  * With RETRO_FLAG_KV_MX4 in dims->flags a cache's keys and values are held in 4.25 bits
  * an element (the elements and scales of the OCP Microscaling Formats specification's
- * MXFP4), for 3.8 times the tokens of bf16 in the same memory and as much less to read.  A head's
+ * MXFP4), a quarter (1 / 3.8) of bf16's bytes.  With the digests, which stay in dtype, a cache of bf16
+ * keys of 128 holds 3.2 times the tokens in the same memory with pages of 16, 3.5 with 32.  A head's
  * vector is cut into blocks of 32 elements.  A block has one exponent byte e and 32 codes: a sign bit and the
  * magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 in the order of the other three bits; an element stands for
  * its code's value times 2^(e - 127), which is exact in bf16.  Storing an element x of dtype (a key
@@ -584,8 +586,8 @@ retro_status retro_chunk_attend(const retro_dims* dims, const retro_kv_cache* ca
  * k_cache and v_cache have to be 16-byte aligned (RETRO_EINVAL).  retro_step is four or five
  * launches then (the append, the scores, the selection, which is a launch of its own for
  * large tables, the attention, combine + merge; nothing that an earlier call has left in the
- * workspace is read), and retro_chunk_attend takes bf16 rows' weights for sequences of few rows as two bf16 halves and
- * for the others as one, retro_decode_attend and retro_step as three, fp32 rows always as three. */
+ * workspace is read), and retro_chunk_attend takes bf16 rows' weights in tiles of 32 rows (always for sequences of up to
+ * 32 / G rows) as two bf16 halves and in tiles of 256 as one, retro_decode_attend and retro_step as three, fp32 rows always as three. */
 
 /* Rows of the cache as keys and values: row j of sequence b, as `chunk` lays them out, is
  * the token at position start_pos[b] + j; k_out, v_out [n_rows][h_k][d] dtype (either may

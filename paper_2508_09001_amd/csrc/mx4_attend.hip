@@ -13,8 +13,8 @@
 // codes, 62 us (187 over pages in bf16): 50 of them at 6.1 TB/s, the rest is the first keys' way and
 // the joins; a token at 32768 18.0 us (32.5), of which 4.6 are the reading, 1.6 the start of all
 // workgroups, 3.8 lengths, layout and page numbers, 1.9 the slowest wavefront's lead, 1.2 the
-// joining of eight wavefronts and 4 that of 32 parts.  8192 rows from 0 519 to 546 us on cards
-// where pages in bf16 take 500 to 510: the matrix units are busy 48 % of the cycles, the vector
+// joining of eight wavefronts and 4 that of 32 parts.  8192 rows from 0 512 to 571 us on cards
+// where pages in bf16 take 486 to 520 (91 to 95 % of their rate): the matrix units are busy 48 % of the cycles, the vector
 // units, which do the softmax and the conversion, 57 %. Two workgroups of a compute unit side by
 // side, with half of the registers and 512 shares, took 82 us for the 16 tokens and 34 for the one,
 // whose 64 parts are joined by one workgroup.

@@ -236,9 +236,11 @@ hipError_t go_tiles(const WindowCall& a, hipStream_t s) {
 // with one tile and 1.95 with two (d 128), the beginning and end of two tiles 0.3 more than those
 // of one, a further round of workgroups on a compute unit 1.2 and 4.7 (those of one tile are two
 // at a time); splits cost a combine of 2.8 us and its partials, 0.54 us a million elements.
-// These are fitted to 3159 drawn bf16 shapes, each measured with one to three tiles in 1, 2, 4 .. 32
-// splits; the choice among those is on average 0.9 % behind the best of its shape, on the shapes
-// of the fit itself.  Three tiles a workgroup were the best of 99 of 3724 draws, by 4 % on average and
+// These are fitted to 3724 draws of bf16 shapes (3159 different ones, d 64 and 128 together), each
+// measured with one to three tiles in 1, 2, 4 .. 32 splits, and serve fp32 as they are.  On other draws, the
+// choice among those splits is behind the best one of its shape by (mean, most) 0.5 and 31 %
+// for bf16 of d 128 (1031 draws), 1.4 and 24 % of d 64 (462), fp32 0.7 and 16 % of d 128 (1524), 0.5 and 13 %
+// of d 64 (709).  Three tiles a workgroup were the best of 99 of 3724 draws, by 4 % on average and
 // 12 % at most (d 64, one split), which is 0.1 % over all, and have no kernel.
 // Some choices: 16 heads of 68 rows, 128 pages, one tile in 3 splits 11.8 us (in 2 13.2, in 4 14.3,
 // in one 15.2); 128 heads of 36 rows, 64 pages, two tiles in one 16.2 (one tile 16.8); 512 heads

@@ -231,7 +231,8 @@ constexpr int kAppendThreads = 128;
 // both to codes, a block by the lanes that hold it; codes and exponents go straight to
 // their places in the page (four tokens' values side by side, so that a wavefront writes
 // 256 bytes in a row), and the digest is that of the codes' values.  21828 rows of 8 KV heads of
-// 128, 124 MB: 28 us, 34 with the instructions of norm and rotation where there is neither.
+// 128, 124 MB: 28 us, 34 with the instructions of norm and rotation where there is neither, 44 with
+// both at work on keys (over pages in bf16 47; fp32 57 and 84).
 template <typename T, int PS, int D, bool MX4>
 __global__ void __launch_bounds__(kAppendThreads) append_rotary_kernel(
     Geometry g, int step, retro_chunk ch, retro_rotary r, char* __restrict__ kc, char* __restrict__ vc,
